@@ -57,7 +57,8 @@ typedef enum {
     SASQ_ERR_WORKSPACE = 3,     /* workspace NULL or smaller than the matching *_workspace() query */
     SASQ_ERR_BAD_SCALE = 4,     /* device-detected: factor is 0, NaN, Inf or has a non-finite reciprocal */
     SASQ_ERR_TIMEOUT = 5,       /* device-detected: a bounded wait inside a kernel gave up */
-    SASQ_ERR_CUDA = 6           /* a CUDA runtime / driver call failed */
+    SASQ_ERR_CUDA = 6,          /* a CUDA runtime / driver call failed */
+    SASQ_ERR_BAD_INDEX = 7      /* device-detected: a page, length or position outside its range; the access was skipped */
 } sasq_status_t;
 
 typedef enum { SASQ_F16 = 0, SASQ_BF16 = 1 } sasq_dtype_t;
@@ -344,6 +345,88 @@ SASQ_API int sasq_static_w8a8_linear_multi_launches(int count, const sasq_linear
 SASQ_API int sasq_static_w8a8_linear_tiles(int64_t T, int64_t N, int num_pairs, int pair_id, int32_t* tiles_host,
                                            int cap);
 
+/* ---- Paged key/value cache: what lies between the q/k/v and the o linears of a decoder layer when serving ----
+ *
+ * A cache is a pool of pages; a page holds `page_size` consecutive positions of ONE sequence, for every KV head.
+ * Element (page, row, head, d) of K or V lies at
+ *   base + page * page_stride + row * token_stride + head * head_stride + d                (strides in elements)
+ * so both orders of a page, tokens first and heads first, are expressed by the strides.  K and V share the strides. */
+typedef enum { SASQ_KV_16BIT = 0,   /* elements of the activations' dtype */
+               SASQ_KV_INT8 = 1     /* int8 codes (Eq. 1, b = 8) under one static factor per KV head */
+} sasq_kv_kind_t;
+
+/* The cache (host struct; the pointers are device pointers, 16-byte aligned; the strides are multiples of 16 bytes). */
+typedef struct {
+    void* k;
+    void* v;
+    const float* k_scale;       /* [num_kv_heads] factors of the codes (SASQ_KV_INT8), else NULL */
+    const float* v_scale;
+    int64_t page_stride, token_stride, head_stride;
+    int64_t num_pages;
+    int32_t page_size;          /* positions per page: 16, 32, 64, 128 or 256 */
+    int32_t num_kv_heads;
+    int32_t head_dim;
+    int32_t kind;               /* sasq_kv_kind_t */
+} sasq_kv_cache_t;
+
+/* The sequences of a call (host struct; the arrays are int32 in DEVICE memory and are read when the kernels run, so
+ * a captured call follows their values).  The new tokens of all sequences lie one after another in q / k / v / out:
+ * sequence b owns rows q_starts[b] ... q_starts[b+1] - 1 (q_starts ascends from >= 0; rows from q_starts[batch] on are
+ * padding, neither read nor written).  New token i of a sequence with n new tokens has position
+ *   p = seq_lens[b] - n + i
+ * and lives in row p % page_size of page page_table[b][p / page_size].  A token with p < 0 has no place: it is not
+ * appended and sees no key. */
+typedef struct {
+    const int32_t* page_table;  /* [batch][page_table_stride] */
+    const int32_t* seq_lens;    /* [batch] keys of the sequence, the new tokens' included */
+    const int32_t* q_starts;    /* [batch + 1] */
+    int64_t page_table_stride;
+    int32_t batch;
+    int32_t max_pages;          /* usable entries of a row of page_table */
+    int32_t total_q;            /* rows of q / k / v / out */
+    int32_t max_q_len;          /* upper bounds of the new tokens and of the keys of a sequence, known to the host: */
+    int32_t max_seq_len;        /* they choose launch shapes only; results do not depend on them */
+    int32_t reserved;           /* must be 0 */
+} sasq_kv_batch_t;
+
+/* Appends the new tokens' keys and values to the cache and applies the position rotation to q and k on the way
+ * (one launch).  With (a, b) = elements (j, j + rot_dim / 2) of a head, or (2j, 2j + 1) when `interleaved`, and
+ * c = cos_sin[p][j], s = cos_sin[p][rot_dim / 2 + j], j < rot_dim / 2:
+ *   a' = fl32(fl32(a c) - fl32(b s)),   b' = fl32(fl32(b c) + fl32(a s))         (fp32, no fused multiply-add)
+ * Elements from rot_dim on, and all of v, pass unchanged.  16-bit destinations get one narrowing; an int8 cache gets
+ * the code of Eq. 1 of the fp32 value, with s = k_scale[head] or v_scale[head].
+ * q: [total_q, num_q_heads, head_dim] of `dt`, row t at q + t * q_stride elements, heads contiguous; k, v: the same
+ * with num_kv_heads.  q_out: the rotated q (rows at q_out_stride); may alias q.  q == q_out == NULL: keys and values
+ * only.  cos_sin: [max_positions, rot_dim] fp32.  Strides are multiples of 8 elements, pointers 16-byte aligned.
+ * head_dim: a multiple of 16 up to 256.  rot_dim: a multiple of 16 up to head_dim (0: no rotation, cos_sin unused).
+ * A position outside cos_sin or the page table, or a page outside the cache, is not written (its q_out rows become
+ * +0) and sets SASQ_ERR_BAD_INDEX; a factor that Eq. 1 cannot use sets SASQ_ERR_BAD_SCALE.  Two new tokens of one call
+ * must not share a cache row. */
+SASQ_API int sasq_rope_kv_append(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, const void* q,
+                                 const void* k, const void* v, void* q_out, int64_t q_stride, int64_t k_stride,
+                                 int64_t v_stride, int64_t q_out_stride, int num_q_heads, const float* cos_sin,
+                                 int64_t max_positions, int rot_dim, int interleaved, int dt, void* stream);
+
+/* Bytes of scratch sasq_paged_attention needs for these shapes (0 for arguments the call itself would refuse). */
+SASQ_API size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch,
+                                               int num_q_heads);
+
+/* Attention of the new tokens over their sequences' cached keys.  Query head c reads KV head c / (num_q_heads /
+ * num_kv_heads).  Token i of sequence b sees the first  causal ? p + 1 : seq_lens[b]  keys:
+ *   s_j = softmax_scale * <q, k_j>,   lse = log sum_j exp(s_j),   out = sum_j exp(s_j - lse) v_j
+ * (for an int8 cache k_j, v_j are code * factor).  A token that sees no key gets out = +0 and lse = -inf.  What the
+ * cache holds past a sequence's keys (NaN included) does not matter.  Logits, maxima, sums and accumulators are fp32;
+ * the probabilities are rounded once to `dt` as operands of the second product.  Bit-identical from run to run.
+ * q: as for sasq_rope_kv_append (already rotated); out: [total_q, num_q_heads, head_dim] of `dt`, rows at out_stride;
+ * must not alias q.  lse: [total_q, num_q_heads] fp32 (natural logarithm) or NULL.  head_dim: 64 or 128.
+ * workspace: >= sasq_paged_attention_workspace() bytes, 16-byte aligned, contents need no initialisation; calls that
+ * share one must be ordered on the stream.  A page or length outside its range sets SASQ_ERR_BAD_INDEX (out
+ * unspecified for that sequence). */
+SASQ_API int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, const void* q,
+                                  void* out, float* lse, int64_t q_stride, int64_t out_stride, int num_q_heads,
+                                  float softmax_scale, int causal, int dt, void* workspace, size_t ws_bytes,
+                                  void* stream);
+
 /* ---- PTQ initialisation (Sec. 4.1), set-up only, not on the hot path ---- */
 
 /* Bytes of scratch sasq_absmax_scale needs. */
@@ -421,7 +504,7 @@ SASQ_API int sasq_debug_int8_issue_rate(int mma_per_pair, int n_cols, double* op
                                         double* mac_per_clk_sm_host, void* stream);
 
 /* Synchronises `stream`, returns the sticky device status word of the current
- * device (SASQ_OK, SASQ_ERR_BAD_SCALE or SASQ_ERR_TIMEOUT) and clears it. */
+ * device (SASQ_OK, SASQ_ERR_BAD_SCALE, SASQ_ERR_TIMEOUT or SASQ_ERR_BAD_INDEX) and clears it. */
 SASQ_API int sasq_device_status(void* stream);
 
 #ifdef __cplusplus

@@ -28,6 +28,8 @@ __all__ = [
     "sasq_fakequant_linear_fp_weights", "sasq_absmax_scale_per_channel", "sasq_running_mean", "LinearDesc", "sasq_static_w8a8_linear_multi_workspace",
     "sasq_static_w8a8_linear_multi", "sasq_static_w8a8_linear_multi_launches", "sasq_set_gang_launch",
     "sasq_debug_int8_issue_rate", "LinearProblems", "QuantTensors",
+    "SASQ_KV_16BIT", "SASQ_KV_INT8", "KVCacheStruct", "KVBatchStruct", "KVCache", "PagedBatch", "sasq_rope_kv_append",
+    "sasq_paged_attention_workspace", "sasq_paged_attention",
 ]
 
 SASQ_F16 = 0
@@ -35,6 +37,8 @@ SASQ_BF16 = 1
 SASQ_FULL_OPERATOR = 0
 SASQ_WITHOUT_ROUND = 1
 SASQ_WITHOUT_CLAMP = 2
+SASQ_KV_16BIT = 0
+SASQ_KV_INT8 = 1
 
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -67,6 +71,22 @@ class LinearDesc(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
                 ("x_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("y", ctypes.c_void_p),
                 ("T", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64)]
+
+
+class KVCacheStruct(ctypes.Structure):
+    """Mirror of sasq_kv_cache_t."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("kind", ctypes.c_int32)]
+
+
+class KVBatchStruct(ctypes.Structure):
+    """Mirror of sasq_kv_batch_t."""
+    _fields_ = [("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("q_starts", ctypes.c_void_p),
+                ("page_table_stride", ctypes.c_int64), ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("total_q", ctypes.c_int32), ("max_q_len", ctypes.c_int32), ("max_seq_len", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -150,6 +170,13 @@ def load_library() -> ctypes.CDLL:
     L.sasq_absmax_scale.argtypes = [vp, i64, i32, i32, vp, vp, sz, vp]
     L.sasq_quantize_weight.restype = i32
     L.sasq_quantize_weight.argtypes = [vp, vp, vp, i64, i64, i32, vp]
+    cache_p, batch_p = ctypes.POINTER(KVCacheStruct), ctypes.POINTER(KVBatchStruct)
+    L.sasq_rope_kv_append.restype = i32
+    L.sasq_rope_kv_append.argtypes = [cache_p, batch_p, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, i64, i32, i32, i32, vp]
+    L.sasq_paged_attention_workspace.restype = sz
+    L.sasq_paged_attention_workspace.argtypes = [cache_p, batch_p, i32]
+    L.sasq_paged_attention.restype = i32
+    L.sasq_paged_attention.argtypes = [cache_p, batch_p, vp, vp, vp, i64, i64, i32, f32, i32, i32, vp, sz, vp]
     _lib = L
     return L
 
@@ -687,3 +714,128 @@ def sasq_fakequant_fwd_bwd_static(x, grad_y, y, grad_x, grad_scale, scale, bits:
                                                         _ptr(grad_scale), int(bool(accumulate)), x.numel(), _dt(x),
                                                         _ptr(scale), int(bits), _stream(stream)),
            "sasq_fakequant_fwd_bwd_static")
+
+
+# ---------------------------------------------------------------------------
+# paged key/value cache
+# ---------------------------------------------------------------------------
+class KVCache:
+    """A paged cache, marshalled once (see LinearProblems).  k, v: [num_pages, page_size, num_kv_heads, head_dim] views
+    of one stride pattern, last dimension contiguous (a pool stored heads first is passed as its .transpose(1, 2));
+    fp16 / bf16, or int8 with k_scale, v_scale: [num_kv_heads] fp32 factors.  Holds references to the tensors."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        for name, t in (("k", k), ("v", v)):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise TypeError(f"{name} must be a CUDA tensor")
+            if t.dim() != 4 or t.stride(3) != 1:
+                raise ValueError(f"{name} must be [num_pages, page_size, num_kv_heads, head_dim] with a contiguous last "
+                                 "dimension")
+            if t.dtype not in (torch.int8, torch.float16, torch.bfloat16):
+                raise TypeError(f"{name} must be int8, float16 or bfloat16, got {t.dtype}")
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must share shape, strides, dtype and device")
+        int8 = k.dtype == torch.int8
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if int8 != (t is not None):
+                raise ValueError(f"{name} goes with an int8 cache, and only with it")
+            if t is not None:
+                _dev(t, name, torch.float32)
+                if t.numel() != k.shape[2]:
+                    raise ValueError(f"{name} must hold one factor per KV head")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.num_kv_heads, self.head_dim, self.dtype = k.shape[2], k.shape[3], k.dtype
+        self.struct = KVCacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.stride(0), k.stride(1), k.stride(2),
+                                    k.shape[0], k.shape[1], k.shape[2], k.shape[3],
+                                    SASQ_KV_INT8 if int8 else SASQ_KV_16BIT)
+        self.ref = ctypes.byref(self.struct)
+
+
+class PagedBatch:
+    """The sequences of a call, marshalled once: page_table [batch, max_pages], seq_lens [batch], q_starts [batch + 1],
+    int32 CUDA tensors whose VALUES may change between calls; total_q rows of q; upper bounds of a sequence's new tokens
+    and keys, known to the host (default: total_q, and what the page table can hold)."""
+
+    def __init__(self, page_table, seq_lens, q_starts, total_q: int, max_q_len: int | None = None,
+                 max_seq_len: int | None = None):
+        if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype != torch.int32:
+            raise TypeError("page_table must be an int32 CUDA tensor")
+        if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be [batch, max_pages] with contiguous rows")
+        _dev(seq_lens, "seq_lens", torch.int32); _dev(q_starts, "q_starts", torch.int32)
+        B, max_pages = page_table.shape
+        if seq_lens.numel() != B or q_starts.numel() != B + 1:
+            raise ValueError("seq_lens must be [batch] and q_starts [batch + 1]")
+        self.page_table, self.seq_lens, self.q_starts = page_table, seq_lens, q_starts
+        self.total_q = int(total_q)
+        longest = 0x7FFFFFFF if max_seq_len is None else int(max_seq_len)
+        self.struct = KVBatchStruct(_ptr(page_table), _ptr(seq_lens), _ptr(q_starts), max(page_table.stride(0), max_pages),
+                                    B, max_pages, self.total_q, self.total_q if max_q_len is None else int(max_q_len),
+                                    longest, 0)
+        self.ref = ctypes.byref(self.struct)
+
+
+def _heads(t, name: str, dtype, total: int, heads: int | None, dim: int):
+    """[total, heads, dim] with each row's heads contiguous; returns (heads, row stride)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != total or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} must be [{total}, {'heads' if heads is None else heads}, {dim}]")
+    if stride[2] != 1 or (shape[1] > 1 and stride[1] != dim):
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
+    return shape[1], (stride[0] if total > 1 else max(stride[0], shape[1] * dim))
+
+
+def sasq_rope_kv_append(cache: KVCache, batch: PagedBatch, q, k, v, q_out, cos_sin, interleaved: bool = False,
+                        stream=None) -> None:
+    """Appends k, v [total_q, num_kv_heads, head_dim] to the cache with the rotation of cos_sin [max_positions, rot_dim]
+    fp32 (None: no rotation) applied to k, and to q [total_q, num_q_heads, head_dim] -> q_out (both None: skip)."""
+    T, K, D = batch.total_q, cache.num_kv_heads, cache.head_dim
+    dt = _dt(k)
+    if cache.dtype is not torch.int8 and cache.dtype != k.dtype:
+        raise TypeError(f"k must have the cache's dtype {cache.dtype}")
+    _, ks = _heads(k, "k", k.dtype, T, K, D)
+    _, vs = _heads(v, "v", k.dtype, T, K, D)
+    H = qs = qos = 0
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        H, qs = _heads(q, "q", k.dtype, T, None, D)
+        _, qos = _heads(q_out, "q_out", k.dtype, T, H, D)
+    positions = rot = 0
+    if cos_sin is not None:
+        _dev(cos_sin, "cos_sin", torch.float32)
+        if cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be [max_positions, rot_dim]")
+        positions, rot = cos_sin.shape
+    _check(load_library().sasq_rope_kv_append(cache.ref, batch.ref, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), qs, ks, vs, qos,
+                                              H, _ptr(cos_sin), positions, rot, int(bool(interleaved)), dt,
+                                              _stream(stream)), "sasq_rope_kv_append")
+
+
+def sasq_paged_attention_workspace(cache: KVCache, batch: PagedBatch, num_q_heads: int) -> int:
+    return int(load_library().sasq_paged_attention_workspace(cache.ref, batch.ref, int(num_q_heads)))
+
+
+def sasq_paged_attention(cache: KVCache, batch: PagedBatch, q, out, workspace, lse=None, scale: float | None = None,
+                         causal: bool = True, stream=None) -> None:
+    """Attention of q [total_q, num_q_heads, head_dim] over the cache -> out of the same shape, lse [total_q, num_q_heads]
+    fp32 or None; scale defaults to head_dim ** -0.5."""
+    T, D = batch.total_q, cache.head_dim
+    dt = _dt(q)
+    if cache.dtype is not torch.int8 and cache.dtype != q.dtype:
+        raise TypeError(f"q must have the cache's dtype {cache.dtype}")
+    H, qs = _heads(q, "q", q.dtype, T, None, D)
+    _, os_ = _heads(out, "out", q.dtype, T, H, D)
+    if lse is not None:
+        _dev(lse, "lse", torch.float32)
+        if tuple(lse.shape) != (T, H):
+            raise ValueError("lse must be [total_q, num_q_heads]")
+    _dev(workspace, "workspace")
+    _check(load_library().sasq_paged_attention(cache.ref, batch.ref, _ptr(q), _ptr(out), _ptr(lse), qs, os_, H,
+                                               D ** -0.5 if scale is None else float(scale), int(bool(causal)), dt,
+                                               _ptr(workspace), _nbytes(workspace), _stream(stream)),
+           "sasq_paged_attention")

@@ -5,6 +5,7 @@ namespace sasq {
 
 int fakequant_status_read_and_clear(cudaStream_t st);
 int linear_status_read_and_clear(cudaStream_t st);
+int paged_status_read_and_clear(cudaStream_t st);
 
 int device_sm_count_if_sm100() {
     // cached per device ordinal; 0 = not queried yet, -1 = not sm_100
@@ -32,6 +33,7 @@ const char* sasq_status_string(int status) {
         case SASQ_ERR_BAD_SCALE: return "SASQ_ERR_BAD_SCALE: a quantization factor is zero or not finite";
         case SASQ_ERR_TIMEOUT: return "SASQ_ERR_TIMEOUT: a bounded wait inside a kernel gave up";
         case SASQ_ERR_CUDA: return "SASQ_ERR_CUDA: a CUDA call failed";
+        case SASQ_ERR_BAD_INDEX: return "SASQ_ERR_BAD_INDEX: a page, length or position outside its range";
         default: return "unknown SASQ status";
     }
 }
@@ -40,7 +42,8 @@ int sasq_device_status(void* stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int a = sasq::fakequant_status_read_and_clear(st);
     const int b = sasq::linear_status_read_and_clear(st);
-    return a > b ? a : b;
+    const int c = sasq::paged_status_read_and_clear(st);
+    return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
 }  // extern "C"

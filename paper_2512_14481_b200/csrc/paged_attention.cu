@@ -1,0 +1,159 @@
+// sasq_paged_attention: host side, and the kernels' instantiations.
+#include "paged_rows.cuh"
+
+namespace sasq {
+
+SASQ_DEFINE_STATUS_WORD(g_paged_status)
+
+int paged_status_read_and_clear(cudaStream_t st) { return g_paged_status_read_and_clear(st); }
+
+int* paged_status_ptr() {
+    static int* cache[64] = {nullptr};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    if (cache[dev] == nullptr) {
+        int* p = nullptr;
+        if (cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_paged_status) != cudaSuccess) return nullptr;
+        cache[dev] = p;
+    }
+    return cache[dev];
+}
+
+namespace {
+
+constexpr int kMaxSms = 256;
+
+struct Layout {
+    size_t ml, o, total;        // byte offsets behind the part items
+};
+Layout layout_of(int blocks, int R, int D) {
+    Layout l;
+    l.ml = (size_t)blocks * sizeof(PartItem);
+    l.o = l.ml + (size_t)2 * blocks * R * sizeof(float2);
+    l.total = l.o + (size_t)2 * blocks * R * D * sizeof(float);
+    return l;
+}
+
+struct Plan {
+    int nb;                     // few-row kernel: blocks of 8 rows
+    int blocks;
+    int R, unit;
+};
+
+int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
+    Plan pl{};
+    const long long rows = (long long)b->max_q_len * (heads / c->num_kv_heads);
+    pl.nb = rows <= 8 ? 1 : 2;
+    pl.R = 8 * pl.nb;
+    pl.unit = kRowsUnit;
+    const long long items = (long long)b->batch * c->num_kv_heads * (rows < 1 ? 1 : ceil_div(rows, pl.R));
+    const long long most = items * (b->max_seq_len < 1 ? 1 : ceil_div(b->max_seq_len, pl.unit));
+    const bool int8 = c->kind == SASQ_KV_INT8, d128 = c->head_dim == 128;
+    const int per_sm = pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
+                                          : (int8 ? kRowsBlocksPerSm<64, 1, true> : kRowsBlocksPerSm<64, 1, false>))
+                                  : kRowsBlocksPerSm<128, 2, false>;
+    const long long fill = (long long)sms * per_sm;
+    pl.blocks = (int)(most < fill ? (most < 1 ? 1 : most) : fill);
+    return pl;
+}
+
+int attend_check(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, int num_q_heads, int dt, PagedParams* p) {
+    const int rc = paged_check(cache, batch, dt, p);
+    if (rc != SASQ_OK) return rc;
+    if (num_q_heads <= 0 || num_q_heads % cache->num_kv_heads != 0) return SASQ_ERR_INVALID_ARG;
+    if (cache->head_dim != 64 && cache->head_dim != 128) return SASQ_ERR_UNSUPPORTED;
+    if ((long long)batch->total_q * (num_q_heads / cache->num_kv_heads) > 0x7FFFFFFF) return SASQ_ERR_UNSUPPORTED;
+    return SASQ_OK;
+}
+
+template <typename Kernel>
+cudaError_t launch(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, const AttendParams& p) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = pdl_attribute();
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+template <int D, int NB, bool BF>
+cudaError_t launch_rows(const AttendParams& p, bool int8, cudaStream_t st) {
+    const cudaError_t e = int8 ? launch(paged_rows_kernel<D, NB, BF, true>, dim3(p.max_blocks), kRowsThreads, 0, st, p)
+                               : launch(paged_rows_kernel<D, NB, BF, false>, dim3(p.max_blocks), kRowsThreads, 0, st, p);
+    if (e != cudaSuccess || !p.split) return e;
+    return launch(paged_join_kernel<8 * NB, D, BF>, dim3(p.max_blocks, NB), 256, 0, st, p);
+}
+
+template <int D, bool BF>
+cudaError_t launch_all(const Plan& pl, const AttendParams& p, bool int8, cudaStream_t st) {
+    return pl.nb == 1 ? launch_rows<D, 1, BF>(p, int8, st) : launch_rows<D, 2, BF>(p, int8, st);
+}
+
+}  // namespace
+}  // namespace sasq
+
+extern "C" {
+
+size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, int num_q_heads) {
+    using namespace sasq;
+    PagedParams p{};
+    if (attend_check(cache, batch, num_q_heads, SASQ_BF16, &p) != SASQ_OK) return 0;
+    const Plan pl = make_plan(cache, batch, num_q_heads, kMaxSms);
+    return layout_of(pl.blocks, pl.R, cache->head_dim).total;
+}
+
+int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, const void* q, void* out, float* lse,
+                         int64_t q_stride, int64_t out_stride, int num_q_heads, float softmax_scale, int causal, int dt,
+                         void* workspace, size_t ws_bytes, void* stream) {
+    using namespace sasq;
+    AttendParams p{};
+    const int rc = attend_check(cache, batch, num_q_heads, dt, &p.c);
+    if (rc != SASQ_OK) return rc;
+    const int64_t row = (int64_t)num_q_heads * cache->head_dim;
+    if (!(softmax_scale == softmax_scale) || softmax_scale - softmax_scale != 0.0f) return SASQ_ERR_INVALID_ARG;
+    if (batch->total_q > 0) {
+        if (q == nullptr || out == nullptr || !aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) || q == out)
+            return SASQ_ERR_INVALID_ARG;
+        if (q_stride < row || out_stride < row || q_stride % 8 != 0 || out_stride % 8 != 0) return SASQ_ERR_INVALID_ARG;
+    }
+    if (batch->total_q == 0 || batch->batch == 0) return SASQ_OK;
+    if (workspace == nullptr || !aligned16(workspace) || ws_bytes < sasq_paged_attention_workspace(cache, batch, num_q_heads))
+        return SASQ_ERR_WORKSPACE;
+    const int sms = device_sm_count_if_sm100();
+    if (sms <= 0 || sms > kMaxSms) return SASQ_ERR_UNSUPPORTED;
+    p.c.status = paged_status_ptr();
+    if (p.c.status == nullptr) return SASQ_ERR_CUDA;
+    const Plan pl = make_plan(cache, batch, num_q_heads, sms);
+    const Layout l = layout_of(pl.blocks, pl.R, cache->head_dim);
+    p.q = static_cast<const uint16_t*>(q);
+    p.out = static_cast<uint16_t*>(out);
+    p.lse = lse;
+    p.q_stride = q_stride;
+    p.out_stride = out_stride;
+    p.heads = num_q_heads;
+    p.group = num_q_heads / cache->num_kv_heads;
+    p.scale = softmax_scale * 1.4426950408889634f;
+    p.causal = causal != 0;
+    // no item has more than one unit when the host's bound says so: nothing to cut, no joining launch
+    p.split = batch->max_seq_len > pl.unit;
+    p.max_blocks = pl.blocks;
+    p.min_units = 1;
+    p.part_items = static_cast<PartItem*>(workspace);
+    p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + l.ml);
+    p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.o);
+    const bool int8 = cache->kind == SASQ_KV_INT8;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    if (cache->head_dim == 128)
+        e = dt == SASQ_BF16 ? launch_all<128, true>(pl, p, int8, st) : launch_all<128, false>(pl, p, int8, st);
+    else
+        e = dt == SASQ_BF16 ? launch_all<64, true>(pl, p, int8, st) : launch_all<64, false>(pl, p, int8, st);
+    return e == cudaSuccess ? SASQ_OK : SASQ_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,259 @@
+// Shared by the paged-cache kernels: the launch parameters, the lookup of a sequence, the division of an attention
+// call's work among its thread blocks, and the int8 codes' conversion.
+#pragma once
+
+#include "common.cuh"
+
+namespace sasq {
+
+int* paged_status_ptr();    // device address of the paged kernels' sticky status word; nullptr if it cannot be had
+
+// What both operators know about the cache and the batch (all sizes validated on the host).
+struct PagedParams {
+    void* k;
+    void* v;
+    const float* k_scale;
+    const float* v_scale;
+    long long page_stride, token_stride, head_stride;     // elements
+    long long num_pages;
+    const int* page_table;
+    const int* seq_lens;
+    const int* q_starts;
+    long long table_stride;
+    int batch, max_pages, total_q;
+    int page_shift;             // log2(page_size)
+    int kv_heads;
+    int* status;
+};
+
+// Host checks common to both operators; fills the shared parameters.
+int paged_check(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int dt, PagedParams* p);
+
+namespace {
+
+// A sequence's new tokens and keys as the device arrays give them, cut to what is safe to touch.
+struct Sequence {
+    int first, new_len, len;
+};
+__device__ __forceinline__ Sequence load_sequence(const PagedParams& p, int b) {
+    Sequence s;
+    const int q0 = p.q_starts[b], q1 = p.q_starts[b + 1];
+    int len = p.seq_lens[b];
+    const long long room = (long long)p.max_pages << p.page_shift;
+    const bool bad = q0 < 0 || q1 < q0 || q1 > p.total_q || len < 0 || len > room;
+    if (bad) atomicMax(p.status, (int)SASQ_ERR_BAD_INDEX);
+    s.first = q0;
+    s.new_len = (q0 < 0 || q1 < q0 || q1 > p.total_q) ? 0 : q1 - q0;
+    s.len = len < 0 ? 0 : (len > room ? (int)room : len);
+    return s;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Work of an attention call.  The rows of one KV head are (new token, query head of the group) pairs, token first; R
+// consecutive rows of a sequence and KV head are an item, and an item's keys are walked in units of KT.  The units of
+// all items, laid end to end (sequence, KV head, item, key), are cut into equal stretches, one per thread block: every
+// block has the same number of units whatever the lengths are, a block walks whole items in the middle of its stretch
+// and at most two part items at its ends.  Part items leave (O, m, l) in the workspace, and a second launch joins them.
+// A split by whole items alone would leave most SMs idle for few long sequences, and a fixed number of splits per item
+// makes the longest sequence of a ragged batch the tail.
+// ---------------------------------------------------------------------------------------------------------------------
+struct Item {
+    int b, h, i;              // sequence, KV head, row tile
+    Sequence s;
+    int units;                // of the whole item
+    int t0, t1;               // this block's units
+    long long first_unit;     // of the item, in the whole call
+};
+
+template <int R, int KT>
+struct Schedule {
+    int group, causal, heads, batch;
+
+    __device__ __forceinline__ int tiles(const Sequence& s) const { return (int)(((long long)s.new_len * group + R - 1) / R); }
+    // keys that the rows of tile i can see at most
+    __device__ __forceinline__ int key_limit(const Sequence& s, int i) const {
+        if (!causal) return s.len;
+        const long long rows = (long long)s.new_len * group;
+        long long last = (long long)(i + 1) * R;
+        last = (last < rows ? last : rows) - 1;
+        const long long lim = (long long)s.len - s.new_len + last / group + 1;
+        return lim < 0 ? 0 : (int)lim;
+    }
+    // an item without keys still counts one unit: its rows have to be written
+    __device__ __forceinline__ int units(const Sequence& s, int i) const {
+        const int n = (key_limit(s, i) + KT - 1) / KT;
+        return n < 1 ? 1 : n;
+    }
+    __device__ __forceinline__ long long head_units(const Sequence& s) const {
+        const int n = tiles(s);
+        if (n == 0) return 0;
+        if (!causal) return (long long)n * units(s, 0);
+        long long sum = 0;
+        for (int i = 0; i < n; ++i) sum += units(s, i);
+        return sum;
+    }
+};
+
+// First unit of block c when `total` units go to n blocks.
+__device__ __forceinline__ long long block_begin(long long total, int c, int n) { return total * c / n; }
+// The block that has unit x.
+__device__ __forceinline__ int block_of(long long total, long long x, int n) { return (int)(((x + 1) * n + total - 1) / total) - 1; }
+
+// Where a block's stretch begins; found by the whole block together.
+struct Start {
+    long long total;          // units of the call
+    long long begin, end;     // this block's
+    long long offset;         // of `begin` in sequence b
+    int b;
+    int blocks;               // blocks that have work
+};
+
+// Every thread of the block calls this; scratch: one long long per warp + one Start, in shared memory.
+template <int THREADS, int R, int KT>
+__device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule<R, KT>& sch, int max_blocks, int min_units,
+                                            long long* scratch, Start* found) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.batch + THREADS - 1) / THREADS;
+    const int b0 = tid * per, b1 = min(b0 + per, p.batch);
+    long long mine = 0;
+    for (int b = b0; b < b1; ++b) mine += sch.head_units(load_sequence(p, b)) * sch.heads;
+    long long incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const long long other = __shfl_up_sync(0xFFFFFFFFu, incl, off);
+        if (lane >= off) incl += other;
+    }
+    if (lane == 31) scratch[warp] = incl;
+    if (tid == 0) found->b = -1;
+    __syncthreads();
+    long long before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        const long long s = scratch[w];
+        before += w < warp ? s : 0;
+        total += s;
+    }
+    long long at = before + incl - mine;
+    const long long want = total / min_units;
+    const int blocks = want < 1 ? 1 : want < max_blocks ? (int)want : max_blocks;
+    const int c = blockIdx.x;
+    const long long begin = c < blocks ? block_begin(total, c, blocks) : total;
+    if (begin >= at && begin < at + mine) {
+        for (int b = b0; b < b1; ++b) {
+            const long long n = sch.head_units(load_sequence(p, b)) * sch.heads;
+            if (begin < at + n) {
+                found->b = b;
+                found->offset = begin - at;
+                break;
+            }
+            at += n;
+        }
+    }
+    __syncthreads();
+    Start st;
+    st.total = total;
+    st.blocks = blocks;
+    st.begin = begin;
+    st.end = c < blocks ? block_begin(total, c + 1, blocks) : total;
+    st.b = found->b;
+    st.offset = st.b >= 0 ? found->offset : 0;
+    return st;
+}
+
+// Walks the items of a block's stretch; every thread keeps its own copy.
+template <int R, int KT>
+struct Walk {
+    Schedule<R, KT> sch;
+    Item it;
+    long long at, end;
+    int n_tiles;
+    bool split;
+
+    // split == false: items are not cut, an item belongs to the block in whose stretch it begins
+    __device__ __forceinline__ bool begin(const PagedParams& p, const Schedule<R, KT>& s, const Start& st, bool may_split) {
+        sch = s;
+        split = may_split;
+        at = st.begin;
+        end = st.end;
+        if (st.b < 0 || at >= end) return false;
+        it.b = st.b;
+        it.s = load_sequence(p, it.b);
+        n_tiles = sch.tiles(it.s);
+        const long long per_head = sch.head_units(it.s);
+        it.h = (int)(st.offset / per_head);
+        long long rest = st.offset - it.h * per_head;
+        it.i = 0;
+        for (;;) {
+            it.units = sch.units(it.s, it.i);
+            if (rest < it.units) break;
+            rest -= it.units;
+            ++it.i;
+        }
+        it.first_unit = at - rest;
+        it.t0 = (int)rest;
+        it.t1 = split ? (int)min((long long)it.units, rest + (end - at)) : it.units;
+        return (split || rest == 0) ? true : next(p);
+    }
+    __device__ __forceinline__ bool next(const PagedParams& p) {
+        at += it.t1 - it.t0;
+        if (at >= end) return false;
+        if (++it.i == n_tiles) {
+            it.i = 0;
+            if (++it.h == sch.heads) {
+                it.h = 0;
+                do {
+                    if (++it.b >= p.batch) return false;      // cannot happen while at < end
+                    it.s = load_sequence(p, it.b);
+                    n_tiles = sch.tiles(it.s);
+                } while (n_tiles == 0);
+            }
+        }
+        it.units = sch.units(it.s, it.i);
+        it.first_unit = at;
+        it.t0 = 0;
+        it.t1 = split ? (int)min((long long)it.units, end - at) : it.units;
+        return true;
+    }
+};
+
+// What the joining launch has to know of an item that starts in block c and ends in another (last < 0: there is none).
+struct PartItem {
+    int last;                 // the block that has the item's end
+    int h;
+    int first_row;            // of the item, among the (token, group head) rows of its sequence
+    int rows;
+    int first_token;          // of the sequence, in q
+    int pad[3];
+};
+
+// ---------------------------------------------------------------------------------------------------------------------
+// int8 codes -> pairs of 16-bit floats, exactly.
+//   bf16: with b the code's byte, 0x4300 | (b & 0x7F) stands for 128 + (b & 0x7F) and 0x4300 | (b & 0x80) for 128 or 256,
+//         and their difference is the code (two's complement: low seven bits less 128 times the sign bit);
+//   f16:  u = b ^ 0x80 = code + 128, 0x6400 | u stands for 1024 + u, less 1152.
+// `which` picks bytes (0, 1) or (2, 3) of the word.
+// ---------------------------------------------------------------------------------------------------------------------
+template <bool BF, int which>
+__device__ __forceinline__ uint32_t codes_to_pair(uint32_t w) {
+    if constexpr (BF) {
+        const uint32_t t = __byte_perm(w, 0x43434343u, which == 0 ? 0x4140 : 0x4342);
+        const uint32_t a = t & 0xFF7FFF7Fu, s = t & 0xFF80FF80u;
+        const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&s));
+        return *reinterpret_cast<const uint32_t*>(&d);
+    } else {
+        const uint32_t t = __byte_perm(w ^ 0x80808080u, 0x64646464u, which == 0 ? 0x4140 : 0x4342);
+        const uint32_t s = 0x64806480u;
+        const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&t), *reinterpret_cast<const __half2*>(&s));
+        return *reinterpret_cast<const uint32_t*>(&d);
+    }
+}
+
+// 2^x by the hardware's approximation (2^-inf = 0)
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+}  // namespace
+}  // namespace sasq

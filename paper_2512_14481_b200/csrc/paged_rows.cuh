@@ -1,0 +1,429 @@
+// Attention for few query rows per KV head (decode steps, drafts): at most 8 * NB rows an item.
+#pragma once
+
+#include "paged_common.cuh"
+
+namespace sasq {
+
+struct AttendParams {
+    PagedParams c;
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;                 // [total_q][heads] or nullptr
+    long long q_stride, out_stride;
+    int heads, group;           // query heads, query heads per KV head
+    float scale;                // softmax_scale * log2(e)
+    int causal;
+    int split;                  // items may be cut among blocks (the joining launch follows)
+    int max_blocks, min_units;
+    PartItem* part_items;       // [max_blocks]
+    float2* part_ml;            // [2 * max_blocks][R]: maximum (log2 units) and sum
+    float* part_o;              // [2 * max_blocks][R][D]
+    long long wait_limit;
+};
+
+namespace {
+
+constexpr int kRowsThreads = 128;
+constexpr int kRowsUnit = 64;             // keys of a unit: 16 per warp
+constexpr float kRescaleAt = 8.0f;        // a row's reference moves once a logit passes it by this many powers of two
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool bf) {
+    if (bf)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint4 ldg_stream16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint2 ldg_stream8(const void* p) {
+    uint2 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+
+// Both products are taken transposed, keys (then dimensions) on the 16-row side of m16n8k16 and query rows on its
+// 8-column side, so that one query row wastes 7/8 of the instruction and not 15/16, and neither K nor V passes through
+// shared memory: a contraction may run over its index in any order, so a lane simply takes the 16 bytes of a key that
+// it loaded as its fragment of the next two or four instructions, and the queries are laid out to match.  For V, pairs
+// of keys are interleaved with byte permutes.  Every warp has its own 16 keys of a unit, its own running maximum, sum
+// and accumulators; the four warps meet once, at the end of the item.
+// blocks that an SM holds: as many as the registers of the fragments leave room for without spilling
+template <int D, int NB, bool INT8>
+constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : (D == 128 && !INT8) ? 3 : 4;
+
+template <int D, int NB, bool BF, bool INT8>
+__global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm<D, NB, INT8>) paged_rows_kernel(const __grid_constant__ AttendParams p) {
+    constexpr int R = 8 * NB;
+    constexpr int kWords = INT8 ? D / 64 : D / 32;          // 16-byte words of a key that a lane takes
+    constexpr int kSteps = D / 16;                          // k16 steps of S, and 16-row blocks of O
+    constexpr int VW = D / 8 * (INT8 ? 1 : 2) / 4;          // 32-bit words of a V row that a lane takes: D / 8 elements
+
+    __shared__ long long scratch[kRowsThreads / 32];
+    __shared__ Start found;
+    __shared__ float sm_m[4][R], sm_l[4][R];
+    __shared__ alignas(16) float sm_o[4][R][D];         // read back four at a time
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
+    pdl_launch_dependents();
+    pdl_wait();
+    const Schedule<R, kRowsUnit> sch{p.group, p.causal, p.c.kv_heads, p.c.batch};
+    const Start st = find_start<kRowsThreads, R, kRowsUnit>(p.c, sch, p.max_blocks, p.min_units, scratch, &found);
+    if (tid == 0) p.part_items[blockIdx.x].last = -1;
+    Walk<R, kRowsUnit> walk;
+    for (bool more = walk.begin(p.c, sch, st, p.split != 0); more; more = walk.next(p.c)) {
+        const Item it = walk.it;
+        const int rows_all = it.s.new_len * p.group;
+        const int first_row = it.i * R;
+        const int rows = min(R, rows_all - first_row);
+        const int limit = sch.key_limit(it.s, it.i);
+        const float scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
+
+        // queries: the fragment of row g of each block of 8 rows, in the order of the keys' words
+        uint32_t qf[NB][2 * kSteps];
+        int row_limit[NB][2];                                // keys that rows 2j, 2j + 1 see
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int r = first_row + nb * 8 + g;
+            const bool valid = r < rows_all;
+            const int tok = valid ? r / p.group : 0;
+            const uint16_t* qr = p.q + (long long)(it.s.first + tok) * p.q_stride +
+                                 (long long)(it.h * p.group + (valid ? r - tok * p.group : 0)) * D;
+#pragma unroll
+            for (int w = 0; w < 2 * kSteps / 4; ++w) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (valid) {
+                    // int8: a lane's 16 codes of a key's word feed 16 elements, here in two halves
+                    const int at = INT8 ? 16 * (j + 4 * (w >> 1)) + 8 * (w & 1) : 8 * (j + 4 * w);
+                    v = *reinterpret_cast<const uint4*>(qr + at);
+                }
+                qf[nb][4 * w] = v.x;
+                qf[nb][4 * w + 1] = v.y;
+                qf[nb][4 * w + 2] = v.z;
+                qf[nb][4 * w + 3] = v.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int rr = first_row + nb * 8 + 2 * j + e;
+                const int lim = p.causal ? it.s.len - it.s.new_len + rr / p.group + 1 : it.s.len;
+                row_limit[nb][e] = min(lim, limit);
+            }
+        }
+
+        float o[kSteps][NB][4];
+        float m[NB][2], l[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            m[nb][0] = m[nb][1] = -INFINITY;
+            l[nb][0] = l[nb][1] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[k][nb][e] = 0.0f;
+        }
+
+        const int elem = INT8 ? 1 : 2;
+        const int* table = p.c.page_table + it.b * p.c.table_stride;
+        const char* kbase = static_cast<const char*>(p.c.k) + it.h * p.c.head_stride * elem;
+        const char* vbase = static_cast<const char*>(p.c.v) + it.h * p.c.head_stride * elem;
+        const int page_mask = (1 << p.c.page_shift) - 1;
+        const int last_key = min(it.t1 * kRowsUnit, limit);
+        int key = it.t0 * kRowsUnit + warp * 16;             // of this warp's step
+
+        // byte offset of key `at` of the sequence, or -1 when its page lies outside the cache
+        auto place = [&](int at) -> long long {
+            const int page = __ldg(table + (at >> p.c.page_shift));
+            if (page < 0 || page >= p.c.num_pages) {
+                atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
+                return -1;
+            }
+            return (page * p.c.page_stride + (at & page_mask) * p.c.token_stride) * elem;
+        };
+        uint4 kw[2][kWords];                                  // keys g and g + 8
+        auto load_k = [&](int at, long long off) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const bool in = off >= 0 && at + g + 8 * r < last_key;
+                const char* row = kbase + off + (long long)(g + 8 * r) * p.c.token_stride * elem;
+#pragma unroll
+                for (int w = 0; w < kWords; ++w)
+                    kw[r][w] = in ? ldg_stream16(row + 16 * (j + 4 * w)) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        uint32_t vw[4][VW];                                   // keys 2j, 2j + 1, 2j + 8, 2j + 9
+        auto load_v = [&](int at, long long off) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int kk = 2 * j + (r & 1) + 8 * (r >> 1);
+                const bool in = off >= 0 && at + kk < last_key;
+                const char* row = vbase + off + (long long)kk * p.c.token_stride * elem;
+                if constexpr (VW == 2) {
+                    const uint2 v = in ? ldg_stream8(row + 8 * g) : make_uint2(0, 0);
+                    vw[r][0] = v.x;
+                    vw[r][1] = v.y;
+                } else {
+#pragma unroll
+                    for (int w = 0; w < VW / 4; ++w) {
+                        const uint4 v = in ? ldg_stream16(row + 16 * (g + 8 * w)) : make_uint4(0, 0, 0, 0);
+                        vw[r][4 * w] = v.x;
+                        vw[r][4 * w + 1] = v.y;
+                        vw[r][4 * w + 2] = v.z;
+                        vw[r][4 * w + 3] = v.w;
+                    }
+                }
+            }
+        };
+
+        long long off = -1, off_next = -1;
+        if (key < last_key) {
+            off = place(key);
+            load_k(key, off);
+            load_v(key, off);
+            if (key + kRowsUnit < last_key) off_next = place(key + kRowsUnit);
+        }
+        while (key < last_key) {
+            // S^T of 16 keys: rows are keys, columns query rows
+            float s[NB][4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nb][e] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                const uint32_t k0[4] = {kw[0][w].x, kw[0][w].y, kw[0][w].z, kw[0][w].w};
+                const uint32_t k1[4] = {kw[1][w].x, kw[1][w].y, kw[1][w].z, kw[1][w].w};
+                if constexpr (INT8) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t a[4] = {codes_to_pair<BF, 0>(k0[e]), codes_to_pair<BF, 0>(k1[e]),
+                                               codes_to_pair<BF, 1>(k0[e]), codes_to_pair<BF, 1>(k1[e])};
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+                            mma_16816(s[nb], a, qf[nb][8 * w + 2 * e], qf[nb][8 * w + 2 * e + 1], BF);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t a[4] = {k0[2 * e], k1[2 * e], k0[2 * e + 1], k1[2 * e + 1]};
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+                            mma_16816(s[nb], a, qf[nb][4 * w + 2 * e], qf[nb][4 * w + 2 * e + 1], BF);
+                    }
+                }
+            }
+            const int key_now = key;
+            const int key_next = key + kRowsUnit;
+            const long long off_now = off_next;
+            if (key_next < last_key) {
+                load_k(key_next, off_now);                    // the next step's keys travel under this step's softmax
+                if (key_next + kRowsUnit < last_key) off_next = place(key_next + kRowsUnit);
+            }
+
+            // running maximum and sum in powers of two; a row's reference m only moves when a logit passes it by
+            // kRescaleAt, so that most steps need neither the shuffles nor the rescaling (P stays below 2^kRescaleAt)
+            bool moves = false;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at = key_now + g + 8 * (e >> 1);
+                    s[nb][e] = at < row_limit[nb][e & 1] ? s[nb][e] * scale : -INFINITY;
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) moves |= fmaxf(s[nb][e], s[nb][e + 2]) > m[nb][e] + kRescaleAt;
+            }
+            if (__any_sync(0xFFFFFFFFu, moves)) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float t = fmaxf(s[nb][e], s[nb][e + 2]);
+                        t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 4));
+                        t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 8));
+                        t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 16));
+                        const float m_new = fmaxf(m[nb][e], t);
+                        const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m[nb][e] - m_new);
+                        m[nb][e] = m_new;
+                        l[nb][e] *= f;
+#pragma unroll
+                        for (int k = 0; k < kSteps; ++k) {
+                            o[k][nb][e] *= f;
+                            o[k][nb][e + 2] *= f;
+                        }
+                    }
+            }
+            uint32_t pf[NB][2];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                float pr[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float ref = m[nb][e & 1] == -INFINITY ? 0.0f : m[nb][e & 1];
+                    pr[e] = exp2_approx(s[nb][e] - ref);
+                    l[nb][e & 1] += pr[e];
+                }
+                pf[nb][0] = transpose_8x8(narrow2<BF>(pr[0], pr[1]));
+                pf[nb][1] = transpose_8x8(narrow2<BF>(pr[2], pr[3]));
+            }
+
+            // O^T += V^T P^T: rows are dimensions, the contraction is over the 16 keys
+            if constexpr (INT8) {
+#pragma unroll
+                for (int w = 0; w < VW; ++w) {
+                    const uint32_t x0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), x1 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
+                    const uint32_t y0 = __byte_perm(vw[2][w], vw[3][w], 0x5140), y1 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
+                    const uint32_t a0[4] = {codes_to_pair<BF, 0>(x0), codes_to_pair<BF, 1>(x0), codes_to_pair<BF, 0>(y0),
+                                            codes_to_pair<BF, 1>(y0)};
+                    const uint32_t a1[4] = {codes_to_pair<BF, 0>(x1), codes_to_pair<BF, 1>(x1), codes_to_pair<BF, 0>(y1),
+                                            codes_to_pair<BF, 1>(y1)};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        mma_16816(o[2 * w][nb], a0, pf[nb][0], pf[nb][1], BF);
+                        mma_16816(o[2 * w + 1][nb], a1, pf[nb][0], pf[nb][1], BF);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < VW; ++w) {
+                    const uint32_t a[4] = {__byte_perm(vw[0][w], vw[1][w], 0x5410), __byte_perm(vw[0][w], vw[1][w], 0x7632),
+                                           __byte_perm(vw[2][w], vw[3][w], 0x5410), __byte_perm(vw[2][w], vw[3][w], 0x7632)};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma_16816(o[w][nb], a, pf[nb][0], pf[nb][1], BF);
+                }
+            }
+            if (key_next < last_key) load_v(key_next, off_now);
+            key = key_next;
+        }
+
+        // the warps' sums meet in shared memory
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float t = l[nb][e];
+                t += __shfl_xor_sync(0xFFFFFFFFu, t, 4);
+                t += __shfl_xor_sync(0xFFFFFFFFu, t, 8);
+                t += __shfl_xor_sync(0xFFFFFFFFu, t, 16);
+                const int r = nb * 8 + 2 * j + e;
+                if (g == 0) {
+                    sm_m[warp][r] = m[nb][e];
+                    sm_l[warp][r] = t;
+                }
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) {
+                    // block k holds, of lane group g, the dimensions at and at + 1
+                    const int at = INT8 ? (D / 8) * g + 2 * k : 8 * (g + 8 * (k >> 2)) + 2 * (k & 3);
+                    *reinterpret_cast<float2*>(&sm_o[warp][r][at]) = make_float2(o[k][nb][e], o[k][nb][e + 2]);
+                }
+            }
+        __syncthreads();
+        const bool whole = it.t0 == 0 && it.t1 == it.units;
+        const int slot = 2 * blockIdx.x + (it.t0 == 0 ? 1 : 0);
+        const float vs = INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f;
+        for (int x = tid * 4; x < rows * D; x += kRowsThreads * 4) {
+            const int r = x / D, d = x % D;
+            float mm = fmaxf(fmaxf(sm_m[0][r], sm_m[1][r]), fmaxf(sm_m[2][r], sm_m[3][r]));
+            const float ref = mm == -INFINITY ? 0.0f : mm;
+            float sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = exp2_approx(sm_m[w][r] - ref);
+                const float4 v = *reinterpret_cast<const float4*>(&sm_o[w][r][d]);
+                sum += f * sm_l[w][r];
+                acc[0] += f * v.x;
+                acc[1] += f * v.y;
+                acc[2] += f * v.z;
+                acc[3] += f * v.w;
+            }
+            if (whole) {
+                const float inv = sum > 0.0f ? vs / sum : 0.0f;
+                const int row = first_row + r, tok = row / p.group;
+                const int head = it.h * p.group + row - tok * p.group;
+                const long long t = it.s.first + tok;
+                *reinterpret_cast<uint2*>(p.out + t * p.out_stride + (long long)head * D + d) =
+                    make_uint2(narrow2<BF>(acc[0] * inv, acc[1] * inv), narrow2<BF>(acc[2] * inv, acc[3] * inv));
+                if (d == 0 && p.lse != nullptr)
+                    p.lse[t * p.heads + head] = sum > 0.0f ? (mm + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            } else {
+                *reinterpret_cast<float4*>(p.part_o + ((long long)slot * R + r) * D + d) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                if (d == 0) p.part_ml[(long long)slot * R + r] = make_float2(mm, sum);
+            }
+        }
+        if (!whole && it.t0 == 0 && tid == 0) {
+            PartItem pi;
+            pi.last = block_of(st.total, it.first_unit + it.units - 1, st.blocks);
+            pi.h = it.h;
+            pi.first_row = first_row;
+            pi.rows = rows;
+            pi.first_token = it.s.first;
+            p.part_items[blockIdx.x] = pi;
+        }
+        __syncthreads();                                       // the next item reuses the shared memory
+    }
+}
+
+// Joins the parts of the item that began in block x and ended in a later one; one warp per row.  The parts lie in the
+// second slot of block x and in the first slots of the blocks after it, and are added in that order.
+template <int R, int D, bool BF>
+__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttendParams p) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int c = blockIdx.x, lane = threadIdx.x & 31;
+    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    const PartItem pi = p.part_items[c];
+    if (pi.last < 0 || r >= pi.rows) return;
+    constexpr int N = D / 32;                                  // elements of a lane
+    auto slot_of = [&](int k) { return (long long)(k == c ? 2 * c + 1 : 2 * k) * R + r; };
+    float m = -INFINITY;
+    for (int k = c + lane; k <= pi.last; k += 32) m = fmaxf(m, p.part_ml[slot_of(k)].x);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f, acc[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = 0.0f;
+#pragma unroll 4
+    for (int k = c; k <= pi.last; ++k) {
+        const long long s = slot_of(k);
+        const float2 ml = p.part_ml[s];
+        const float f = exp2_approx(ml.x - ref);
+        sum += f * ml.y;
+        const float* src = p.part_o + s * D + lane * N;
+        if constexpr (N == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(src);
+            acc[0] += f * v.x;
+            acc[1] += f * v.y;
+            acc[2] += f * v.z;
+            acc[3] += f * v.w;
+        } else {
+            const float2 v = *reinterpret_cast<const float2*>(src);
+            acc[0] += f * v.x;
+            acc[1] += f * v.y;
+        }
+    }
+    const float vs = p.c.v_scale != nullptr ? __ldg(p.c.v_scale + pi.h) : 1.0f;
+    const float inv = sum > 0.0f ? vs / sum : 0.0f;
+    const int row = pi.first_row + r, tok = row / p.group;
+    const int head = pi.h * p.group + row - tok * p.group;
+    const long long t = pi.first_token + tok;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + t * p.out_stride + (long long)head * D + lane * N);
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) dst[e] = narrow2<BF>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    if (lane == 0 && p.lse != nullptr)
+        p.lse[t * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+}
+
+}  // namespace
+}  // namespace sasq
