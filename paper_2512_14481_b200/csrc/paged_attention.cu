@@ -1,5 +1,8 @@
 // sasq_paged_attention: host side, and the kernels' instantiations.
+#include <atomic>
+
 #include "paged_rows.cuh"
+#include "paged_tiles.cuh"
 
 namespace sasq {
 
@@ -35,6 +38,7 @@ Layout layout_of(int blocks, int R, int D) {
 }
 
 struct Plan {
+    bool tiles;                 // the tensor-core kernel for many rows; else the few-row kernel
     int nb;                     // few-row kernel: blocks of 8 rows
     int blocks;
     int R, unit;
@@ -45,13 +49,14 @@ int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
     Plan pl{};
     const long long rows = (long long)b->max_q_len * (heads / c->num_kv_heads);
+    pl.tiles = rows > 16 && c->kind == SASQ_KV_16BIT && c->num_pages > 0;
     pl.nb = rows <= 8 ? 1 : 2;
-    pl.R = 8 * pl.nb;
-    pl.unit = kRowsUnit;
+    pl.R = pl.tiles ? kTileRows : 8 * pl.nb;
+    pl.unit = pl.tiles ? kTileKeys : kRowsUnit;
     const long long items = (long long)b->batch * c->num_kv_heads * (rows < 1 ? 1 : ceil_div(rows, pl.R));
     const long long most = items * (b->max_seq_len < 1 ? 1 : ceil_div(b->max_seq_len, pl.unit));
     const bool int8 = c->kind == SASQ_KV_INT8, d128 = c->head_dim == 128;
-    const int per_sm = pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
+    const int per_sm = pl.tiles ? 1 : pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
                                           : (int8 ? kRowsBlocksPerSm<64, 1, true> : kRowsBlocksPerSm<64, 1, false>))
                                   : kRowsBlocksPerSm<128, 2, false>;
     const long long fill = (long long)sms * per_sm;
@@ -89,8 +94,67 @@ cudaError_t launch_rows(const AttendParams& p, bool int8, cudaStream_t st) {
     return launch(paged_join_kernel<8 * NB, D, BF>, dim3(p.max_blocks, NB), 256, 0, st, p);
 }
 
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static std::atomic<EncodeTiledFn> fn{nullptr};
+    if (fn.load() == nullptr) {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn.store(reinterpret_cast<EncodeTiledFn>(f));
+    }
+    return fn.load();
+}
+
+// 16-bit pages as [page][head][row][dim]: boxes of 64 dims x up to 128 rows of one page and head, 128-byte swizzle; a
+// page index outside the cache reads zeros.
+bool encode_pages(CUtensorMap* m, const sasq_kv_cache_t* c, void* base, int dt) {
+    const EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->page_size, (cuuint64_t)c->num_kv_heads, (cuuint64_t)c->num_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)c->token_stride * 2, (cuuint64_t)c->head_stride * 2, (cuuint64_t)c->page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(c->page_size < kTileKeys ? c->page_size : kTileKeys), 1, 1};
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    return fn(m, dt == SASQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, bool BF>
-cudaError_t launch_all(const Plan& pl, const AttendParams& p, bool int8, cudaStream_t st) {
+cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
+    static std::atomic<unsigned long long> ready{0};          // devices whose shared-memory limit has been raised
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (!(ready.load() >> (dev & 63) & 1)) {
+        e = cudaFuncSetAttribute(paged_tiles_kernel<D, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTileSmem<D>);
+        if (e != cudaSuccess) return e;
+        ready.fetch_or(1ull << (dev & 63));
+    }
+    CUtensorMap map_k, map_v;
+    if (!encode_pages(&map_k, c, c->k, BF ? SASQ_BF16 : SASQ_F16) || !encode_pages(&map_v, c, c->v, BF ? SASQ_BF16 : SASQ_F16))
+        return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)p.max_blocks);
+    cfg.blockDim = dim3(kTileThreads);
+    cfg.dynamicSmemBytes = kTileSmem<D>;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = pdl_attribute();
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF>, map_k, map_v, p);
+    if (e != cudaSuccess || !p.split) return e;
+    return launch(paged_join_kernel<kTileRows, D, BF>, dim3(p.max_blocks, kTileRows / 8), 256, 0, st, p);
+}
+
+template <int D, bool BF>
+cudaError_t launch_all(const Plan& pl, const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
+    const bool int8 = c->kind == SASQ_KV_INT8;
+    if (pl.tiles) return launch_tiles<D, BF>(p, c, st);
     return pl.nb == 1 ? launch_rows<D, 1, BF>(p, int8, st) : launch_rows<D, 2, BF>(p, int8, st);
 }
 
@@ -137,22 +201,23 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.out_stride = out_stride;
     p.heads = num_q_heads;
     p.group = num_q_heads / cache->num_kv_heads;
-    p.scale = softmax_scale * 1.4426950408889634f;
+    // A zero scale would turn masked logits, -inf, into NaN; one this small gives the same equal weights.
+    p.scale = softmax_scale == 0.0f ? 1e-30f : softmax_scale * 1.4426950408889634f;
     p.causal = causal != 0;
     // no item has more than one unit when the host's bound says so: nothing to cut, no joining launch
     p.split = batch->max_seq_len > pl.unit;
     p.max_blocks = pl.blocks;
     p.min_units = 1;
+    p.wait_limit = 1LL << 31;
     p.part_items = static_cast<PartItem*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + l.ml);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.o);
-    const bool int8 = cache->kind == SASQ_KV_INT8;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (cache->head_dim == 128)
-        e = dt == SASQ_BF16 ? launch_all<128, true>(pl, p, int8, st) : launch_all<128, false>(pl, p, int8, st);
+        e = dt == SASQ_BF16 ? launch_all<128, true>(pl, p, cache, st) : launch_all<128, false>(pl, p, cache, st);
     else
-        e = dt == SASQ_BF16 ? launch_all<64, true>(pl, p, int8, st) : launch_all<64, false>(pl, p, int8, st);
+        e = dt == SASQ_BF16 ? launch_all<64, true>(pl, p, cache, st) : launch_all<64, false>(pl, p, cache, st);
     return e == cudaSuccess ? SASQ_OK : SASQ_ERR_CUDA;
 }
 
