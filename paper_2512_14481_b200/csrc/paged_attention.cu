@@ -41,19 +41,23 @@ struct Plan {
     bool tiles;                 // the tensor-core kernel for many rows; else the few-row kernel
     int nb;                     // few-row kernel: blocks of 8 rows
     int blocks;
-    int R, unit;
+    int rows;                   // of an item
+    int slot_rows;              // room for an item's rows in a part slot
+    int unit;
 };
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
     Plan pl{};
-    const long long rows = (long long)b->max_q_len * (heads / c->num_kv_heads);
-    pl.tiles = rows > 16 && c->kind == SASQ_KV_16BIT && c->num_pages > 0;
+    const int group = heads / c->num_kv_heads;
+    const long long rows = (long long)b->max_q_len * group;
+    pl.tiles = rows > 16 && group <= 128 && c->kind == SASQ_KV_16BIT && c->num_pages > 0;
     pl.nb = rows <= 8 ? 1 : 2;
-    pl.R = pl.tiles ? kTileRows : 8 * pl.nb;
+    pl.rows = pl.tiles ? 2 * (128 / group * group) : 8 * pl.nb;
+    pl.slot_rows = pl.tiles ? 256 : pl.rows;
     pl.unit = pl.tiles ? kTileKeys : kRowsUnit;
-    const long long items = (long long)b->batch * c->num_kv_heads * (rows < 1 ? 1 : ceil_div(rows, pl.R));
+    const long long items = (long long)b->batch * c->num_kv_heads * (rows < 1 ? 1 : ceil_div(rows, pl.rows));
     const long long most = items * (b->max_seq_len < 1 ? 1 : ceil_div(b->max_seq_len, pl.unit));
     const bool int8 = c->kind == SASQ_KV_INT8, d128 = c->head_dim == 128;
     const int per_sm = pl.tiles ? 1 : pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
@@ -69,7 +73,7 @@ int attend_check(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, int
     if (rc != SASQ_OK) return rc;
     if (num_q_heads <= 0 || num_q_heads % cache->num_kv_heads != 0) return SASQ_ERR_INVALID_ARG;
     if (cache->head_dim != 64 && cache->head_dim != 128) return SASQ_ERR_UNSUPPORTED;
-    if ((long long)batch->total_q * (num_q_heads / cache->num_kv_heads) > 0x7FFFFFFF) return SASQ_ERR_UNSUPPORTED;
+    if ((long long)batch->total_q * (num_q_heads / cache->num_kv_heads) > (1 << 30)) return SASQ_ERR_UNSUPPORTED;
     return SASQ_OK;
 }
 
@@ -91,7 +95,7 @@ cudaError_t launch_rows(const AttendParams& p, bool int8, cudaStream_t st) {
     const cudaError_t e = int8 ? launch(paged_rows_kernel<D, NB, BF, true>, dim3(p.max_blocks), kRowsThreads, 0, st, p)
                                : launch(paged_rows_kernel<D, NB, BF, false>, dim3(p.max_blocks), kRowsThreads, 0, st, p);
     if (e != cudaSuccess || !p.split) return e;
-    return launch(paged_join_kernel<8 * NB, D, BF>, dim3(p.max_blocks, NB), 256, 0, st, p);
+    return launch(paged_join_kernel<8 * NB, 8 * NB, D, BF>, dim3(p.max_blocks, NB), 256, 0, st, p);
 }
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -110,18 +114,33 @@ EncodeTiledFn encode_fn() {
     return fn.load();
 }
 
-// 16-bit pages as [page][head][row][dim]: boxes of 64 dims x up to 128 rows of one page and head, 128-byte swizzle; a
-// page index outside the cache reads zeros.
-bool encode_pages(CUtensorMap* m, const sasq_kv_cache_t* c, void* base, int dt) {
+template <bool BF>
+bool encode_map(CUtensorMap* m, void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     const EncodeTiledFn fn = encode_fn();
-    if (fn == nullptr) return false;
-    const cuuint64_t dims[4] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->page_size, (cuuint64_t)c->num_kv_heads, (cuuint64_t)c->num_pages};
-    const cuuint64_t strides[3] = {(cuuint64_t)c->token_stride * 2, (cuuint64_t)c->head_stride * 2, (cuuint64_t)c->page_stride * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)(c->page_size < kTileKeys ? c->page_size : kTileKeys), 1, 1};
     const cuuint32_t one[4] = {1, 1, 1, 1};
-    return fn(m, dt == SASQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, box, one,
+    return fn != nullptr &&
+           fn(m, BF ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, base, dims, strides, box, one,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// 16-bit pages as [page][head][row][dim]: boxes of 64 dims x up to 128 rows of one page and head, 128-byte swizzle; a
+// page index outside the cache reads zeros.
+template <int D, bool BF>
+bool encode_pages(CUtensorMap* m, const sasq_kv_cache_t* c, void* base) {
+    const cuuint64_t dims[4] = {D, (cuuint64_t)c->page_size, (cuuint64_t)c->num_kv_heads, (cuuint64_t)c->num_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)c->token_stride * 2, (cuuint64_t)c->head_stride * 2, (cuuint64_t)c->page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(c->page_size < kTileKeys ? c->page_size : kTileKeys), 1, 1};
+    return encode_map<BF>(m, base, 4, dims, strides, box);
+}
+
+// queries as [token][head][dim]: boxes of 64 dims x the heads of a group x the tokens of a row tile
+template <int D, bool BF>
+bool encode_queries(CUtensorMap* m, const AttendParams& p) {
+    const cuuint64_t dims[3] = {D, (cuuint64_t)p.heads, (cuuint64_t)p.c.total_q};
+    const cuuint64_t strides[2] = {D * 2, (cuuint64_t)p.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)p.group, (cuuint32_t)(128 / p.group)};
+    return encode_map<BF>(m, const_cast<uint16_t*>(p.q), 3, dims, strides, box);
 }
 
 template <int D, bool BF>
@@ -135,8 +154,8 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, cudaSt
         if (e != cudaSuccess) return e;
         ready.fetch_or(1ull << (dev & 63));
     }
-    CUtensorMap map_k, map_v;
-    if (!encode_pages(&map_k, c, c->k, BF ? SASQ_BF16 : SASQ_F16) || !encode_pages(&map_v, c, c->v, BF ? SASQ_BF16 : SASQ_F16))
+    CUtensorMap map_q, map_k, map_v;
+    if (!encode_queries<D, BF>(&map_q, p) || !encode_pages<D, BF>(&map_k, c, c->k) || !encode_pages<D, BF>(&map_v, c, c->v))
         return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)p.max_blocks);
@@ -146,9 +165,9 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, cudaSt
     cudaLaunchAttribute attr = pdl_attribute();
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF>, map_k, map_v, p);
+    e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF>, map_q, map_k, map_v, p);
     if (e != cudaSuccess || !p.split) return e;
-    return launch(paged_join_kernel<kTileRows, D, BF>, dim3(p.max_blocks, kTileRows / 8), 256, 0, st, p);
+    return launch(paged_join_kernel<256, 128, D, BF>, dim3(p.max_blocks, 256 / 8), 256, 0, st, p);
 }
 
 template <int D, bool BF>
@@ -168,7 +187,7 @@ size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, const sasq_k
     PagedParams p{};
     if (attend_check(cache, batch, num_q_heads, SASQ_BF16, &p) != SASQ_OK) return 0;
     const Plan pl = make_plan(cache, batch, num_q_heads, kMaxSms);
-    return layout_of(pl.blocks, pl.R, cache->head_dim).total;
+    return layout_of(pl.blocks, pl.slot_rows, cache->head_dim).total;
 }
 
 int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, const void* q, void* out, float* lse,
@@ -193,7 +212,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.c.status = paged_status_ptr();
     if (p.c.status == nullptr) return SASQ_ERR_CUDA;
     const Plan pl = make_plan(cache, batch, num_q_heads, sms);
-    const Layout l = layout_of(pl.blocks, pl.R, cache->head_dim);
+    const Layout l = layout_of(pl.blocks, pl.slot_rows, cache->head_dim);
     p.q = static_cast<const uint16_t*>(q);
     p.out = static_cast<uint16_t*>(out);
     p.lse = lse;
@@ -207,6 +226,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     // no item has more than one unit when the host's bound says so: nothing to cut, no joining launch
     p.split = batch->max_seq_len > pl.unit;
     p.max_blocks = pl.blocks;
+    p.item_rows = pl.rows;
     p.min_units = 1;
     p.wait_limit = 1LL << 31;
     p.part_items = static_cast<PartItem*>(workspace);

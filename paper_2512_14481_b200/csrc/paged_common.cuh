@@ -49,8 +49,8 @@ __device__ __forceinline__ Sequence load_sequence(const PagedParams& p, int b) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Work of an attention call.  The rows of one KV head are (new token, query head of the group) pairs, token first; R
-// consecutive rows of a sequence and KV head are an item, and an item's keys are walked in units of KT.  The units of
+// Work of an attention call.  The rows of one KV head are (new token, query head of the group) pairs, token first; a
+// fixed number of consecutive rows of a sequence and KV head are an item, and an item's keys are walked in units of KT.  The units of
 // all items, laid end to end (sequence, KV head, item, key), are cut into equal stretches, one per thread block: every
 // block has the same number of units whatever the lengths are, a block walks whole items in the middle of its stretch
 // and at most two part items at its ends.  Part items leave (O, m, l) in the workspace, and a second launch joins them.
@@ -65,19 +65,16 @@ struct Item {
     long long first_unit;     // of the item, in the whole call
 };
 
-template <int R, int KT>
+template <int KT>
 struct Schedule {
-    int group, causal, heads, batch;
+    int rows;                 // of an item
+    int group, causal, heads;
 
-    __device__ __forceinline__ int tiles(const Sequence& s) const { return (int)(((long long)s.new_len * group + R - 1) / R); }
+    __device__ __forceinline__ int tiles(const Sequence& s) const { return (s.new_len * group + rows - 1) / rows; }
     // keys that the rows of tile i can see at most
     __device__ __forceinline__ int key_limit(const Sequence& s, int i) const {
         if (!causal) return s.len;
-        const long long rows = (long long)s.new_len * group;
-        long long last = (long long)(i + 1) * R;
-        last = (last < rows ? last : rows) - 1;
-        const long long lim = (long long)s.len - s.new_len + last / group + 1;
-        return lim < 0 ? 0 : (int)lim;
+        return max(0, s.len - s.new_len + (min((i + 1) * rows, s.new_len * group) - 1) / group + 1);
     }
     // an item without keys still counts one unit: its rows have to be written
     __device__ __forceinline__ int units(const Sequence& s, int i) const {
@@ -109,8 +106,8 @@ struct Start {
 };
 
 // Every thread of the block calls this; scratch: one long long per warp + one Start, in shared memory.
-template <int THREADS, int R, int KT>
-__device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule<R, KT>& sch, int max_blocks, int min_units,
+template <int THREADS, int KT>
+__device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule<KT>& sch, int max_blocks, int min_units,
                                             long long* scratch, Start* found) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.batch + THREADS - 1) / THREADS;
@@ -161,16 +158,16 @@ __device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule
 }
 
 // Walks the items of a block's stretch; every thread keeps its own copy.
-template <int R, int KT>
+template <int KT>
 struct Walk {
-    Schedule<R, KT> sch;
+    Schedule<KT> sch;
     Item it;
     long long at, end;
     int n_tiles;
     bool split;
 
     // split == false: items are not cut, an item belongs to the block in whose stretch it begins
-    __device__ __forceinline__ bool begin(const PagedParams& p, const Schedule<R, KT>& s, const Start& st, bool may_split) {
+    __device__ __forceinline__ bool begin(const PagedParams& p, const Schedule<KT>& s, const Start& st, bool may_split) {
         sch = s;
         split = may_split;
         at = st.begin;
@@ -223,7 +220,8 @@ struct PartItem {
     int first_row;            // of the item, among the (token, group head) rows of its sequence
     int rows;
     int first_token;          // of the sequence, in q
-    int pad[3];
+    int tile_rows;            // rows that each row tile of the item uses
+    int pad[2];
 };
 
 // ---------------------------------------------------------------------------------------------------------------------

@@ -16,6 +16,7 @@ struct AttendParams {
     int causal;
     int split;                  // items may be cut among blocks (the joining launch follows)
     int max_blocks, min_units;
+    int item_rows;              // rows of an item
     PartItem* part_items;       // [max_blocks]
     float2* part_ml;            // [2 * max_blocks][R]: maximum (log2 units) and sum
     float* part_o;              // [2 * max_blocks][R][D]
@@ -79,10 +80,10 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm<D, NB, INT8>) p
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
     pdl_launch_dependents();
     pdl_wait();
-    const Schedule<R, kRowsUnit> sch{p.group, p.causal, p.c.kv_heads, p.c.batch};
-    const Start st = find_start<kRowsThreads, R, kRowsUnit>(p.c, sch, p.max_blocks, p.min_units, scratch, &found);
+    const Schedule<kRowsUnit> sch{R, p.group, p.causal, p.c.kv_heads};
+    const Start st = find_start<kRowsThreads, kRowsUnit>(p.c, sch, p.max_blocks, p.min_units, scratch, &found);
     if (tid == 0) p.part_items[blockIdx.x].last = -1;
-    Walk<R, kRowsUnit> walk;
+    Walk<kRowsUnit> walk;
     for (bool more = walk.begin(p.c, sch, st, p.split != 0); more; more = walk.next(p.c)) {
         const Item it = walk.it;
         const int rows_all = it.s.new_len * p.group;
@@ -368,6 +369,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm<D, NB, INT8>) p
             pi.first_row = first_row;
             pi.rows = rows;
             pi.first_token = it.s.first;
+            pi.tile_rows = R;
             p.part_items[blockIdx.x] = pi;
         }
         __syncthreads();                                       // the next item reuses the shared memory
@@ -375,15 +377,17 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm<D, NB, INT8>) p
 }
 
 // Joins the parts of the item that began in block x and ended in a later one; one warp per row.  The parts lie in the
-// second slot of block x and in the first slots of the blocks after it, and are added in that order.
-template <int R, int D, bool BF>
+// second slot of block x and in the first slots of the blocks after it, and are added in that order.  R rows of a slot,
+// in row tiles of TILE of which an item may use fewer.
+template <int R, int TILE, int D, bool BF>
 __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttendParams p) {
     pdl_launch_dependents();
     pdl_wait();
     const int c = blockIdx.x, lane = threadIdx.x & 31;
     const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
     const PartItem pi = p.part_items[c];
-    if (pi.last < 0 || r >= pi.rows) return;
+    const int item_row = r / TILE * pi.tile_rows + r % TILE;
+    if (pi.last < 0 || r % TILE >= pi.tile_rows || item_row >= pi.rows) return;
     constexpr int N = D / 32;                                  // elements of a lane
     auto slot_of = [&](int k) { return (long long)(k == c ? 2 * c + 1 : 2 * k) * R + r; };
     float m = -INFINITY;
@@ -415,7 +419,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
     }
     const float vs = p.c.v_scale != nullptr ? __ldg(p.c.v_scale + pi.h) : 1.0f;
     const float inv = sum > 0.0f ? vs / sum : 0.0f;
-    const int row = pi.first_row + r, tok = row / p.group;
+    const int row = pi.first_row + item_row, tok = row / p.group;
     const int head = pi.h * p.group + row - tok * p.group;
     const long long t = pi.first_token + tok;
     uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + t * p.out_stride + (long long)head * D + lane * N);

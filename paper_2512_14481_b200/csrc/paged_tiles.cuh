@@ -13,6 +13,12 @@ __device__ __forceinline__ void tma_load_4d(uint32_t smem_dst, const CUtensorMap
         ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
 // D[tmem] (+)= A[tmem] * B[smem]: 16-bit A, two elements per 32-bit column
 __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -55,13 +61,14 @@ constexpr uint32_t kIdescBTransposed = 1u << 16;     // instruction descriptor: 
 
 namespace {
 
-constexpr int kTileRows = 256;            // rows of an item: two MMA tiles of 128
+// An item is two row tiles, each the tokens whose heads fit 128 MMA rows: 128 / group tokens, so that a row tile is one
+// box of q (of a group of five heads 125 rows are used).
 constexpr int kTileKeys = 128;            // keys of a unit
-constexpr int kTileThreads = 384;         // warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: loads; 10, 11 idle
+constexpr int kTileThreads = 384;         // warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q; 11 idle
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10;
 // registers a thread: 168 at launch (384 x 168 of the SM's 65,536), then moved from the last four warps to the softmax,
 // which holds a row of 128 logits: 208 + 208 + 88 = 3 x 168
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
 
 template <int D>
 struct TileShape {
@@ -73,7 +80,7 @@ struct TileShape {
 
 struct TileTail {
     uint64_t kv_full[8], kv_empty[8];
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
     uint64_t drain;
     long long scratch[kTileThreads / 32];
     Start found;
@@ -102,16 +109,37 @@ __device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, TileTa
     return true;
 }
 
-// tiles of 128 keys that row tile x (0 or 1) of an item takes part in
-__device__ __forceinline__ int tile_count(const Schedule<kTileRows, kTileKeys>& sch, const Item& it, int x) {
-    const long long rows = (long long)it.s.new_len * sch.group;
-    const long long first = (long long)it.i * kTileRows + 128 * x;
+using TileSchedule = Schedule<kTileKeys>;
+using TileWalk = Walk<kTileKeys>;
+
+// end of the units of an item, in this block, that row tile x takes part in (it.t0 or less: none)
+__device__ __forceinline__ int tile_end(const TileSchedule& sch, const Item& it, int x) {
+    const int half = sch.rows >> 1;
+    const int rows = it.s.new_len * sch.group, first = it.i * sch.rows + half * x;
     if (first >= rows) return 0;
-    if (!sch.causal) return (it.s.len + kTileKeys - 1) / kTileKeys;
-    const long long last = (first + 128 < rows ? first + 128 : rows) - 1;
-    const long long lim = (long long)it.s.len - it.s.new_len + last / sch.group + 1;
-    return lim <= 0 ? 0 : (int)((lim + kTileKeys - 1) / kTileKeys);
+    const int lim = sch.causal ? it.s.len - it.s.new_len + (min(first + half, rows) - 1) / sch.group + 1 : it.s.len;
+    return min(it.t1, (lim + kTileKeys - 1) / kTileKeys);
 }
+
+// The units of a block in order, for the roles that work on both row tiles; items without keys are passed over.
+struct Unit {
+    int t, t0, end[2], t_end;
+    bool more;
+    __device__ __forceinline__ void enter(const PagedParams& p, const TileSchedule& sch, TileWalk& walk) {
+        for (; more; more = walk.next(p)) {
+            end[0] = tile_end(sch, walk.it, 0);
+            end[1] = tile_end(sch, walk.it, 1);
+            t_end = max(end[0], end[1]);
+            t = t0 = walk.it.t0;
+            if (t < t_end) return;
+        }
+    }
+    __device__ __forceinline__ void next(const PagedParams& p, const TileSchedule& sch, TileWalk& walk) {
+        if (++t < t_end) return;
+        more = walk.next(p);
+        enter(p, sch, walk);
+    }
+};
 
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
     uint64_t r;
@@ -134,15 +162,23 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return d;
 }
 
-// Two row tiles X = 0, 1 of 128 rows share every K and V tile.  Per unit and row tile:
+template <bool MORE, int N>
+__device__ __forceinline__ void registers_to() {
+    if constexpr (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Two row tiles x = 0, 1 share every K and V tile.  Per unit and row tile:
 //   S = Q K^T       (MMA, both operands in shared memory, S in TMEM)
 //   P = 2^(scale S - m), row sums, P back to TMEM over S as 16-bit pairs     (one thread per row, 4 warps per row tile)
 //   O += P V        (MMA, P in TMEM, V in shared memory with the keys along its rows, O in TMEM)
-// While the softmax warps of one row tile work, the MMAs of the other run.
+// While the softmax warps of one row tile work, the MMAs of the other run.  S of the next unit is asked for right behind
+// the PV that frees it, across items too: the next item's queries are fetched as soon as the last QK has read the old
+// ones, so that its first S is there when the softmax warps have stored the old item's rows.
 template <int D, bool BF>
 __global__ void __launch_bounds__(kTileThreads, 1)
-paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                   const __grid_constant__ AttendParams p) {
+paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendParams p) {
     using Shape = TileShape<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -157,7 +193,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             ptx::mbar_init(&tail->kv_empty[s], 1);
         }
         for (int x = 0; x < 2; ++x) {
-            ptx::mbar_init(&tail->q_full[x], 128);
+            ptx::mbar_init(&tail->q_full[x], 1);
+            ptx::mbar_init(&tail->q_empty[x], 1);
             ptx::mbar_init(&tail->s_full[x], 1);
             ptx::mbar_init(&tail->p_full[x], 128);
             ptx::mbar_init(&tail->o_full[x], 1);
@@ -165,6 +202,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         ptx::mbar_init(&tail->drain, 1);
         tail->abort_flag = 0;
         ptx::mbar_init_fence();
+        ptx::prefetch_tensormap(&map_q);
         ptx::prefetch_tensormap(&map_k);
         ptx::prefetch_tensormap(&map_v);
     }
@@ -179,51 +217,52 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     pdl_launch_dependents();
     pdl_wait();
 
-    const Schedule<kTileRows, kTileKeys> sch{p.group, p.causal, p.c.kv_heads, p.c.batch};
-    const Start st = find_start<kTileThreads, kTileRows, kTileKeys>(p.c, sch, p.max_blocks, p.min_units, tail->scratch, &tail->found);
+    const TileSchedule sch{p.item_rows, p.group, p.causal, p.c.kv_heads};
+    const Start st = find_start<kTileThreads, kTileKeys>(p.c, sch, p.max_blocks, p.min_units, tail->scratch, &tail->found);
     if (tid == 0) p.part_items[blockIdx.x].last = -1;
-    Walk<kTileRows, kTileKeys> walk;
-    bool more = walk.begin(p.c, sch, st, p.split != 0);
+    TileWalk walk;
+    const bool any_work = walk.begin(p.c, sch, st, p.split != 0);
+    bool ok = true;
+    // whole warps wait together: a role goes on, or gives up, as a warp
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        ok = ok && tile_wait(bar, parity, tail, p);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        return ok;
+    };
 
-    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    // every role sets its registers inside its own branch: the compiler allots them by the branch's last such instruction
     if (warp == kLoadWarp) {
-        // ---------------- loads: K and V of each unit, in turn, a lane per page ----------------
+        // ---------------- K and V of each unit, in turn, a lane per page ----------------
+        registers_to<false, kOtherRegs>();
         int slot = 0;
         uint32_t phase = 0;
-        bool ok = true;
         const int box = min(1 << p.c.page_shift, kTileKeys);
         const int boxes = kTileKeys / box;
         const int page_mask = (1 << p.c.page_shift) - 1;
-        for (; more && ok; more = walk.next(p.c)) {
-            const Item& it = walk.it;
-            const int* table = p.c.page_table + it.b * p.c.table_stride;
-            const int t_end = min(it.t1, max(tile_count(sch, it, 0), tile_count(sch, it, 1)));
-            for (int t = it.t0; t < t_end && ok; ++t) {
-                const int key = t * kTileKeys + lane * box;
-                int page = (int)p.c.num_pages;                  // outside the cache: the copy fills in zeros
-                if (lane < boxes && key < it.s.len) {
-                    const int entry = __ldg(table + (key >> p.c.page_shift));
-                    if (entry < 0 || entry >= p.c.num_pages) atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
-                    else page = entry;
-                }
+        Unit u;
+        u.more = any_work;
+        for (u.enter(p.c, sch, walk); u.more && ok; u.next(p.c, sch, walk)) {
+            const int key = u.t * kTileKeys + lane * box;
+            int page = (int)p.c.num_pages;                      // outside the cache: the copy fills in zeros
+            if (lane < boxes && key < walk.it.s.len) {
+                const int entry = __ldg(p.c.page_table + walk.it.b * p.c.table_stride + (key >> p.c.page_shift));
+                if (entry < 0 || entry >= p.c.num_pages) atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
+                else page = entry;
+            }
 #pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    ok = ok && tile_wait(&tail->kv_empty[slot], phase ^ 1u, tail, p);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) break;
-                    if (lane == 0) ptx::mbar_arrive_expect_tx(&tail->kv_full[slot], Shape::kSlotBytes);
-                    __syncwarp();
-                    if (lane < boxes) {
-                        const uint32_t dst = ptx::smem_u32(ring) + slot * Shape::kSlotBytes + lane * box * 128;
+            for (int kv = 0; kv < 2; ++kv) {
+                if (!wait(&tail->kv_empty[slot], phase ^ 1u)) break;
+                if (lane == 0) ptx::mbar_arrive_expect_tx(&tail->kv_full[slot], Shape::kSlotBytes);
+                __syncwarp();
+                if (lane < boxes) {
+                    const uint32_t dst = ptx::smem_u32(ring) + slot * Shape::kSlotBytes + lane * box * 128;
 #pragma unroll
-                        for (int half = 0; half < Shape::kHalves; ++half)
-                            ptx::tma_load_4d(dst + half * kTileKeys * 128, kv == 0 ? &map_k : &map_v, &tail->kv_full[slot], half * 64,
-                                             key & page_mask, it.h, page);
-                    }
-                    __syncwarp();
-                    if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; }
+                    for (int half = 0; half < Shape::kHalves; ++half)
+                        ptx::tma_load_4d(dst + half * kTileKeys * 128, kv == 0 ? &map_k : &map_v, &tail->kv_full[slot], half * 64,
+                                         key & page_mask, walk.it.h, page);
                 }
+                __syncwarp();
+                if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; }
             }
         }
         // gave up: copies still in flight must land before the block's shared memory goes away
@@ -236,101 +275,119 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
         }
         __syncwarp();
+    } else if (warp == kQueryWarp) {
+        // ---------------- Q of each item ----------------
+        registers_to<false, kOtherRegs>();
+        uint32_t filled[2] = {0, 0};                            // times that each row tile's queries were asked for
+        const int tokens = 128 / p.group;
+        for (bool more = any_work; more && ok; more = walk.next(p.c)) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (!ok || tile_end(sch, walk.it, x) <= walk.it.t0) continue;
+                if (!wait(&tail->q_empty[x], (filled[x] & 1u) ^ 1u)) continue;
+                ++filled[x];
+                if (lane == 0) {
+                    ptx::mbar_arrive_expect_tx(&tail->q_full[x], (uint32_t)(tokens * p.group * D * 2));
+#pragma unroll
+                    for (int half = 0; half < Shape::kHalves; ++half)
+                        ptx::tma_load_3d(ptx::smem_u32(q_smem) + x * Shape::kQBytes + half * 128 * 128, &map_q, &tail->q_full[x], half * 64,
+                                         walk.it.h * p.group, walk.it.s.first + (2 * walk.it.i + x) * tokens);
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok && lane == 0) {
+            for (int x = 0; x < 2; ++x) {
+                const long long t0 = clock64();
+                while (filled[x] != 0 && !ptx::mbar_try_wait(&tail->q_full[x], (filled[x] & 1u) ^ 1u))
+                    if (clock64() - t0 > (1LL << 24)) break;
+            }
+        }
+        __syncwarp();
     } else if (warp == kMmaWarp) {
         // ---------------- MMAs ----------------
+        registers_to<false, kOtherRegs>();
         constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, BF);
         constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF) | ptx::kIdescBTransposed;
         int slot = 0;
         uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-        bool ok = true;
         auto advance = [&] { if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; } };
         const uint32_t ring_addr = ptx::smem_u32(ring), q_addr = ptx::smem_u32(q_smem);
-        auto qk = [&](int x, int k_slot) {                        // issued by one lane
-            const uint64_t a = ptx::smem_desc_k_major_sw128(q_addr + x * Shape::kQBytes);
-            const uint64_t b = ptx::smem_desc_k_major_sw128(ring_addr + k_slot * Shape::kSlotBytes);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uint64_t at = (uint64_t)(((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4);
-                ptx::mma_f16_ss(tmem + x * 128, a + at, b + at, idesc_s, k != 0);
+        // S of row tile x for unit u, whose keys are in k_slot
+        auto qk = [&](const Unit& u, int x, int k_slot) {
+            if (u.t == u.t0) {
+                if (!wait(&tail->q_full[x], q_phase[x])) return;
+                q_phase[x] ^= 1u;
             }
-            ptx::mma_commit(&tail->s_full[x]);
-        };
-        auto pv = [&](int x, int v_slot, bool first) {
-            const uint64_t b = ptx::smem_desc_mn_major_sw128(ring_addr + v_slot * Shape::kSlotBytes, kTileKeys * 128);
-#pragma unroll
-            for (int k = 0; k < kTileKeys / 16; ++k)
-                ptx::mma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + 8 * k, b + (uint64_t)(k * 2048 >> 4), idesc_o, !(first && k == 0));
-            ptx::mma_commit(&tail->o_full[x]);
-        };
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            ok = ok && tile_wait(bar, parity, tail, p);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            return ok;
-        };
-        for (; more && ok; more = walk.next(p.c)) {
-            const Item& it = walk.it;
-            const int n0 = tile_count(sch, it, 0), n1 = tile_count(sch, it, 1);
-            const int t_end = min(it.t1, max(n0, n1));
-            if (it.t0 >= t_end) continue;
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                if (it.t0 < (x == 0 ? n0 : n1)) {
-                    if (!wait(&tail->q_full[x], q_phase[x])) break;
-                    q_phase[x] ^= 1u;
-                }
-            if (!ok) break;
             ptx::tc_fence_after_sync();
-            if (!wait(&tail->kv_full[slot], phase)) break;
             if (ptx::elect_one()) {
-                if (it.t0 < n0) qk(0, slot);
-                if (it.t0 < n1) qk(1, slot);
-                ptx::mma_commit(&tail->kv_empty[slot]);
+                const uint64_t a = ptx::smem_desc_k_major_sw128(q_addr + x * Shape::kQBytes);
+                const uint64_t b = ptx::smem_desc_k_major_sw128(ring_addr + k_slot * Shape::kSlotBytes);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint64_t at = (uint64_t)(((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4);
+                    ptx::mma_f16_ss(tmem + x * 128, a + at, b + at, idesc_s, k != 0);
+                }
+                ptx::mma_commit(&tail->s_full[x]);
+                if (u.t + 1 == u.end[x]) ptx::mma_commit(&tail->q_empty[x]);
             }
             __syncwarp();
-            advance();
-            for (int t = it.t0; t < t_end; ++t) {
-                const int v_slot = slot;
-                if (!wait(&tail->kv_full[v_slot], phase)) break;
-                // rows of V behind the sequence's last key: whatever they hold is multiplied by P = 0, and must be finite
-                const int valid = it.s.len - t * kTileKeys;
-                if (valid < kTileKeys) {
-                    uint8_t* v = ring + (size_t)v_slot * Shape::kSlotBytes;
-                    for (int x = lane; x < (kTileKeys - valid) * 8 * Shape::kHalves; x += 32) {
-                        const int half = x / ((kTileKeys - valid) * 8), y = x % ((kTileKeys - valid) * 8);
-                        *reinterpret_cast<uint4*>(v + half * kTileKeys * 128 + valid * 128 + y * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                }
-                advance();
-                const int k_slot = slot;
-                const bool next = t + 1 < t_end;
-                if (next) {
-                    if (!wait(&tail->kv_full[k_slot], phase)) break;
-                    advance();
-                }
+        };
+        Unit u;
+        u.more = any_work;
+        u.enter(p.c, sch, walk);
+        if (u.more && wait(&tail->kv_full[slot], phase)) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int n = x == 0 ? n0 : n1;
-                    if (t < n) {
-                        if (!wait(&tail->p_full[x], p_phase[x])) break;
-                        p_phase[x] ^= 1u;
-                        ptx::tc_fence_after_sync();
-                        if (ptx::elect_one()) {
-                            pv(x, v_slot, t == it.t0);
-                            if (next && t + 1 < n) qk(x, k_slot);
-                        }
-                        __syncwarp();
-                    }
-                    if (x == 1 && ptx::elect_one()) {
-                        ptx::mma_commit(&tail->kv_empty[v_slot]);
-                        if (next) ptx::mma_commit(&tail->kv_empty[k_slot]);
+            for (int x = 0; x < 2; ++x)
+                if (u.t < u.end[x] && ok) qk(u, x, slot);
+            if (ptx::elect_one()) ptx::mma_commit(&tail->kv_empty[slot]);
+            __syncwarp();
+            advance();
+        }
+        while (u.more && ok) {
+            const Unit now = u;
+            const int v_slot = slot, valid = walk.it.s.len - now.t * kTileKeys;
+            u.next(p.c, sch, walk);
+            if (!wait(&tail->kv_full[v_slot], phase)) break;
+            // rows of V behind the sequence's last key: whatever they hold is multiplied by P = 0, and must be finite
+            if (valid < kTileKeys) {
+                uint8_t* v = ring + (size_t)v_slot * Shape::kSlotBytes + valid * 128;
+                for (int y = lane; y < (kTileKeys - valid) * 8; y += 32)
+#pragma unroll
+                    for (int half = 0; half < Shape::kHalves; ++half)
+                        *reinterpret_cast<uint4*>(v + half * kTileKeys * 128 + y * 16) = make_uint4(0, 0, 0, 0);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+            }
+            advance();
+            const int k_slot = slot;
+            if (u.more) {
+                if (!wait(&tail->kv_full[k_slot], phase)) break;
+                advance();
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (now.t < now.end[x] && ok) {
+                    if (!wait(&tail->p_full[x], p_phase[x])) break;
+                    p_phase[x] ^= 1u;
+                    ptx::tc_fence_after_sync();
+                    if (ptx::elect_one()) {
+                        const uint64_t b = ptx::smem_desc_mn_major_sw128(ring_addr + v_slot * Shape::kSlotBytes, kTileKeys * 128);
+#pragma unroll
+                        for (int k = 0; k < kTileKeys / 16; ++k)
+                            ptx::mma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + 8 * k, b + (uint64_t)(k * 2048 >> 4), idesc_o,
+                                            now.t != now.t0 || k != 0);
+                        ptx::mma_commit(&tail->o_full[x]);
                     }
                     __syncwarp();
                 }
-                if (!ok) break;
+                if (u.more && u.t < u.end[x] && ok) qk(u, x, k_slot);
             }
-            if (!ok) break;
+            if (ptx::elect_one()) {
+                ptx::mma_commit(&tail->kv_empty[v_slot]);
+                if (u.more) ptx::mma_commit(&tail->kv_empty[k_slot]);
+            }
+            __syncwarp();
         }
         if (!ok) {                        // MMAs still running must end before shared memory and TMEM go away
             if (ptx::elect_one()) {
@@ -341,59 +398,26 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
             __syncwarp();
         }
-    } else if (warp < 8) {
+    } else if (warp > kQueryWarp) {
+        registers_to<false, kOtherRegs>();
+    } else {
         // ---------------- softmax: row tile x, one row per thread ----------------
+        registers_to<true, kSoftmaxRegs>();
         const int x = warp >> 2, quad = warp & 3;
         const int row = quad * 32 + lane;                          // of the row tile
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + 256 + x * D;
-        uint32_t s_phase = 0, o_phase = 0;                         // o_phase: parity of the last PV asked for
-        bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            ok = ok && tile_wait(bar, parity, tail, p);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            return ok;
-        };
-        for (; more && ok; more = walk.next(p.c)) {
+        const float scale = fabsf(p.scale);
+        const uint32_t flip = p.scale < 0.0f ? 0x80000000u : 0u;   // a negative scale: maxima are of the negated logits
+        uint32_t s_phase = 0, o_phase = 0;                         // o_phase: PVs asked for
+        for (bool more = any_work; more && ok; more = walk.next(p.c)) {
             const Item& it = walk.it;
-            const int rows_all = it.s.new_len * p.group;
-            const int tile_row = it.i * kTileRows + x * 128;       // first row of the row tile, among the sequence's
-            const int n = tile_count(sch, it, x);
-            const int t_end = min(it.t1, n);
-            const bool any = it.t0 < t_end;                        // this row tile sees keys of this block's units
-            // queries into the swizzled tile, 16 bytes a lane, two rows of D = 128 (four of D = 64) at a time.  Every MMA
-            // that read the last ones has been waited for.
-            if (any) {
-                constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks;
-                const int chunk = lane % kChunks, sub = lane / kChunks;
-                uint8_t* dst = q_smem + x * Shape::kQBytes + (chunk >> 3) * 128 * 128;
-                const bool flip = p.scale < 0.0f;
-#pragma unroll 4
-                for (int i = 0; i < 32 / kAtOnce; ++i) {
-                    const int r = quad * 32 + i * kAtOnce + sub;
-                    const int rr = tile_row + r;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (rr < rows_all) {
-                        const int tok = rr / p.group;
-                        v = *reinterpret_cast<const uint4*>(p.q + (long long)(it.s.first + tok) * p.q_stride +
-                                                            (long long)(it.h * p.group + rr - tok * p.group) * D + chunk * 8);
-                        if (flip) {
-                            v.x ^= 0x80008000u;
-                            v.y ^= 0x80008000u;
-                            v.z ^= 0x80008000u;
-                            v.w ^= 0x80008000u;
-                        }
-                    }
-                    *reinterpret_cast<uint4*>(dst + r * 128 + (((chunk & 7) ^ (r & 7)) * 16)) = v;
-                }
-                ptx::fence_proxy_async_smem();
-                ptx::mbar_arrive(&tail->q_full[x]);
-            }
-
-            const float scale = fabsf(p.scale);
-            const int limit = sch.key_limit(it.s, it.i);
-            int row_limit = limit;
-            if (p.causal && tile_row + row < rows_all) row_limit = it.s.len - it.s.new_len + (tile_row + row) / p.group + 1;
+            const int half = sch.rows >> 1;
+            const int item_row = it.i * sch.rows + x * half + row; // among the sequence's rows
+            const bool valid = row < half && item_row < it.s.new_len * p.group;
+            const int t_end = tile_end(sch, it, x);
+            int row_limit = sch.key_limit(it.s, it.i);
+            if (p.causal && valid) row_limit = it.s.len - it.s.new_len + item_row / p.group + 1;
             float m = -INFINITY;                                   // reference, in powers of two
             uint64_t sum2 = 0;                                     // two partial sums of P
             for (int t = it.t0; t < t_end; ++t) {
@@ -404,6 +428,12 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
                 for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(s_addr + c * 32, s[c]);
                 ptx::tmem_ld_wait();
+                if (flip != 0) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) s[c][e] ^= 0x80000000u;
+                }
                 const int seen = row_limit - t * kTileKeys;
                 if (__any_sync(0xFFFFFFFFu, seen < kTileKeys)) {
 #pragma unroll
@@ -463,6 +493,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
             if (!ok) break;
             // ---- the item's rows
+            const bool any = it.t0 < t_end;
             if (any) {
                 if (!wait(&tail->o_full[x], o_phase ^ 1u)) break;
                 ptx::tc_fence_after_sync();
@@ -470,13 +501,11 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             const float2 sums = unpack2(sum2);
             const float sum = sums.x + sums.y;
             const bool whole = it.t0 == 0 && it.t1 == it.units;
-            const int slot = 2 * blockIdx.x + (it.t0 == 0 ? 1 : 0);
-            const bool valid = tile_row + row < rows_all;
             const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-            const int tok = (tile_row + row) / p.group;
-            const int head = it.h * p.group + (tile_row + row) - tok * p.group;
+            const int tok = item_row / p.group;
+            const int head = it.h * p.group + item_row - tok * p.group;
             const long long token = it.s.first + tok;
-            const long long part_row = (long long)slot * kTileRows + x * 128 + row;
+            const long long part_row = (long long)(2 * blockIdx.x + (it.t0 == 0 ? 1 : 0)) * 256 + x * 128 + row;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 uint32_t o[32];
@@ -510,9 +539,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 PartItem pi;
                 pi.last = block_of(st.total, it.first_unit + it.units - 1, st.blocks);
                 pi.h = it.h;
-                pi.first_row = it.i * kTileRows;
-                pi.rows = min(kTileRows, rows_all - it.i * kTileRows);
+                pi.first_row = it.i * sch.rows;
+                pi.rows = min(sch.rows, it.s.new_len * p.group - it.i * sch.rows);
                 pi.first_token = it.s.first;
+                pi.tile_rows = half;
                 p.part_items[blockIdx.x] = pi;
             }
             ptx::tc_fence_before_sync();                           // O has been read: the next item's first PV may overwrite it
