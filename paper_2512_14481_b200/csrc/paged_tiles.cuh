@@ -64,11 +64,9 @@ namespace {
 // An item is two row tiles, each the tokens whose heads fit 128 MMA rows: 128 / group tokens, so that a row tile is one
 // box of q (of a group of five heads 125 rows are used).
 constexpr int kTileKeys = 128;            // keys of a unit
-constexpr int kTileThreads = 384;         // warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q; 11 idle
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10;
-// registers a thread: 168 at launch (384 x 168 of the SM's 65,536), then moved from the last four warps to the softmax,
-// which holds a row of 128 logits: 208 + 208 + 88 = 3 x 168
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+constexpr int kHalfKeys = 64;             // keys of a softmax step: S and P of one half in TMEM while the other half's S is made
+constexpr int kTileThreads = 384;         // warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q; 11: V's tails
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11;
 
 template <int D>
 struct TileShape {
@@ -79,8 +77,9 @@ struct TileShape {
 };
 
 struct TileTail {
-    uint64_t kv_full[8], kv_empty[8];
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+    uint64_t kv_full[8], kv_empty[8], raw_full[8];   // raw_full: a V tile whose last rows are still to be cleared
+    uint64_t q_full[2], q_empty[2];
+    uint64_t s_full[2][2], p_full[2][2], o_full[2][2];      // [row tile][half of the unit's keys]
     uint64_t drain;
     long long scratch[kTileThreads / 32];
     Start found;
@@ -162,10 +161,34 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return d;
 }
 
-template <bool MORE, int N>
-__device__ __forceinline__ void registers_to() {
-    if constexpr (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// Of every 8 pairs of a row this many take 2^x from a polynomial on the FMA pipe, the others from the special-function
+// unit (which needs 8 cycles per warp and exponential, as long as the two MMAs of the same logits take).
+#ifndef POLYP
+#define POLYP 0
+#endif
+constexpr int kPolyPairs = POLYP;
+
+// 2^x for two values: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), a polynomial
+// of degree 4 for 2^f on [-1/2, 1/2] (least maximum relative error, 2.6e-6, by Remez exchange), and n added to the exponent.
+// x below -125 counts as -125.
+__device__ __forceinline__ uint64_t exp2_poly(float2 x) {
+    const uint64_t z = pack2(fmaxf(x.x, -125.0f), fmaxf(x.y, -125.0f));
+    const uint64_t big = pack2(12582912.0f, 12582912.0f);
+    const uint64_t t = add2(z, big);
+    const uint64_t f = fma2(add2(t, pack2(-12582912.0f, -12582912.0f)), pack2(-1.0f, -1.0f), z);
+    uint64_t y = fma2(f, pack2(0.009570102207362652f, 0.009570102207362652f), pack2(0.05591785907745361f, 0.05591785907745361f));
+    y = fma2(y, f, pack2(0.240247443318367f, 0.240247443318367f));
+    y = fma2(y, f, pack2(0.6931217908859253f, 0.6931217908859253f));
+    y = fma2(y, f, pack2(0.9999992847442627f, 0.9999992847442627f));
+    const float2 n = unpack2(t), v = unpack2(y);
+    return pack2(__uint_as_float(__float_as_uint(v.x) + (__float_as_uint(n.x) << 23)),
+                 __uint_as_float(__float_as_uint(v.y) + (__float_as_uint(n.y) << 23)));
 }
 
 // Two row tiles x = 0, 1 share every K and V tile.  Per unit and row tile:
@@ -191,13 +214,16 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         for (int s = 0; s < Shape::kSlots; ++s) {
             ptx::mbar_init(&tail->kv_full[s], 1);
             ptx::mbar_init(&tail->kv_empty[s], 1);
+            ptx::mbar_init(&tail->raw_full[s], 1);
         }
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&tail->q_full[x], 1);
             ptx::mbar_init(&tail->q_empty[x], 1);
-            ptx::mbar_init(&tail->s_full[x], 1);
-            ptx::mbar_init(&tail->p_full[x], 128);
-            ptx::mbar_init(&tail->o_full[x], 1);
+            for (int half = 0; half < 2; ++half) {
+                ptx::mbar_init(&tail->s_full[x][half], 1);
+                ptx::mbar_init(&tail->p_full[x][half], 128);
+                ptx::mbar_init(&tail->o_full[x][half], 1);
+            }
         }
         ptx::mbar_init(&tail->drain, 1);
         tail->abort_flag = 0;
@@ -230,10 +256,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         return ok;
     };
 
-    // every role sets its registers inside its own branch: the compiler allots them by the branch's last such instruction
     if (warp == kLoadWarp) {
         // ---------------- K and V of each unit, in turn, a lane per page ----------------
-        registers_to<false, kOtherRegs>();
         int slot = 0;
         uint32_t phase = 0;
         const int box = min(1 << p.c.page_shift, kTileKeys);
@@ -252,13 +276,15 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 if (!wait(&tail->kv_empty[slot], phase ^ 1u)) break;
-                if (lane == 0) ptx::mbar_arrive_expect_tx(&tail->kv_full[slot], Shape::kSlotBytes);
+                // a V tile that ends behind the sequence's last key goes to the warp that clears its tail first
+                uint64_t* full = kv == 1 && walk.it.s.len - u.t * kTileKeys < kTileKeys ? &tail->raw_full[slot] : &tail->kv_full[slot];
+                if (lane == 0) ptx::mbar_arrive_expect_tx(full, Shape::kSlotBytes);
                 __syncwarp();
                 if (lane < boxes) {
                     const uint32_t dst = ptx::smem_u32(ring) + slot * Shape::kSlotBytes + lane * box * 128;
 #pragma unroll
                     for (int half = 0; half < Shape::kHalves; ++half)
-                        ptx::tma_load_4d(dst + half * kTileKeys * 128, kv == 0 ? &map_k : &map_v, &tail->kv_full[slot], half * 64,
+                        ptx::tma_load_4d(dst + half * kTileKeys * 128, kv == 0 ? &map_k : &map_v, full, half * 64,
                                          key & page_mask, walk.it.h, page);
                 }
                 __syncwarp();
@@ -266,6 +292,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         }
         // gave up: copies still in flight must land before the block's shared memory goes away
+        // (a tile with a tail to clear may never be announced; the limit is far above a copy's flight)
         if (!ok && lane == 0) {
             for (int s = 0; s < Shape::kSlots; ++s) {
                 const long long t0 = clock64();
@@ -277,7 +304,6 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         __syncwarp();
     } else if (warp == kQueryWarp) {
         // ---------------- Q of each item ----------------
-        registers_to<false, kOtherRegs>();
         uint32_t filled[2] = {0, 0};                            // times that each row tile's queries were asked for
         const int tokens = 128 / p.group;
         for (bool more = any_work; more && ok; more = walk.next(p.c)) {
@@ -305,111 +331,122 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        // ---------------- MMAs ----------------
-        registers_to<false, kOtherRegs>();
-        constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, BF);
-        constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF) | ptx::kIdescBTransposed;
-        int slot = 0;
-        uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-        auto advance = [&] { if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; } };
-        const uint32_t ring_addr = ptx::smem_u32(ring), q_addr = ptx::smem_u32(q_smem);
-        // S of row tile x for unit u, whose keys are in k_slot
-        auto qk = [&](const Unit& u, int x, int k_slot) {
-            if (u.t == u.t0) {
-                if (!wait(&tail->q_full[x], q_phase[x])) return;
-                q_phase[x] ^= 1u;
-            }
-            ptx::tc_fence_after_sync();
-            if (ptx::elect_one()) {
-                const uint64_t a = ptx::smem_desc_k_major_sw128(q_addr + x * Shape::kQBytes);
-                const uint64_t b = ptx::smem_desc_k_major_sw128(ring_addr + k_slot * Shape::kSlotBytes);
+        // ---------------- MMAs, all by one lane (which lets the descriptors live in uniform registers) ----------------
+        if (ptx::elect_one()) {
+            constexpr uint32_t idesc_s = ptx::idesc_f16(128, kHalfKeys, BF);
+            constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF) | ptx::kIdescBTransposed;
+            int slot = 0;
+            uint32_t phase = 0, q_phase = 0, p_phase = 0;             // q_phase, p_phase: a bit per row tile
+            auto advance = [&] { if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; } };
+            const uint64_t q_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(q_smem));
+            const uint64_t k_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(ring));
+            const uint64_t v_desc = ptx::smem_desc_mn_major_sw128(ptx::smem_u32(ring), kTileKeys * 128);
+            // S of row tile x for half `part` of unit u, whose keys are in k_slot
+            auto qk = [&](const Unit& u, int x, int part, int k_slot) {
+                if (u.t == u.t0 && part == 0) {
+                    ok = ok && tile_wait(&tail->q_full[x], q_phase >> x & 1u, tail, p);
+                    if (!ok) return;
+                    q_phase ^= 1u << x;
+                    ptx::tc_fence_after_sync();
+                }
+                const uint64_t a = q_desc + (uint64_t)(x * (Shape::kQBytes >> 4));
+                const uint64_t b = k_desc + (uint64_t)(k_slot * (Shape::kSlotBytes >> 4) + part * (kHalfKeys * 128 >> 4));
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint64_t at = (uint64_t)(((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4);
-                    ptx::mma_f16_ss(tmem + x * 128, a + at, b + at, idesc_s, k != 0);
+                    ptx::mma_f16_ss(tmem + x * 128 + part * kHalfKeys, a + at, b + at, idesc_s, k != 0);
                 }
-                ptx::mma_commit(&tail->s_full[x]);
-                if (u.t + 1 == u.end[x]) ptx::mma_commit(&tail->q_empty[x]);
+                ptx::mma_commit(&tail->s_full[x][part]);
+                if (u.t + 1 == u.end[x] && part == 1) ptx::mma_commit(&tail->q_empty[x]);
+            };
+            Unit u;
+            u.more = any_work;
+            u.enter(p.c, sch, walk);
+            if (u.more) {
+                ok = tile_wait(&tail->kv_full[slot], phase, tail, p);
+                ptx::tc_fence_after_sync();
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (u.t < u.end[x] && ok) qk(u, x, part, slot);
+                ptx::mma_commit(&tail->kv_empty[slot]);
+                advance();
             }
-            __syncwarp();
-        };
+            while (u.more && ok) {
+                const Unit now = u;
+                const int v_slot = slot;
+                ok = tile_wait(&tail->kv_full[v_slot], phase, tail, p);
+                advance();
+                const int k_slot = slot;
+                u.next(p.c, sch, walk);
+                if (u.more && ok) {
+                    ok = tile_wait(&tail->kv_full[k_slot], phase, tail, p);
+                    advance();
+                }
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (now.t < now.end[x] && ok) {
+                            ok = tile_wait(&tail->p_full[x][part], p_phase >> x & 1u, tail, p);
+                            if (!ok) break;
+                            if (part == 1) p_phase ^= 1u << x;
+                            ptx::tc_fence_after_sync();
+                            const uint64_t b = v_desc + (uint64_t)(v_slot * (Shape::kSlotBytes >> 4) + part * (kHalfKeys * 128 >> 4));
+#pragma unroll
+                            for (int k = 0; k < kHalfKeys / 16; ++k)
+                                ptx::mma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + part * kHalfKeys + 8 * k, b + (uint64_t)(k * 2048 >> 4),
+                                                idesc_o, now.t != now.t0 || part != 0 || k != 0);
+                            ptx::mma_commit(&tail->o_full[x][part]);
+                        }
+                        if (u.more && u.t < u.end[x] && ok) qk(u, x, part, k_slot);
+                    }
+                }
+                ptx::mma_commit(&tail->kv_empty[v_slot]);
+                if (u.more) ptx::mma_commit(&tail->kv_empty[k_slot]);
+            }
+            if (!ok) {                    // MMAs still running must end before shared memory and TMEM go away
+                ptx::mma_commit(&tail->drain);
+                const long long t0 = clock64();
+                while (!ptx::mbar_try_wait(&tail->drain, 0))
+                    if (clock64() - t0 > (1LL << 24)) break;
+            }
+        }
+        __syncwarp();
+    } else if (warp == kTailWarp) {
+        // ---------------- rows of V behind a sequence's last key ----------------
+        // Whatever they hold is multiplied by P = 0, and must be finite.  The copy of such a tile is announced here, and
+        // the MMAs learn of it when the rows are zero.
+        int slot = 1;                                               // of the unit's V: slots go K, V, K, V, ...
+        uint32_t phases = 0;                                        // a bit per slot
         Unit u;
         u.more = any_work;
-        u.enter(p.c, sch, walk);
-        if (u.more && wait(&tail->kv_full[slot], phase)) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                if (u.t < u.end[x] && ok) qk(u, x, slot);
-            if (ptx::elect_one()) ptx::mma_commit(&tail->kv_empty[slot]);
-            __syncwarp();
-            advance();
-        }
-        while (u.more && ok) {
-            const Unit now = u;
-            const int v_slot = slot, valid = walk.it.s.len - now.t * kTileKeys;
-            u.next(p.c, sch, walk);
-            if (!wait(&tail->kv_full[v_slot], phase)) break;
-            // rows of V behind the sequence's last key: whatever they hold is multiplied by P = 0, and must be finite
+        for (u.enter(p.c, sch, walk); u.more && ok; u.next(p.c, sch, walk)) {
+            const int valid = walk.it.s.len - u.t * kTileKeys;
             if (valid < kTileKeys) {
-                uint8_t* v = ring + (size_t)v_slot * Shape::kSlotBytes + valid * 128;
+                if (!wait(&tail->raw_full[slot], phases >> slot & 1u)) break;
+                phases ^= 1u << slot;
+                uint8_t* v = ring + (size_t)slot * Shape::kSlotBytes + valid * 128;
                 for (int y = lane; y < (kTileKeys - valid) * 8; y += 32)
 #pragma unroll
                     for (int half = 0; half < Shape::kHalves; ++half)
                         *reinterpret_cast<uint4*>(v + half * kTileKeys * 128 + y * 16) = make_uint4(0, 0, 0, 0);
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&tail->kv_full[slot]);
             }
-            advance();
-            const int k_slot = slot;
-            if (u.more) {
-                if (!wait(&tail->kv_full[k_slot], phase)) break;
-                advance();
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (now.t < now.end[x] && ok) {
-                    if (!wait(&tail->p_full[x], p_phase[x])) break;
-                    p_phase[x] ^= 1u;
-                    ptx::tc_fence_after_sync();
-                    if (ptx::elect_one()) {
-                        const uint64_t b = ptx::smem_desc_mn_major_sw128(ring_addr + v_slot * Shape::kSlotBytes, kTileKeys * 128);
-#pragma unroll
-                        for (int k = 0; k < kTileKeys / 16; ++k)
-                            ptx::mma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + 8 * k, b + (uint64_t)(k * 2048 >> 4), idesc_o,
-                                            now.t != now.t0 || k != 0);
-                        ptx::mma_commit(&tail->o_full[x]);
-                    }
-                    __syncwarp();
-                }
-                if (u.more && u.t < u.end[x] && ok) qk(u, x, k_slot);
-            }
-            if (ptx::elect_one()) {
-                ptx::mma_commit(&tail->kv_empty[v_slot]);
-                if (u.more) ptx::mma_commit(&tail->kv_empty[k_slot]);
-            }
-            __syncwarp();
+            slot = (slot + 2) % Shape::kSlots;
         }
-        if (!ok) {                        // MMAs still running must end before shared memory and TMEM go away
-            if (ptx::elect_one()) {
-                ptx::mma_commit(&tail->drain);
-                const long long t0 = clock64();
-                while (!ptx::mbar_try_wait(&tail->drain, 0))
-                    if (clock64() - t0 > (1LL << 24)) break;
-            }
-            __syncwarp();
-        }
-    } else if (warp > kQueryWarp) {
-        registers_to<false, kOtherRegs>();
     } else {
         // ---------------- softmax: row tile x, one row per thread ----------------
-        registers_to<true, kSoftmaxRegs>();
         const int x = warp >> 2, quad = warp & 3;
         const int row = quad * 32 + lane;                          // of the row tile
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + 256 + x * D;
         const float scale = fabsf(p.scale);
         const uint32_t flip = p.scale < 0.0f ? 0x80000000u : 0u;   // a negative scale: maxima are of the negated logits
-        uint32_t s_phase = 0, o_phase = 0;                         // o_phase: PVs asked for
+        uint32_t s_phase = 0;                                      // parity of the unit whose S is waited for
         for (bool more = any_work; more && ok; more = walk.next(p.c)) {
             const Item& it = walk.it;
             const int half = sch.rows >> 1;
@@ -420,44 +457,44 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (p.causal && valid) row_limit = it.s.len - it.s.new_len + item_row / p.group + 1;
             float m = -INFINITY;                                   // reference, in powers of two
             uint64_t sum2 = 0;                                     // two partial sums of P
-            for (int t = it.t0; t < t_end; ++t) {
-                if (!wait(&tail->s_full[x], s_phase)) break;
-                s_phase ^= 1u;
+            for (int h = 2 * it.t0; h < 2 * t_end; ++h) {          // halves of units
+                const int part = h & 1;
+                // S(h) was asked for behind the second product of h - 2, which is therefore done as well: of the products
+                // only that of h - 1 can be outstanding, and a parity of its barrier is not mistaken for an older one
+                if (!wait(&tail->s_full[x][part], s_phase)) break;
+                if (part == 1) s_phase ^= 1u;
                 ptx::tc_fence_after_sync();
-                uint32_t s[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(s_addr + c * 32, s[c]);
+                uint32_t s[2][32];
+                ptx::tmem_ld_32x32(s_addr + part * kHalfKeys, s[0]);
+                ptx::tmem_ld_32x32(s_addr + part * kHalfKeys + 32, s[1]);
                 ptx::tmem_ld_wait();
                 if (flip != 0) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) s[c][e] ^= 0x80000000u;
+                    for (int e = 0; e < 64; ++e) s[e >> 5][e & 31] ^= 0x80000000u;
                 }
-                const int seen = row_limit - t * kTileKeys;
-                if (__any_sync(0xFFFFFFFFu, seen < kTileKeys)) {
+                const int seen = row_limit - h * kHalfKeys;
+                if (__any_sync(0xFFFFFFFFu, seen < kHalfKeys)) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (c * 32 + e >= seen) s[c][e] = 0xFF800000u;      // -inf
+                    for (int e = 0; e < 64; ++e)
+                        if (e >= seen) s[e >> 5][e & 31] = 0xFF800000u;      // -inf
                 }
                 float top[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    top[c] = __uint_as_float(s[c][0]);
+                    const uint32_t* w = s[c >> 1] + 16 * (c & 1);
+                    top[c] = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 #pragma unroll
-                    for (int e = 1; e < 32; ++e) top[c] = fmaxf(top[c], __uint_as_float(s[c][e]));
+                    for (int e = 2; e < 16; e += 2) top[c] = max3(top[c], __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
                 }
-                const float tile_max = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
-                if (__any_sync(0xFFFFFFFFu, tile_max > m + kRescaleAt)) {
-                    const float m_new = fmaxf(m, tile_max);
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+                if (__any_sync(0xFFFFFFFFu, most > m + kRescaleAt)) {
+                    const float m_new = fmaxf(m, most);
                     const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m - m_new);
                     m = m_new;
                     const float2 old = unpack2(sum2);
                     sum2 = pack2(old.x * f, old.y * f);
-                    if (t > it.t0) {
-                        if (!wait(&tail->o_full[x], o_phase ^ 1u)) break;
+                    if (h > 2 * it.t0) {
+                        if (!wait(&tail->o_full[x][part ^ 1], s_phase ^ 1u)) break;
                         ptx::tc_fence_after_sync();
 #pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
@@ -472,34 +509,35 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 const float ref = m == -INFINITY ? 0.0f : m;
                 const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-ref, -ref);
+                uint32_t pk[32];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t pk[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int col = c * 64 + 2 * e;
-                        const float2 z = unpack2(fma2(pack2(__uint_as_float(s[col >> 5][col & 31]), __uint_as_float(s[col >> 5][(col & 31) + 1])),
-                                                      scale2, ref2));
-                        const float p0 = exp2_approx(z.x), p1 = exp2_approx(z.y);
-                        sum2 = add2(sum2, pack2(p0, p1));
-                        pk[e] = narrow2<BF>(p0, p1);
+                for (int e = 0; e < 32; ++e) {
+                    const float2 z = unpack2(fma2(pack2(__uint_as_float(s[e >> 4][2 * e & 31]), __uint_as_float(s[e >> 4][(2 * e & 31) + 1])),
+                                                  scale2, ref2));
+                    uint64_t pr;
+                    if (e % 8 < kPolyPairs) {
+                        pr = exp2_poly(z);
+                    } else {
+                        pr = pack2(exp2_approx(z.x), exp2_approx(z.y));
                     }
-                    ptx::tmem_st_32x32(s_addr + c * 32, pk);
+                    sum2 = add2(sum2, pr);
+                    const float2 both = unpack2(pr);
+                    pk[e] = narrow2<BF>(both.x, both.y);
                 }
+                ptx::tmem_st_32x32(s_addr + part * kHalfKeys, pk);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before_sync();
-                ptx::mbar_arrive(&tail->p_full[x]);
-                o_phase ^= 1u;
+                ptx::mbar_arrive(&tail->p_full[x][part]);
             }
             if (!ok) break;
             // ---- the item's rows
             const bool any = it.t0 < t_end;
             if (any) {
-                if (!wait(&tail->o_full[x], o_phase ^ 1u)) break;
+                if (!wait(&tail->o_full[x][1], s_phase ^ 1u)) break;
                 ptx::tc_fence_after_sync();
             }
             const float2 sums = unpack2(sum2);
-            const float sum = sums.x + sums.y;
+            const float sum = m == -INFINITY ? 0.0f : sums.x + sums.y;   // no key: exp2_poly is not quite 0 at -inf
             const bool whole = it.t0 == 0 && it.t1 == it.units;
             const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
             const int tok = item_row / p.group;
