@@ -52,7 +52,7 @@ Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, in
     Plan pl{};
     const int group = heads / c->num_kv_heads;
     const long long rows = (long long)b->max_q_len * group;
-    pl.tiles = rows > 16 && group <= 128 && c->kind == SASQ_KV_16BIT && c->num_pages > 0;
+    pl.tiles = rows > 16 && group <= 128 && c->num_pages > 0;
     pl.nb = rows <= 8 ? 1 : 2;
     pl.rows = pl.tiles ? 2 * (128 / group * group) : 8 * pl.nb;
     pl.slot_rows = pl.tiles ? 256 : pl.rows;
@@ -143,29 +143,29 @@ bool encode_queries(CUtensorMap* m, const AttendParams& p) {
     return encode_map<BF>(m, const_cast<uint16_t*>(p.q), 3, dims, strides, box);
 }
 
-template <int D, bool BF>
+template <int D, bool BF, bool INT8>
 cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
     static std::atomic<unsigned long long> ready{0};          // devices whose shared-memory limit has been raised
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (!(ready.load() >> (dev & 63) & 1)) {
-        e = cudaFuncSetAttribute(paged_tiles_kernel<D, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTileSmem<D>);
+        e = cudaFuncSetAttribute(paged_tiles_kernel<D, BF, INT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTileSmem<D>);
         if (e != cudaSuccess) return e;
         ready.fetch_or(1ull << (dev & 63));
     }
-    CUtensorMap map_q, map_k, map_v;
-    if (!encode_queries<D, BF>(&map_q, p) || !encode_pages<D, BF>(&map_k, c, c->k) || !encode_pages<D, BF>(&map_v, c, c->v))
-        return cudaErrorInvalidValue;
+    CUtensorMap map_q{}, map_k{}, map_v{};
+    if (!encode_queries<D, BF>(&map_q, p)) return cudaErrorInvalidValue;
+    if (!INT8 && (!encode_pages<D, BF>(&map_k, c, c->k) || !encode_pages<D, BF>(&map_v, c, c->v))) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)p.max_blocks);
-    cfg.blockDim = dim3(kTileThreads);
+    cfg.blockDim = dim3(kTileThreads<INT8>);
     cfg.dynamicSmemBytes = kTileSmem<D>;
     cfg.stream = st;
     cudaLaunchAttribute attr = pdl_attribute();
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF>, map_q, map_k, map_v, p);
+    e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF, INT8>, map_q, map_k, map_v, p);
     if (e != cudaSuccess || !p.split) return e;
     return launch(paged_join_kernel<256, 128, D, BF>, dim3(p.max_blocks, 256 / 8), 256, 0, st, p);
 }
@@ -173,7 +173,7 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, cudaSt
 template <int D, bool BF>
 cudaError_t launch_all(const Plan& pl, const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
     const bool int8 = c->kind == SASQ_KV_INT8;
-    if (pl.tiles) return launch_tiles<D, BF>(p, c, st);
+    if (pl.tiles) return int8 ? launch_tiles<D, BF, true>(p, c, st) : launch_tiles<D, BF, false>(p, c, st);
     return pl.nb == 1 ? launch_rows<D, 1, BF>(p, int8, st) : launch_rows<D, 2, BF>(p, int8, st);
 }
 

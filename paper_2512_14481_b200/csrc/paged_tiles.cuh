@@ -41,6 +41,13 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t* v)
           "r"(v[30]), "r"(v[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+          "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Descriptor of an operand whose contraction index runs along the ROWS of the same 128-byte-swizzled tile (MN-major):
@@ -64,9 +71,14 @@ namespace {
 // An item is two row tiles, each the tokens whose heads fit 128 MMA rows: 128 / group tokens, so that a row tile is one
 // box of q (of a group of five heads 125 rows are used).
 constexpr int kTileKeys = 128;            // keys of a unit
-constexpr int kHalfKeys = 64;             // keys of a softmax step: S and P of one half in TMEM while the other half's S is made
-constexpr int kTileThreads = 384;         // warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q; 11: V's tails
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11;
+// Warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q; 11: V's tails.  With an int8 cache warps
+// 12-15 fetch and convert K and V, and 9 and 11 are idle.
+template <bool INT8>
+constexpr int kTileThreads = INT8 ? 512 : 384;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11, kConvertWarp = 12;
+// Registers of a thread.  384 threads get 168 each, enough for every role.  512 get 128 at launch, of which the four-warp
+// groups without a row of logits give some to the softmax: 144 + 144 + 112 + 112 = 4 x 128.
+constexpr int kSoftmaxRegs = 144, kOtherRegs = 112;
 
 template <int D>
 struct TileShape {
@@ -79,9 +91,9 @@ struct TileShape {
 struct TileTail {
     uint64_t kv_full[8], kv_empty[8], raw_full[8];   // raw_full: a V tile whose last rows are still to be cleared
     uint64_t q_full[2], q_empty[2];
-    uint64_t s_full[2][2], p_full[2][2], o_full[2][2];      // [row tile][half of the unit's keys]
+    uint64_t s_full[2], p_full[2][2], o_full[2];            // p_full: either half of the unit's keys
     uint64_t drain;
-    long long scratch[kTileThreads / 32];
+    long long scratch[16];
     Start found;
     uint32_t tmem_base;
     volatile int abort_flag;
@@ -191,6 +203,86 @@ __device__ __forceinline__ uint64_t exp2_poly(float2 x) {
                  __uint_as_float(__float_as_uint(v.y) + (__float_as_uint(n.y) << 23)));
 }
 
+// The warps that fill the ring from an int8 cache (128 threads, `me` of them): K and V of each unit in turn, in the layout
+// that the 16-bit copies leave: keys along the rows, 128-byte swizzle.  Keys behind the sequence's last are zeros.
+template <int D, bool BF>
+__device__ __forceinline__ void convert_tiles(const AttendParams& p, const TileSchedule& sch, TileWalk& walk, bool any_work, int me,
+                                              uint8_t* ring, TileTail* tail) {
+    using Shape = TileShape<D>;
+    constexpr int kWords = D / 16;                 // 16-byte words of a key's codes; as many steps make a tile
+    constexpr int kKeys = 128 / kWords;            // keys of a step
+    const int word = me % kWords, first = me / kWords;
+    const int page_mask = (1 << p.c.page_shift) - 1;
+    // the word's two chunks of 8 elements; half a row's lanes store the second first, which spreads them over the banks
+    uint8_t* const column = ring + (word >> 2) * kTileKeys * 128;
+    const int chunk = 2 * (word & 3), turn = word >> 2 & 1;
+    Unit u;
+    u.more = any_work;
+    u.enter(p.c, sch, walk);
+    int pages[kWords];                             // of this thread's keys of the unit, -1: no key
+    auto look_up = [&] {
+        const int* table = p.c.page_table + walk.it.b * p.c.table_stride;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const int key = u.t * kTileKeys + i * kKeys + first;
+            pages[i] = key < walk.it.s.len ? __ldg(table + (key >> p.c.page_shift)) : -1;
+            if (key < walk.it.s.len && (pages[i] < 0 || pages[i] >= p.c.num_pages)) {
+                atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
+                pages[i] = -1;
+            }
+        }
+    };
+    auto load = [&](const void* base, uint4 (&v)[kWords]) {
+        const char* head = static_cast<const char*>(base) + walk.it.h * p.c.head_stride + word * 16;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const int row = (u.t * kTileKeys + i * kKeys + first) & page_mask;
+            v[i] = pages[i] >= 0 ? ldg_stream16(head + pages[i] * p.c.page_stride + row * p.c.token_stride) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    auto store = [&](const uint4 (&v)[kWords]) {
+        ok = ok && tile_wait(&tail->kv_empty[slot], phase ^ 1u, tail, p);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) return;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const int r = i * kKeys + first;
+            uint8_t* row = column + (size_t)slot * Shape::kSlotBytes + r * 128;
+            const uint32_t lo[4] = {codes_to_pair<BF, 0>(v[i].x), codes_to_pair<BF, 1>(v[i].x), codes_to_pair<BF, 0>(v[i].y),
+                                    codes_to_pair<BF, 1>(v[i].y)};
+            const uint32_t hi[4] = {codes_to_pair<BF, 0>(v[i].z), codes_to_pair<BF, 1>(v[i].z), codes_to_pair<BF, 0>(v[i].w),
+                                    codes_to_pair<BF, 1>(v[i].w)};
+            uint4 a = make_uint4(lo[0], lo[1], lo[2], lo[3]), b = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            if (turn) {
+                const uint4 c = a;
+                a = b;
+                b = c;
+            }
+            *reinterpret_cast<uint4*>(row + (((chunk + turn) ^ (r & 7)) << 4)) = a;
+            *reinterpret_cast<uint4*>(row + (((chunk + (turn ^ 1)) ^ (r & 7)) << 4)) = b;
+        }
+        ptx::fence_proxy_async_smem();
+        ptx::mbar_arrive(&tail->kv_full[slot]);
+        if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; }
+    };
+    uint4 k[kWords], v[kWords];
+    if (u.more) {
+        look_up();
+        load(p.c.k, k);
+    }
+    while (u.more && ok) {
+        load(p.c.v, v);
+        u.next(p.c, sch, walk);
+        if (u.more) look_up();
+        store(k);
+        if (u.more) load(p.c.k, k);
+        store(v);
+    }
+}
+
 // Two row tiles x = 0, 1 share every K and V tile.  Per unit and row tile:
 //   S = Q K^T       (MMA, both operands in shared memory, S in TMEM)
 //   P = 2^(scale S - m), row sums, P back to TMEM over S as 16-bit pairs     (one thread per row, 4 warps per row tile)
@@ -198,8 +290,16 @@ __device__ __forceinline__ uint64_t exp2_poly(float2 x) {
 // While the softmax warps of one row tile work, the MMAs of the other run.  S of the next unit is asked for right behind
 // the PV that frees it, across items too: the next item's queries are fetched as soon as the last QK has read the old
 // ones, so that its first S is there when the softmax warps have stored the old item's rows.
-template <int D, bool BF>
-__global__ void __launch_bounds__(kTileThreads, 1)
+template <bool INT8, bool MORE, int N>
+__device__ __forceinline__ void registers_to() {
+    if constexpr (INT8) {
+        if constexpr (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+    }
+}
+
+template <int D, bool BF, bool INT8>
+__global__ void __launch_bounds__(kTileThreads<INT8>, 1)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendParams p) {
     using Shape = TileShape<D>;
@@ -212,25 +312,26 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
     if (tid == 0) {
         for (int s = 0; s < Shape::kSlots; ++s) {
-            ptx::mbar_init(&tail->kv_full[s], 1);
+            ptx::mbar_init(&tail->kv_full[s], INT8 ? 128 : 1);
             ptx::mbar_init(&tail->kv_empty[s], 1);
             ptx::mbar_init(&tail->raw_full[s], 1);
         }
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&tail->q_full[x], 1);
             ptx::mbar_init(&tail->q_empty[x], 1);
-            for (int half = 0; half < 2; ++half) {
-                ptx::mbar_init(&tail->s_full[x][half], 1);
-                ptx::mbar_init(&tail->p_full[x][half], 128);
-                ptx::mbar_init(&tail->o_full[x][half], 1);
-            }
+            ptx::mbar_init(&tail->s_full[x], 1);
+            ptx::mbar_init(&tail->p_full[x][0], 128);
+            ptx::mbar_init(&tail->p_full[x][1], 128);
+            ptx::mbar_init(&tail->o_full[x], 1);
         }
         ptx::mbar_init(&tail->drain, 1);
         tail->abort_flag = 0;
         ptx::mbar_init_fence();
         ptx::prefetch_tensormap(&map_q);
-        ptx::prefetch_tensormap(&map_k);
-        ptx::prefetch_tensormap(&map_v);
+        if constexpr (!INT8) {
+            ptx::prefetch_tensormap(&map_k);
+            ptx::prefetch_tensormap(&map_v);
+        }
     }
     if (warp == kMmaWarp) {
         ptx::tmem_alloc(&tail->tmem_base, 512);
@@ -244,7 +345,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     pdl_wait();
 
     const TileSchedule sch{p.item_rows, p.group, p.causal, p.c.kv_heads};
-    const Start st = find_start<kTileThreads, kTileKeys>(p.c, sch, p.max_blocks, p.min_units, tail->scratch, &tail->found);
+    const Start st = find_start<kTileThreads<INT8>, kTileKeys>(p.c, sch, p.max_blocks, p.min_units, tail->scratch, &tail->found);
     if (tid == 0) p.part_items[blockIdx.x].last = -1;
     TileWalk walk;
     const bool any_work = walk.begin(p.c, sch, st, p.split != 0);
@@ -257,6 +358,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     };
 
     if (warp == kLoadWarp) {
+        registers_to<INT8, false, kOtherRegs>();
         // ---------------- K and V of each unit, in turn, a lane per page ----------------
         int slot = 0;
         uint32_t phase = 0;
@@ -264,7 +366,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int boxes = kTileKeys / box;
         const int page_mask = (1 << p.c.page_shift) - 1;
         Unit u;
-        u.more = any_work;
+        u.more = any_work && !INT8;
         for (u.enter(p.c, sch, walk); u.more && ok; u.next(p.c, sch, walk)) {
             const int key = u.t * kTileKeys + lane * box;
             int page = (int)p.c.num_pages;                      // outside the cache: the copy fills in zeros
@@ -303,6 +405,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
     } else if (warp == kQueryWarp) {
+        registers_to<INT8, false, kOtherRegs>();
         // ---------------- Q of each item ----------------
         uint32_t filled[2] = {0, 0};                            // times that each row tile's queries were asked for
         const int tokens = 128 / p.group;
@@ -331,9 +434,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
+        registers_to<INT8, false, kOtherRegs>();
         // ---------------- MMAs, all by one lane (which lets the descriptors live in uniform registers) ----------------
         if (ptx::elect_one()) {
-            constexpr uint32_t idesc_s = ptx::idesc_f16(128, kHalfKeys, BF);
+            constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, BF);
             constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF) | ptx::kIdescBTransposed;
             int slot = 0;
             uint32_t phase = 0, q_phase = 0, p_phase = 0;             // q_phase, p_phase: a bit per row tile
@@ -341,23 +445,23 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const uint64_t q_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(q_smem));
             const uint64_t k_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(ring));
             const uint64_t v_desc = ptx::smem_desc_mn_major_sw128(ptx::smem_u32(ring), kTileKeys * 128);
-            // S of row tile x for half `part` of unit u, whose keys are in k_slot
-            auto qk = [&](const Unit& u, int x, int part, int k_slot) {
-                if (u.t == u.t0 && part == 0) {
+            // S of row tile x for unit u, whose keys are in k_slot
+            auto qk = [&](const Unit& u, int x, int k_slot) {
+                if (u.t == u.t0) {
                     ok = ok && tile_wait(&tail->q_full[x], q_phase >> x & 1u, tail, p);
                     if (!ok) return;
                     q_phase ^= 1u << x;
                     ptx::tc_fence_after_sync();
                 }
                 const uint64_t a = q_desc + (uint64_t)(x * (Shape::kQBytes >> 4));
-                const uint64_t b = k_desc + (uint64_t)(k_slot * (Shape::kSlotBytes >> 4) + part * (kHalfKeys * 128 >> 4));
+                const uint64_t b = k_desc + (uint64_t)(k_slot * (Shape::kSlotBytes >> 4));
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint64_t at = (uint64_t)(((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4);
-                    ptx::mma_f16_ss(tmem + x * 128 + part * kHalfKeys, a + at, b + at, idesc_s, k != 0);
+                    ptx::mma_f16_ss(tmem + x * 128, a + at, b + at, idesc_s, k != 0);
                 }
-                ptx::mma_commit(&tail->s_full[x][part]);
-                if (u.t + 1 == u.end[x] && part == 1) ptx::mma_commit(&tail->q_empty[x]);
+                ptx::mma_commit(&tail->s_full[x]);
+                if (u.t + 1 == u.end[x]) ptx::mma_commit(&tail->q_empty[x]);
             };
             Unit u;
             u.more = any_work;
@@ -366,10 +470,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ok = tile_wait(&tail->kv_full[slot], phase, tail, p);
                 ptx::tc_fence_after_sync();
 #pragma unroll
-                for (int part = 0; part < 2; ++part)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-                        if (u.t < u.end[x] && ok) qk(u, x, part, slot);
+                for (int x = 0; x < 2; ++x)
+                    if (u.t < u.end[x] && ok) qk(u, x, slot);
                 ptx::mma_commit(&tail->kv_empty[slot]);
                 advance();
             }
@@ -385,23 +487,24 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     advance();
                 }
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
+                for (int x = 0; x < 2; ++x) {
+                    if (now.t < now.end[x]) {
+                        // the first half's keys are multiplied while the softmax warps work on the second's
+                        const uint64_t b = v_desc + (uint64_t)(v_slot * (Shape::kSlotBytes >> 4));
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (now.t < now.end[x] && ok) {
-                            ok = tile_wait(&tail->p_full[x][part], p_phase >> x & 1u, tail, p);
+                        for (int part = 0; part < 2; ++part) {
+                            ok = ok && tile_wait(&tail->p_full[x][part], p_phase >> x & 1u, tail, p);
                             if (!ok) break;
-                            if (part == 1) p_phase ^= 1u << x;
                             ptx::tc_fence_after_sync();
-                            const uint64_t b = v_desc + (uint64_t)(v_slot * (Shape::kSlotBytes >> 4) + part * (kHalfKeys * 128 >> 4));
 #pragma unroll
-                            for (int k = 0; k < kHalfKeys / 16; ++k)
-                                ptx::mma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + part * kHalfKeys + 8 * k, b + (uint64_t)(k * 2048 >> 4),
-                                                idesc_o, now.t != now.t0 || part != 0 || k != 0);
-                            ptx::mma_commit(&tail->o_full[x][part]);
+                            for (int k = 4 * part; k < 4 * part + 4; ++k)
+                                ptx::mma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + 8 * k, b + (uint64_t)(k * 2048 >> 4), idesc_o,
+                                                now.t != now.t0 || k != 0);
                         }
-                        if (u.more && u.t < u.end[x] && ok) qk(u, x, part, k_slot);
+                        p_phase ^= 1u << x;
+                        ptx::mma_commit(&tail->o_full[x]);
                     }
+                    if (u.more && u.t < u.end[x] && ok) qk(u, x, k_slot);
                 }
                 ptx::mma_commit(&tail->kv_empty[v_slot]);
                 if (u.more) ptx::mma_commit(&tail->kv_empty[k_slot]);
@@ -415,13 +518,14 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
     } else if (warp == kTailWarp) {
+        registers_to<INT8, false, kOtherRegs>();
         // ---------------- rows of V behind a sequence's last key ----------------
         // Whatever they hold is multiplied by P = 0, and must be finite.  The copy of such a tile is announced here, and
         // the MMAs learn of it when the rows are zero.
         int slot = 1;                                               // of the unit's V: slots go K, V, K, V, ...
         uint32_t phases = 0;                                        // a bit per slot
         Unit u;
-        u.more = any_work;
+        u.more = any_work && !INT8;
         for (u.enter(p.c, sch, walk); u.more && ok; u.next(p.c, sch, walk)) {
             const int valid = walk.it.s.len - u.t * kTileKeys;
             if (valid < kTileKeys) {
@@ -438,14 +542,18 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             slot = (slot + 2) % Shape::kSlots;
         }
+    } else if (INT8 && warp >= kConvertWarp) {
+        // ---------------- int8 cache: K and V of each unit, converted on the way to shared memory ----------------
+        // 16 codes a thread and step; the next tile's codes travel while this one's are converted.
+        registers_to<INT8, false, kOtherRegs>();
+        if constexpr (INT8) convert_tiles<D, BF>(p, sch, walk, any_work, tid - 32 * kConvertWarp, ring, tail);
     } else {
+        registers_to<INT8, true, kSoftmaxRegs>();
         // ---------------- softmax: row tile x, one row per thread ----------------
         const int x = warp >> 2, quad = warp & 3;
         const int row = quad * 32 + lane;                          // of the row tile
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + 256 + x * D;
-        const float scale = fabsf(p.scale);
-        const uint32_t flip = p.scale < 0.0f ? 0x80000000u : 0u;   // a negative scale: maxima are of the negated logits
         uint32_t s_phase = 0;                                      // parity of the unit whose S is waited for
         for (bool more = any_work; more && ok; more = walk.next(p.c)) {
             const Item& it = walk.it;
@@ -455,91 +563,104 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const int t_end = tile_end(sch, it, x);
             int row_limit = sch.key_limit(it.s, it.i);
             if (p.causal && valid) row_limit = it.s.len - it.s.new_len + item_row / p.group + 1;
+            const float signed_scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
+            const float scale = fabsf(signed_scale);
+            const uint32_t flip = signed_scale < 0.0f ? 0x80000000u : 0u;    // maxima are then of the negated logits
             float m = -INFINITY;                                   // reference, in powers of two
             uint64_t sum2 = 0;                                     // two partial sums of P
-            for (int h = 2 * it.t0; h < 2 * t_end; ++h) {          // halves of units
-                const int part = h & 1;
-                // S(h) was asked for behind the second product of h - 2, which is therefore done as well: of the products
-                // only that of h - 1 can be outstanding, and a parity of its barrier is not mistaken for an older one
-                if (!wait(&tail->s_full[x][part], s_phase)) break;
-                if (part == 1) s_phase ^= 1u;
+            for (int t = it.t0; t < t_end; ++t) {
+                if (!wait(&tail->s_full[x], s_phase)) break;
+                s_phase ^= 1u;
                 ptx::tc_fence_after_sync();
+                const int seen = row_limit - t * kTileKeys;
+                const bool cut = __any_sync(0xFFFFFFFFu, seen < kTileKeys);
+                // The row is read twice: for its maximum, second half first, and for the exponentials, whose first half is
+                // still in registers.  128 logits and what is made of them do not fit a thread's registers.
                 uint32_t s[2][32];
-                ptx::tmem_ld_32x32(s_addr + part * kHalfKeys, s[0]);
-                ptx::tmem_ld_32x32(s_addr + part * kHalfKeys + 32, s[1]);
-                ptx::tmem_ld_wait();
-                if (flip != 0) {
+                auto fetch = [&](int part) {
+                    ptx::tmem_ld_32x32(s_addr + part * 64, s[0]);
+                    ptx::tmem_ld_32x32(s_addr + part * 64 + 32, s[1]);
+                    ptx::tmem_ld_wait();
+                    if (flip != 0) {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e) s[e >> 5][e & 31] ^= 0x80000000u;
-                }
-                const int seen = row_limit - h * kHalfKeys;
-                if (__any_sync(0xFFFFFFFFu, seen < kHalfKeys)) {
+                        for (int e = 0; e < 64; ++e) s[e >> 5][e & 31] ^= 0x80000000u;
+                    }
+                    if (cut) {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
-                        if (e >= seen) s[e >> 5][e & 31] = 0xFF800000u;      // -inf
-                }
-                float top[4];
+                        for (int e = 0; e < 64; ++e)
+                            if (part * 64 + e >= seen) s[e >> 5][e & 31] = 0xFF800000u;      // -inf
+                    }
+                };
+                auto most_of = [&]() {
+                    float top[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint32_t* w = s[c >> 1] + 16 * (c & 1);
-                    top[c] = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t* w = s[c >> 1] + 16 * (c & 1);
+                        top[c] = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 #pragma unroll
-                    for (int e = 2; e < 16; e += 2) top[c] = max3(top[c], __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
-                }
-                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+                        for (int e = 2; e < 16; e += 2) top[c] = max3(top[c], __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
+                    }
+                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                };
+                fetch(1);
+                float most = most_of();
+                fetch(0);
+                most = fmaxf(most, most_of()) * scale;
                 if (__any_sync(0xFFFFFFFFu, most > m + kRescaleAt)) {
                     const float m_new = fmaxf(m, most);
                     const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m - m_new);
                     m = m_new;
                     const float2 old = unpack2(sum2);
                     sum2 = pack2(old.x * f, old.y * f);
-                    if (h > 2 * it.t0) {
-                        if (!wait(&tail->o_full[x][part ^ 1], s_phase ^ 1u)) break;
-                        ptx::tc_fence_after_sync();
+                    if (t > it.t0) {          // S(t) was asked for behind the second product of t - 1, which is done as well
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 32) {
-                            uint32_t o[32];
-                            ptx::tmem_ld_32x32(o_addr + c, o);
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            ptx::tmem_ld_32x16(o_addr + c, o);
                             ptx::tmem_ld_wait();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            ptx::tmem_st_32x32(o_addr + c, o);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            ptx::tmem_st_32x16(o_addr + c, o);
                         }
                     }
                 }
                 const float ref = m == -INFINITY ? 0.0f : m;
                 const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-ref, -ref);
-                uint32_t pk[32];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float2 z = unpack2(fma2(pack2(__uint_as_float(s[e >> 4][2 * e & 31]), __uint_as_float(s[e >> 4][(2 * e & 31) + 1])),
-                                                  scale2, ref2));
-                    uint64_t pr;
-                    if (e % 8 < kPolyPairs) {
-                        pr = exp2_poly(z);
-                    } else {
-                        pr = pack2(exp2_approx(z.x), exp2_approx(z.y));
+                for (int part = 0; part < 2; ++part) {
+                    if (part == 1) fetch(1);
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float2 z = unpack2(fma2(pack2(__uint_as_float(s[e >> 4][2 * e & 31]), __uint_as_float(s[e >> 4][(2 * e & 31) + 1])),
+                                                      scale2, ref2));
+                        uint64_t pr;
+                        if (e % 8 < kPolyPairs) {
+                            pr = exp2_poly(z);
+                        } else {
+                            pr = pack2(exp2_approx(z.x), exp2_approx(z.y));
+                        }
+                        sum2 = add2(sum2, pr);
+                        const float2 both = unpack2(pr);
+                        pk[e] = narrow2<BF>(both.x, both.y);
                     }
-                    sum2 = add2(sum2, pr);
-                    const float2 both = unpack2(pr);
-                    pk[e] = narrow2<BF>(both.x, both.y);
+                    ptx::tmem_st_32x32(s_addr + part * 32, pk);
+                    ptx::tmem_st_wait();
+                    ptx::tc_fence_before_sync();
+                    ptx::mbar_arrive(&tail->p_full[x][part]);
                 }
-                ptx::tmem_st_32x32(s_addr + part * kHalfKeys, pk);
-                ptx::tmem_st_wait();
-                ptx::tc_fence_before_sync();
-                ptx::mbar_arrive(&tail->p_full[x][part]);
             }
             if (!ok) break;
             // ---- the item's rows
             const bool any = it.t0 < t_end;
             if (any) {
-                if (!wait(&tail->o_full[x][1], s_phase ^ 1u)) break;
+                if (!wait(&tail->o_full[x], s_phase ^ 1u)) break;
                 ptx::tc_fence_after_sync();
             }
             const float2 sums = unpack2(sum2);
             const float sum = m == -INFINITY ? 0.0f : sums.x + sums.y;   // no key: exp2_poly is not quite 0 at -inf
             const bool whole = it.t0 == 0 && it.t1 == it.units;
-            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const float inv = sum > 0.0f ? (INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f) / sum : 0.0f;
             const int tok = item_row / p.group;
             const int head = it.h * p.group + item_row - tok * p.group;
             const long long token = it.s.first + tok;
