@@ -72,13 +72,17 @@ namespace {
 // box of q (of a group of five heads 125 rows are used).
 constexpr int kTileKeys = 128;            // keys of a unit
 // Warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q; 11: V's tails.  With an int8 cache warps
-// 12-15 fetch and convert K and V, and 9 and 11 are idle.
+// 12-19 fetch and convert K and V, and 9 and 11 are idle.
+// readers of the item queue: the softmax warps, the MMA lane, and whoever fetches K and V
 template <bool INT8>
-constexpr int kTileThreads = INT8 ? 512 : 384;
+constexpr int kReaders = 8 + 1 + (INT8 ? 8 : 2);
+template <bool INT8>
+constexpr int kTileThreads = INT8 ? 640 : 384;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11, kConvertWarp = 12;
-// Registers of a thread.  384 threads get 168 each, enough for every role.  512 get 128 at launch, of which the four-warp
-// groups without a row of logits give some to the softmax: 144 + 144 + 112 + 112 = 4 x 128.
-constexpr int kSoftmaxRegs = 144, kOtherRegs = 112;
+constexpr int kConvertThreads = 256;
+// Registers of a thread.  384 threads get 168 each, enough for every role.  640 get 96 at launch, of which the four-warp
+// groups without a row of logits give some to the softmax: 2 x 128 + 64 + 2 x 80 = 5 x 96.
+constexpr int kSoftmaxRegs = 128, kOtherRegs = 64, kConvertRegs = 80;
 
 template <int D>
 struct TileShape {
@@ -88,12 +92,28 @@ struct TileShape {
     static constexpr int kQBytes = 128 * D * 2;                // of one row tile
 };
 
+// An item as its readers need it.
+struct TileItem {
+    int valid;                // 0: the block's work ends here
+    int b, h, len;            // sequence, KV head, keys
+    int before;               // keys before the first new token
+    int first_token;          // of the sequence, in q
+    int first_row, rows;      // of the item, and of its sequence: (token, head) pairs
+    int limit;                // keys that its last row sees
+    int t0, end[2];           // units of this block: from, and to for either row tile
+    int whole;                // the block has all units of the item
+    int last;                 // the block that has its last unit
+};
+constexpr int kItems = 4;     // items in the queue
+
 struct TileTail {
+    TileItem items[kItems];
+    uint64_t item_full[kItems], item_empty[kItems];
     uint64_t kv_full[8], kv_empty[8], raw_full[8];   // raw_full: a V tile whose last rows are still to be cleared
     uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2], p_full[2][2], o_full[2];            // p_full: either half of the unit's keys
     uint64_t drain;
-    long long scratch[16];
+    long long scratch[20];
     Start found;
     uint32_t tmem_base;
     volatile int abort_flag;
@@ -132,23 +152,26 @@ __device__ __forceinline__ int tile_end(const TileSchedule& sch, const Item& it,
     return min(it.t1, (lim + kTileKeys - 1) / kTileKeys);
 }
 
-// The units of a block in order, for the roles that work on both row tiles; items without keys are passed over.
-struct Unit {
-    int t, t0, end[2], t_end;
-    bool more;
-    __device__ __forceinline__ void enter(const PagedParams& p, const TileSchedule& sch, TileWalk& walk) {
-        for (; more; more = walk.next(p)) {
-            end[0] = tile_end(sch, walk.it, 0);
-            end[1] = tile_end(sch, walk.it, 1);
-            t_end = max(end[0], end[1]);
-            t = t0 = walk.it.t0;
-            if (t < t_end) return;
-        }
+// A role's place in the queue of items that one warp walks for all; a whole warp, or one lane, holds a reader.
+struct ItemReader {
+    TileTail* tail;
+    const AttendParams& p;
+    int n;
+    bool ok, more;
+    // waits for item n; `more` says whether there is one
+    template <bool WARP>
+    __device__ __forceinline__ void fetch() {
+        ok = tile_wait(&tail->item_full[n & (kItems - 1)], n / kItems & 1u, tail, p);
+        if (WARP) ok = __all_sync(0xFFFFFFFFu, ok);
+        more = ok && tail->items[n & (kItems - 1)].valid != 0;
     }
-    __device__ __forceinline__ void next(const PagedParams& p, const TileSchedule& sch, TileWalk& walk) {
-        if (++t < t_end) return;
-        more = walk.next(p);
-        enter(p, sch, walk);
+    __device__ __forceinline__ const TileItem& item() const { return tail->items[n & (kItems - 1)]; }
+    // done with item n; one thread per reader arrives
+    template <bool WARP>
+    __device__ __forceinline__ void leave(bool arrives) {
+        if (WARP) __syncwarp();
+        if (arrives) ptx::mbar_arrive(&tail->item_empty[n & (kItems - 1)]);
+        ++n;
     }
 };
 
@@ -203,83 +226,90 @@ __device__ __forceinline__ uint64_t exp2_poly(float2 x) {
                  __uint_as_float(__float_as_uint(v.y) + (__float_as_uint(n.y) << 23)));
 }
 
-// The warps that fill the ring from an int8 cache (128 threads, `me` of them): K and V of each unit in turn, in the layout
+// The warps that fill the ring from an int8 cache (`me` of kConvertThreads): K and V of each unit in turn, in the layout
 // that the 16-bit copies leave: keys along the rows, 128-byte swizzle.  Keys behind the sequence's last are zeros.
 template <int D, bool BF>
-__device__ __forceinline__ void convert_tiles(const AttendParams& p, const TileSchedule& sch, TileWalk& walk, bool any_work, int me,
-                                              uint8_t* ring, TileTail* tail) {
+__device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uint8_t* ring, TileTail* tail) {
     using Shape = TileShape<D>;
-    constexpr int kWords = D / 16;                 // 16-byte words of a key's codes; as many steps make a tile
-    constexpr int kKeys = 128 / kWords;            // keys of a step
-    const int word = me % kWords, first = me / kWords;
+    constexpr int kWords = D / 16;                 // 16-byte words of a key's codes
+    constexpr int kKeys = kConvertThreads / kWords;        // keys of a step
+    constexpr int kSteps = kTileKeys / kKeys;
+    const int word = me % kWords, first = me / kWords, lane = me & 31;
     const int page_mask = (1 << p.c.page_shift) - 1;
     // the word's two chunks of 8 elements; half a row's lanes store the second first, which spreads them over the banks
     uint8_t* const column = ring + (word >> 2) * kTileKeys * 128;
     const int chunk = 2 * (word & 3), turn = word >> 2 & 1;
-    Unit u;
-    u.more = any_work;
-    u.enter(p.c, sch, walk);
-    int pages[kWords];                             // of this thread's keys of the unit, -1: no key
-    auto look_up = [&] {
-        const int* table = p.c.page_table + walk.it.b * p.c.table_stride;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            const int key = u.t * kTileKeys + i * kKeys + first;
-            pages[i] = key < walk.it.s.len ? __ldg(table + (key >> p.c.page_shift)) : -1;
-            if (key < walk.it.s.len && (pages[i] < 0 || pages[i] >= p.c.num_pages)) {
-                atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
-                pages[i] = -1;
-            }
-        }
+    ItemReader items{tail, p, 0, true, false};
+    bool ok = true, more;
+    int t = 0, t_end = 0, len = 0, h = 0;
+    const int* table = nullptr;
+    auto next = [&] {                              // the next unit
+        if (++t < t_end) return;
+        do {
+            items.template fetch<true>();
+            ok = ok && items.ok;
+            more = items.more;
+            if (!more) return;
+            const TileItem& it = items.item();
+            t = it.t0;
+            t_end = max(it.end[0], it.end[1]);
+            len = it.len;
+            h = it.h;
+            table = p.c.page_table + it.b * p.c.table_stride;
+            items.template leave<true>(lane == 0);
+        } while (t >= t_end);
     };
-    auto load = [&](const void* base, uint4 (&v)[kWords]) {
-        const char* head = static_cast<const char*>(base) + walk.it.h * p.c.head_stride + word * 16;
+    // a lane looks up the page of 16 keys of the unit; the others ask it
+    auto look_up = [&] {
+        const int key = t * kTileKeys + 16 * (lane & 7);
+        return more && key < len ? __ldg(table + (key >> p.c.page_shift)) : -1;
+    };
+    auto load = [&](const void* base, int entry, uint4 (&v)[kSteps]) {
+        const char* head = static_cast<const char*>(base) + h * p.c.head_stride + word * 16;
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            const int row = (u.t * kTileKeys + i * kKeys + first) & page_mask;
-            v[i] = pages[i] >= 0 ? ldg_stream16(head + pages[i] * p.c.page_stride + row * p.c.token_stride) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kSteps; ++i) {
+            const int key = t * kTileKeys + i * kKeys + first;
+            const int page = __shfl_sync(0xFFFFFFFFu, entry, (i * kKeys + first) >> 4);
+            const bool in = key < len && page >= 0 && page < p.c.num_pages;
+            v[i] = in ? ldg_stream16(head + page * p.c.page_stride + (key & page_mask) * p.c.token_stride) : make_uint4(0, 0, 0, 0);
         }
     };
     int slot = 0;
     uint32_t phase = 0;
-    bool ok = true;
-    auto store = [&](const uint4 (&v)[kWords]) {
+    auto store = [&](const uint4 (&v)[kSteps]) {
         ok = ok && tile_wait(&tail->kv_empty[slot], phase ^ 1u, tail, p);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) return;
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) {
+        for (int i = 0; i < kSteps; ++i) {
             const int r = i * kKeys + first;
             uint8_t* row = column + (size_t)slot * Shape::kSlotBytes + r * 128;
-            const uint32_t lo[4] = {codes_to_pair<BF, 0>(v[i].x), codes_to_pair<BF, 1>(v[i].x), codes_to_pair<BF, 0>(v[i].y),
-                                    codes_to_pair<BF, 1>(v[i].y)};
-            const uint32_t hi[4] = {codes_to_pair<BF, 0>(v[i].z), codes_to_pair<BF, 1>(v[i].z), codes_to_pair<BF, 0>(v[i].w),
-                                    codes_to_pair<BF, 1>(v[i].w)};
-            uint4 a = make_uint4(lo[0], lo[1], lo[2], lo[3]), b = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            if (turn) {
-                const uint4 c = a;
-                a = b;
-                b = c;
-            }
-            *reinterpret_cast<uint4*>(row + (((chunk + turn) ^ (r & 7)) << 4)) = a;
-            *reinterpret_cast<uint4*>(row + (((chunk + (turn ^ 1)) ^ (r & 7)) << 4)) = b;
+            const uint4 lo = make_uint4(codes_to_pair<BF, 0>(v[i].x), codes_to_pair<BF, 1>(v[i].x), codes_to_pair<BF, 0>(v[i].y),
+                                        codes_to_pair<BF, 1>(v[i].y));
+            const uint4 hi = make_uint4(codes_to_pair<BF, 0>(v[i].z), codes_to_pair<BF, 1>(v[i].z), codes_to_pair<BF, 0>(v[i].w),
+                                        codes_to_pair<BF, 1>(v[i].w));
+            *reinterpret_cast<uint4*>(row + (((chunk + turn) ^ (r & 7)) << 4)) = turn ? hi : lo;
+            *reinterpret_cast<uint4*>(row + (((chunk + (turn ^ 1)) ^ (r & 7)) << 4)) = turn ? lo : hi;
         }
         ptx::fence_proxy_async_smem();
         ptx::mbar_arrive(&tail->kv_full[slot]);
         if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; }
     };
-    uint4 k[kWords], v[kWords];
-    if (u.more) {
-        look_up();
-        load(p.c.k, k);
-    }
-    while (u.more && ok) {
-        load(p.c.v, v);
-        u.next(p.c, sch, walk);
-        if (u.more) look_up();
+    // The next unit's keys travel while this one's values are converted, its values while its keys are; its page
+    // entries come half a unit earlier.
+    uint4 k[kSteps], v[kSteps];
+    next();
+    int entry = look_up();
+    if (more) load(p.c.k, entry, k);
+    while (more && ok) {
+        if (t * kTileKeys + 16 * (lane & 7) < len && (entry < 0 || entry >= p.c.num_pages))
+            atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
+        load(p.c.v, entry, v);
+        next();
+        entry = look_up();
         store(k);
-        if (u.more) load(p.c.k, k);
-        store(v);
+        if (more) load(p.c.k, entry, k);
+        if (ok) store(v);
     }
 }
 
@@ -312,7 +342,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
     if (tid == 0) {
         for (int s = 0; s < Shape::kSlots; ++s) {
-            ptx::mbar_init(&tail->kv_full[s], INT8 ? 128 : 1);
+            ptx::mbar_init(&tail->kv_full[s], INT8 ? kConvertThreads : 1);
             ptx::mbar_init(&tail->kv_empty[s], 1);
             ptx::mbar_init(&tail->raw_full[s], 1);
         }
@@ -325,6 +355,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             ptx::mbar_init(&tail->o_full[x], 1);
         }
         ptx::mbar_init(&tail->drain, 1);
+        for (int i = 0; i < kItems; ++i) {
+            ptx::mbar_init(&tail->item_full[i], 1);
+            ptx::mbar_init(&tail->item_empty[i], kReaders<INT8>);
+        }
         tail->abort_flag = 0;
         ptx::mbar_init_fence();
         ptx::prefetch_tensormap(&map_q);
@@ -347,8 +381,6 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const TileSchedule sch{p.item_rows, p.group, p.causal, p.c.kv_heads};
     const Start st = find_start<kTileThreads<INT8>, kTileKeys>(p.c, sch, p.max_blocks, p.min_units, tail->scratch, &tail->found);
     if (tid == 0) p.part_items[blockIdx.x].last = -1;
-    TileWalk walk;
-    const bool any_work = walk.begin(p.c, sch, st, p.split != 0);
     bool ok = true;
     // whole warps wait together: a role goes on, or gives up, as a warp
     auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -365,32 +397,38 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int box = min(1 << p.c.page_shift, kTileKeys);
         const int boxes = kTileKeys / box;
         const int page_mask = (1 << p.c.page_shift) - 1;
-        Unit u;
-        u.more = any_work && !INT8;
-        for (u.enter(p.c, sch, walk); u.more && ok; u.next(p.c, sch, walk)) {
-            const int key = u.t * kTileKeys + lane * box;
-            int page = (int)p.c.num_pages;                      // outside the cache: the copy fills in zeros
-            if (lane < boxes && key < walk.it.s.len) {
-                const int entry = __ldg(p.c.page_table + walk.it.b * p.c.table_stride + (key >> p.c.page_shift));
-                if (entry < 0 || entry >= p.c.num_pages) atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
-                else page = entry;
-            }
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-                if (!wait(&tail->kv_empty[slot], phase ^ 1u)) break;
-                // a V tile that ends behind the sequence's last key goes to the warp that clears its tail first
-                uint64_t* full = kv == 1 && walk.it.s.len - u.t * kTileKeys < kTileKeys ? &tail->raw_full[slot] : &tail->kv_full[slot];
-                if (lane == 0) ptx::mbar_arrive_expect_tx(full, Shape::kSlotBytes);
-                __syncwarp();
-                if (lane < boxes) {
-                    const uint32_t dst = ptx::smem_u32(ring) + slot * Shape::kSlotBytes + lane * box * 128;
-#pragma unroll
-                    for (int half = 0; half < Shape::kHalves; ++half)
-                        ptx::tma_load_4d(dst + half * kTileKeys * 128, kv == 0 ? &map_k : &map_v, full, half * 64,
-                                         key & page_mask, walk.it.h, page);
+        ItemReader items{tail, p, 0, true, false};
+        for (; !INT8 && ok; items.template leave<true>(lane == 0)) {
+            items.template fetch<true>();
+            ok = items.ok;
+            if (!items.more) break;
+            const TileItem it = items.item();
+            const int t_end = max(it.end[0], it.end[1]);
+            for (int t = it.t0; t < t_end && ok; ++t) {
+                const int key = t * kTileKeys + lane * box;
+                int page = (int)p.c.num_pages;                  // outside the cache: the copy fills in zeros
+                if (lane < boxes && key < it.len) {
+                    const int entry = __ldg(p.c.page_table + it.b * p.c.table_stride + (key >> p.c.page_shift));
+                    if (entry < 0 || entry >= p.c.num_pages) atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
+                    else page = entry;
                 }
-                __syncwarp();
-                if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; }
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    if (!wait(&tail->kv_empty[slot], phase ^ 1u)) break;
+                    // a V tile that ends behind the sequence's last key goes to the warp that clears its tail first
+                    uint64_t* full = kv == 1 && it.len - t * kTileKeys < kTileKeys ? &tail->raw_full[slot] : &tail->kv_full[slot];
+                    if (lane == 0) ptx::mbar_arrive_expect_tx(full, Shape::kSlotBytes);
+                    __syncwarp();
+                    if (lane < boxes) {
+                        const uint32_t dst = ptx::smem_u32(ring) + slot * Shape::kSlotBytes + lane * box * 128;
+#pragma unroll
+                        for (int half = 0; half < Shape::kHalves; ++half)
+                            ptx::tma_load_4d(dst + half * kTileKeys * 128, kv == 0 ? &map_k : &map_v, full, half * 64, key & page_mask, it.h,
+                                             page);
+                    }
+                    __syncwarp();
+                    if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; }
+                }
             }
         }
         // gave up: copies still in flight must land before the block's shared memory goes away
@@ -406,13 +444,41 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         __syncwarp();
     } else if (warp == kQueryWarp) {
         registers_to<INT8, false, kOtherRegs>();
-        // ---------------- Q of each item ----------------
+        // ---------------- the block's items, for everyone, and their Q ----------------
         uint32_t filled[2] = {0, 0};                            // times that each row tile's queries were asked for
         const int tokens = 128 / p.group;
-        for (bool more = any_work; more && ok; more = walk.next(p.c)) {
+        TileWalk walk;
+        int n = 0;
+        for (bool more = walk.begin(p.c, sch, st, p.split != 0);; more = walk.next(p.c), ++n) {
+            const int at = n & (kItems - 1);
+            if (!wait(&tail->item_empty[at], (n / kItems & 1u) ^ 1u)) break;
+            const Item& w = walk.it;
+            TileItem it;
+            it.valid = more;
+            if (more) {
+                it.b = w.b;
+                it.h = w.h;
+                it.len = w.s.len;
+                it.before = w.s.len - w.s.new_len;
+                it.first_token = w.s.first;
+                it.first_row = w.i * sch.rows;
+                it.rows = w.s.new_len * p.group;
+                it.limit = sch.key_limit(w.s, w.i);
+                it.t0 = w.t0;
+                it.end[0] = tile_end(sch, w, 0);
+                it.end[1] = tile_end(sch, w, 1);
+                it.whole = w.t0 == 0 && w.t1 == w.units;
+                it.last = block_of(st.total, w.first_unit + w.units - 1, st.blocks);
+            }
+            if (lane == 0) {
+                tail->items[at] = it;
+                ptx::mbar_arrive(&tail->item_full[at]);
+            }
+            __syncwarp();
+            if (!more) break;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (!ok || tile_end(sch, walk.it, x) <= walk.it.t0) continue;
+                if (!ok || it.end[x] <= it.t0) continue;
                 if (!wait(&tail->q_empty[x], (filled[x] & 1u) ^ 1u)) continue;
                 ++filled[x];
                 if (lane == 0) {
@@ -420,10 +486,11 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                     for (int half = 0; half < Shape::kHalves; ++half)
                         ptx::tma_load_3d(ptx::smem_u32(q_smem) + x * Shape::kQBytes + half * 128 * 128, &map_q, &tail->q_full[x], half * 64,
-                                         walk.it.h * p.group, walk.it.s.first + (2 * walk.it.i + x) * tokens);
+                                         it.h * p.group, it.first_token + it.first_row / p.group + x * tokens);
                 }
                 __syncwarp();
             }
+            if (!ok) break;
         }
         if (!ok && lane == 0) {
             for (int x = 0; x < 2; ++x) {
@@ -445,6 +512,26 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const uint64_t q_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(q_smem));
             const uint64_t k_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(ring));
             const uint64_t v_desc = ptx::smem_desc_mn_major_sw128(ptx::smem_u32(ring), kTileKeys * 128);
+            // The units in order; items without keys are passed over.
+            struct Unit {
+                int t, t0, end[2], t_end;
+                bool more;
+            };
+            ItemReader items{tail, p, 0, true, false};
+            auto enter = [&](Unit& u) {
+                for (;;) {
+                    items.template fetch<false>();
+                    ok = ok && items.ok;
+                    u.more = items.more;
+                    if (!u.more) return;
+                    u.t = u.t0 = items.item().t0;
+                    u.end[0] = items.item().end[0];
+                    u.end[1] = items.item().end[1];
+                    u.t_end = max(u.end[0], u.end[1]);
+                    items.template leave<false>(true);
+                    if (u.t < u.t_end) return;
+                }
+            };
             // S of row tile x for unit u, whose keys are in k_slot
             auto qk = [&](const Unit& u, int x, int k_slot) {
                 if (u.t == u.t0) {
@@ -464,8 +551,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (u.t + 1 == u.end[x]) ptx::mma_commit(&tail->q_empty[x]);
             };
             Unit u;
-            u.more = any_work;
-            u.enter(p.c, sch, walk);
+            enter(u);
             if (u.more) {
                 ok = tile_wait(&tail->kv_full[slot], phase, tail, p);
                 ptx::tc_fence_after_sync();
@@ -481,7 +567,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ok = tile_wait(&tail->kv_full[v_slot], phase, tail, p);
                 advance();
                 const int k_slot = slot;
-                u.next(p.c, sch, walk);
+                if (++u.t == u.t_end) enter(u);
                 if (u.more && ok) {
                     ok = tile_wait(&tail->kv_full[k_slot], phase, tail, p);
                     advance();
@@ -524,51 +610,62 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // the MMAs learn of it when the rows are zero.
         int slot = 1;                                               // of the unit's V: slots go K, V, K, V, ...
         uint32_t phases = 0;                                        // a bit per slot
-        Unit u;
-        u.more = any_work && !INT8;
-        for (u.enter(p.c, sch, walk); u.more && ok; u.next(p.c, sch, walk)) {
-            const int valid = walk.it.s.len - u.t * kTileKeys;
-            if (valid < kTileKeys) {
-                if (!wait(&tail->raw_full[slot], phases >> slot & 1u)) break;
-                phases ^= 1u << slot;
-                uint8_t* v = ring + (size_t)slot * Shape::kSlotBytes + valid * 128;
-                for (int y = lane; y < (kTileKeys - valid) * 8; y += 32)
+        ItemReader items{tail, p, 0, true, false};
+        for (; !INT8 && ok; items.template leave<true>(lane == 0)) {
+            items.template fetch<true>();
+            ok = items.ok;
+            if (!items.more) break;
+            const TileItem it = items.item();
+            const int t_end = max(it.end[0], it.end[1]);
+            for (int t = it.t0; t < t_end; ++t) {
+                const int valid = it.len - t * kTileKeys;
+                if (valid < kTileKeys) {
+                    if (!wait(&tail->raw_full[slot], phases >> slot & 1u)) break;
+                    phases ^= 1u << slot;
+                    uint8_t* v = ring + (size_t)slot * Shape::kSlotBytes + valid * 128;
+                    for (int y = lane; y < (kTileKeys - valid) * 8; y += 32)
 #pragma unroll
-                    for (int half = 0; half < Shape::kHalves; ++half)
-                        *reinterpret_cast<uint4*>(v + half * kTileKeys * 128 + y * 16) = make_uint4(0, 0, 0, 0);
-                ptx::fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&tail->kv_full[slot]);
+                        for (int half = 0; half < Shape::kHalves; ++half)
+                            *reinterpret_cast<uint4*>(v + half * kTileKeys * 128 + y * 16) = make_uint4(0, 0, 0, 0);
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&tail->kv_full[slot]);
+                }
+                slot = (slot + 2) % Shape::kSlots;
             }
-            slot = (slot + 2) % Shape::kSlots;
         }
     } else if (INT8 && warp >= kConvertWarp) {
         // ---------------- int8 cache: K and V of each unit, converted on the way to shared memory ----------------
         // 16 codes a thread and step; the next tile's codes travel while this one's are converted.
-        registers_to<INT8, false, kOtherRegs>();
-        if constexpr (INT8) convert_tiles<D, BF>(p, sch, walk, any_work, tid - 32 * kConvertWarp, ring, tail);
+        registers_to<INT8, false, kConvertRegs>();
+        if constexpr (INT8) convert_tiles<D, BF>(p, tid - 32 * kConvertWarp, ring, tail);
     } else {
         registers_to<INT8, true, kSoftmaxRegs>();
         // ---------------- softmax: row tile x, one row per thread ----------------
         const int x = warp >> 2, quad = warp & 3;
+        const int half = sch.rows >> 1;
         const int row = quad * 32 + lane;                          // of the row tile
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + 256 + x * D;
         uint32_t s_phase = 0;                                      // parity of the unit whose S is waited for
-        for (bool more = any_work; more && ok; more = walk.next(p.c)) {
-            const Item& it = walk.it;
-            const int half = sch.rows >> 1;
-            const int item_row = it.i * sch.rows + x * half + row; // among the sequence's rows
-            const bool valid = row < half && item_row < it.s.new_len * p.group;
-            const int t_end = tile_end(sch, it, x);
-            int row_limit = sch.key_limit(it.s, it.i);
-            if (p.causal && valid) row_limit = it.s.len - it.s.new_len + item_row / p.group + 1;
+        ItemReader items{tail, p, 0, true, false};
+        for (; ok; items.template leave<true>(lane == 0)) {
+            items.template fetch<true>();
+            ok = items.ok;
+            if (!items.more) break;
+            const TileItem& it = items.item();
+            const int t0 = it.t0, t_end = it.end[x];
+            const bool any = t0 < t_end;                           // this row tile sees keys of this block's units
+            const int item_row = it.first_row + x * half + row;    // among the sequence's rows
+            const bool valid = row < half && item_row < it.rows;
+            int row_limit = it.limit;
+            if (p.causal && valid) row_limit = it.before + item_row / p.group + 1;
             const float signed_scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
             const float scale = fabsf(signed_scale);
             const uint32_t flip = signed_scale < 0.0f ? 0x80000000u : 0u;    // maxima are then of the negated logits
             float m = -INFINITY;                                   // reference, in powers of two
             uint64_t sum2 = 0;                                     // two partial sums of P
-            for (int t = it.t0; t < t_end; ++t) {
+            for (int t = t0; t < t_end; ++t) {
                 if (!wait(&tail->s_full[x], s_phase)) break;
                 s_phase ^= 1u;
                 ptx::tc_fence_after_sync();
@@ -612,7 +709,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     m = m_new;
                     const float2 old = unpack2(sum2);
                     sum2 = pack2(old.x * f, old.y * f);
-                    if (t > it.t0) {          // S(t) was asked for behind the second product of t - 1, which is done as well
+                    if (t > t0) {          // S(t) was asked for behind the second product of t - 1, which is done as well
 #pragma unroll 1
                         for (int c = 0; c < D; c += 16) {
                             uint32_t o[16];
@@ -652,19 +749,18 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             if (!ok) break;
             // ---- the item's rows
-            const bool any = it.t0 < t_end;
             if (any) {
                 if (!wait(&tail->o_full[x], s_phase ^ 1u)) break;
                 ptx::tc_fence_after_sync();
             }
             const float2 sums = unpack2(sum2);
             const float sum = m == -INFINITY ? 0.0f : sums.x + sums.y;   // no key: exp2_poly is not quite 0 at -inf
-            const bool whole = it.t0 == 0 && it.t1 == it.units;
+            const bool whole = it.whole;
             const float inv = sum > 0.0f ? (INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f) / sum : 0.0f;
             const int tok = item_row / p.group;
             const int head = it.h * p.group + item_row - tok * p.group;
-            const long long token = it.s.first + tok;
-            const long long part_row = (long long)(2 * blockIdx.x + (it.t0 == 0 ? 1 : 0)) * 256 + x * 128 + row;
+            const long long token = it.first_token + tok;
+            const long long part_row = (long long)(2 * blockIdx.x + (t0 == 0 ? 1 : 0)) * 256 + x * 128 + row;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 uint32_t o[32];
@@ -694,13 +790,13 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (valid && whole && p.lse != nullptr)
                 p.lse[token * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             if (valid && !whole) p.part_ml[part_row] = make_float2(m, sum);
-            if (!whole && it.t0 == 0 && tid == 0) {
+            if (!whole && t0 == 0 && tid == 0) {
                 PartItem pi;
-                pi.last = block_of(st.total, it.first_unit + it.units - 1, st.blocks);
+                pi.last = it.last;
                 pi.h = it.h;
-                pi.first_row = it.i * sch.rows;
-                pi.rows = min(sch.rows, it.s.new_len * p.group - it.i * sch.rows);
-                pi.first_token = it.s.first;
+                pi.first_row = it.first_row;
+                pi.rows = min(sch.rows, it.rows - it.first_row);
+                pi.first_token = it.first_token;
                 pi.tile_rows = half;
                 p.part_items[blockIdx.x] = pi;
             }
