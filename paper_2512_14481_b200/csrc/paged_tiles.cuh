@@ -100,11 +100,19 @@ struct TileItem {
     int first_token;          // of the sequence, in q
     int first_row, rows;      // of the item, and of its sequence: (token, head) pairs
     int limit;                // keys that its last row sees
-    int t0, end[2];           // units of this block: from, and to for either row tile
+    int t0, tiles;            // units of this block: the first, and how many
+    int fold;                 // 0, or: the item has rows for one row tile only, and both work on them, the first on
+                              // units t0 ... t0 + fold - 1 and the second on the others
+    int begin[2], end[2];     // units of either row tile
     int whole;                // the block has all units of the item
     int last;                 // the block that has its last unit
 };
 constexpr int kItems = 4;     // items in the queue
+
+// Unit i of an item in the order in which K and V are fetched.
+__device__ __forceinline__ int unit_of(const TileItem& it, int i) {
+    return it.fold == 0 ? it.t0 + i : it.t0 + (i >> 1) + (i & 1) * it.fold;
+}
 
 struct TileTail {
     TileItem items[kItems];
@@ -112,7 +120,8 @@ struct TileTail {
     uint64_t kv_full[8], kv_empty[8], raw_full[8];   // raw_full: a V tile whose last rows are still to be cleared
     uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2], p_full[2][2], o_full[2];            // p_full: either half of the unit's keys
-    uint64_t drain;
+    uint64_t drain, meet[4];
+    float2 other[128];        // reference and sum of the second row tile's rows, for the first
     long long scratch[20];
     Start found;
     uint32_t tmem_base;
@@ -121,6 +130,7 @@ struct TileTail {
 
 template <int D>
 constexpr size_t kTileSmem = 1024 + 2 * (size_t)TileShape<D>::kQBytes + (size_t)TileShape<D>::kSlots * TileShape<D>::kSlotBytes + sizeof(TileTail);
+static_assert(kTileSmem<128> <= 227 * 1024 && kTileSmem<64> <= 227 * 1024, "a block's shared memory");
 
 // Bounded wait of one thread: false if the phase did not complete in time or another role gave up.
 __device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, TileTail* tail, const AttendParams& p) {
@@ -241,36 +251,37 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
     const int chunk = 2 * (word & 3), turn = word >> 2 & 1;
     ItemReader items{tail, p, 0, true, false};
     bool ok = true, more;
-    int t = 0, t_end = 0, len = 0, h = 0;
+    TileItem it{};
+    int i = 0, t = 0;
     const int* table = nullptr;
     auto next = [&] {                              // the next unit
-        if (++t < t_end) return;
-        do {
+        for (++i; i >= it.tiles; i = 0) {
             items.template fetch<true>();
             ok = ok && items.ok;
             more = items.more;
             if (!more) return;
-            const TileItem& it = items.item();
-            t = it.t0;
-            t_end = max(it.end[0], it.end[1]);
-            len = it.len;
-            h = it.h;
+            it = items.item();
             table = p.c.page_table + it.b * p.c.table_stride;
             items.template leave<true>(lane == 0);
-        } while (t >= t_end);
+            if (it.tiles > 0) {
+                i = 0;
+                break;
+            }
+        }
+        t = unit_of(it, i);
     };
     // a lane looks up the page of 16 keys of the unit; the others ask it
     auto look_up = [&] {
         const int key = t * kTileKeys + 16 * (lane & 7);
-        return more && key < len ? __ldg(table + (key >> p.c.page_shift)) : -1;
+        return more && key < it.len ? __ldg(table + (key >> p.c.page_shift)) : -1;
     };
     auto load = [&](const void* base, int entry, uint4 (&v)[kSteps]) {
-        const char* head = static_cast<const char*>(base) + h * p.c.head_stride + word * 16;
+        const char* head = static_cast<const char*>(base) + it.h * p.c.head_stride + word * 16;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int key = t * kTileKeys + i * kKeys + first;
             const int page = __shfl_sync(0xFFFFFFFFu, entry, (i * kKeys + first) >> 4);
-            const bool in = key < len && page >= 0 && page < p.c.num_pages;
+            const bool in = key < it.len && page >= 0 && page < p.c.num_pages;
             v[i] = in ? ldg_stream16(head + page * p.c.page_stride + (key & page_mask) * p.c.token_stride) : make_uint4(0, 0, 0, 0);
         }
     };
@@ -302,7 +313,7 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
     int entry = look_up();
     if (more) load(p.c.k, entry, k);
     while (more && ok) {
-        if (t * kTileKeys + 16 * (lane & 7) < len && (entry < 0 || entry >= p.c.num_pages))
+        if (t * kTileKeys + 16 * (lane & 7) < it.len && (entry < 0 || entry >= p.c.num_pages))
             atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
         load(p.c.v, entry, v);
         next();
@@ -355,6 +366,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             ptx::mbar_init(&tail->o_full[x], 1);
         }
         ptx::mbar_init(&tail->drain, 1);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&tail->meet[i], 64);
         for (int i = 0; i < kItems; ++i) {
             ptx::mbar_init(&tail->item_full[i], 1);
             ptx::mbar_init(&tail->item_empty[i], kReaders<INT8>);
@@ -403,8 +415,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             ok = items.ok;
             if (!items.more) break;
             const TileItem it = items.item();
-            const int t_end = max(it.end[0], it.end[1]);
-            for (int t = it.t0; t < t_end && ok; ++t) {
+            for (int i = 0; i < it.tiles && ok; ++i) {
+                const int t = unit_of(it, i);
                 const int key = t * kTileKeys + lane * box;
                 int page = (int)p.c.num_pages;                  // outside the cache: the copy fills in zeros
                 if (lane < boxes && key < it.len) {
@@ -465,8 +477,16 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 it.rows = w.s.new_len * p.group;
                 it.limit = sch.key_limit(w.s, w.i);
                 it.t0 = w.t0;
-                it.end[0] = tile_end(sch, w, 0);
-                it.end[1] = tile_end(sch, w, 1);
+                it.begin[0] = it.begin[1] = w.t0;
+                it.end[0] = max(w.t0, tile_end(sch, w, 0));
+                it.end[1] = max(w.t0, tile_end(sch, w, 1));
+                it.tiles = max(it.end[0], it.end[1]) - w.t0;
+                it.fold = it.first_row + (sch.rows >> 1) >= it.rows && it.tiles > 1 ? (it.tiles + 1) >> 1 : 0;
+                if (it.fold != 0) {
+                    it.begin[1] = w.t0 + it.fold;
+                    it.end[1] = it.end[0];
+                    it.end[0] = it.begin[1];
+                }
                 it.whole = w.t0 == 0 && w.t1 == w.units;
                 it.last = block_of(st.total, w.first_unit + w.units - 1, st.blocks);
             }
@@ -478,7 +498,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (!more) break;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (!ok || it.end[x] <= it.t0) continue;
+                if (!ok || it.end[x] == it.begin[x]) continue;
                 if (!wait(&tail->q_empty[x], (filled[x] & 1u) ^ 1u)) continue;
                 ++filled[x];
                 if (lane == 0) {
@@ -486,7 +506,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                     for (int half = 0; half < Shape::kHalves; ++half)
                         ptx::tma_load_3d(ptx::smem_u32(q_smem) + x * Shape::kQBytes + half * 128 * 128, &map_q, &tail->q_full[x], half * 64,
-                                         it.h * p.group, it.first_token + it.first_row / p.group + x * tokens);
+                                         it.h * p.group, it.first_token + it.first_row / p.group + (it.fold != 0 ? 0 : x * tokens));
                 }
                 __syncwarp();
             }
@@ -506,77 +526,79 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, BF);
             constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF) | ptx::kIdescBTransposed;
-            int slot = 0;
-            uint32_t phase = 0, q_phase = 0, p_phase = 0;             // q_phase, p_phase: a bit per row tile
-            auto advance = [&] { if (++slot == Shape::kSlots) { slot = 0; phase ^= 1u; } };
+            uint32_t q_phase = 0, p_phase = 0;                        // a bit per row tile
             const uint64_t q_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(q_smem));
             const uint64_t k_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(ring));
             const uint64_t v_desc = ptx::smem_desc_mn_major_sw128(ptx::smem_u32(ring), kTileKeys * 128);
-            // The units in order; items without keys are passed over.
-            struct Unit {
-                int t, t0, end[2], t_end;
+            // Steps: a unit for both row tiles, or (fold) a unit for each.  K and V tiles pass through the ring in the order
+            // of the units, K before V; `at` is the step's first tile among all of the block's.
+            struct Step {
+                int j, n[2], steps, fold;
+                uint32_t at;
                 bool more;
             };
             ItemReader items{tail, p, 0, true, false};
-            auto enter = [&](Unit& u) {
+            auto enter = [&](Step& u) {
                 for (;;) {
                     items.template fetch<false>();
                     ok = ok && items.ok;
                     u.more = items.more;
                     if (!u.more) return;
-                    u.t = u.t0 = items.item().t0;
-                    u.end[0] = items.item().end[0];
-                    u.end[1] = items.item().end[1];
-                    u.t_end = max(u.end[0], u.end[1]);
+                    const TileItem& it = items.item();
+                    u.j = 0;
+                    u.n[0] = it.end[0] - it.begin[0];
+                    u.n[1] = it.end[1] - it.begin[1];
+                    u.steps = max(u.n[0], u.n[1]);
+                    u.fold = it.fold != 0;
                     items.template leave<false>(true);
-                    if (u.t < u.t_end) return;
+                    if (u.steps > 0) return;
                 }
             };
-            // S of row tile x for unit u, whose keys are in k_slot
-            auto qk = [&](const Unit& u, int x, int k_slot) {
-                if (u.t == u.t0) {
+            auto arrived = [&](uint32_t tile) {
+                ok = ok && tile_wait(&tail->kv_full[tile % Shape::kSlots], tile / Shape::kSlots & 1u, tail, p);
+                return ok;
+            };
+            auto free_slot = [&](uint32_t tile) { ptx::mma_commit(&tail->kv_empty[tile % Shape::kSlots]); };
+            // S of row tile x for step u
+            auto qk = [&](const Step& u, int x) {
+                const uint32_t tile = u.at + (u.fold ? 2 * x : 0);
+                if (u.j == 0) {
                     ok = ok && tile_wait(&tail->q_full[x], q_phase >> x & 1u, tail, p);
-                    if (!ok) return;
                     q_phase ^= 1u << x;
-                    ptx::tc_fence_after_sync();
                 }
+                if (!arrived(tile)) return;
+                ptx::tc_fence_after_sync();
                 const uint64_t a = q_desc + (uint64_t)(x * (Shape::kQBytes >> 4));
-                const uint64_t b = k_desc + (uint64_t)(k_slot * (Shape::kSlotBytes >> 4));
+                const uint64_t b = k_desc + (uint64_t)(tile % Shape::kSlots * (Shape::kSlotBytes >> 4));
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint64_t at = (uint64_t)(((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4);
                     ptx::mma_f16_ss(tmem + x * 128, a + at, b + at, idesc_s, k != 0);
                 }
                 ptx::mma_commit(&tail->s_full[x]);
-                if (u.t + 1 == u.end[x]) ptx::mma_commit(&tail->q_empty[x]);
+                if (u.j + 1 == u.n[x]) ptx::mma_commit(&tail->q_empty[x]);
+                if (u.fold) free_slot(tile);
             };
-            Unit u;
+            Step u;
+            u.at = 0;
             enter(u);
             if (u.more) {
-                ok = tile_wait(&tail->kv_full[slot], phase, tail, p);
-                ptx::tc_fence_after_sync();
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
-                    if (u.t < u.end[x] && ok) qk(u, x, slot);
-                ptx::mma_commit(&tail->kv_empty[slot]);
-                advance();
+                    if (u.j < u.n[x] && ok) qk(u, x);
+                if (!u.fold) free_slot(u.at);
             }
             while (u.more && ok) {
-                const Unit now = u;
-                const int v_slot = slot;
-                ok = tile_wait(&tail->kv_full[v_slot], phase, tail, p);
-                advance();
-                const int k_slot = slot;
-                if (++u.t == u.t_end) enter(u);
-                if (u.more && ok) {
-                    ok = tile_wait(&tail->kv_full[k_slot], phase, tail, p);
-                    advance();
-                }
+                const Step now = u;
+                u.at += now.fold && now.j < now.n[1] ? 4 : 2;
+                if (++u.j == u.steps) enter(u);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    if (now.t < now.end[x]) {
+                    if (now.j < now.n[x] && ok) {
+                        const uint32_t tile = now.at + (now.fold ? 2 * x : 0) + 1;
+                        if (!arrived(tile)) break;
                         // the first half's keys are multiplied while the softmax warps work on the second's
-                        const uint64_t b = v_desc + (uint64_t)(v_slot * (Shape::kSlotBytes >> 4));
+                        const uint64_t b = v_desc + (uint64_t)(tile % Shape::kSlots * (Shape::kSlotBytes >> 4));
 #pragma unroll
                         for (int part = 0; part < 2; ++part) {
                             ok = ok && tile_wait(&tail->p_full[x][part], p_phase >> x & 1u, tail, p);
@@ -585,15 +607,16 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                             for (int k = 4 * part; k < 4 * part + 4; ++k)
                                 ptx::mma_f16_ts(tmem + 256 + x * D, tmem + x * 128 + 8 * k, b + (uint64_t)(k * 2048 >> 4), idesc_o,
-                                                now.t != now.t0 || k != 0);
+                                                now.j != 0 || k != 0);
                         }
                         p_phase ^= 1u << x;
                         ptx::mma_commit(&tail->o_full[x]);
+                        if (now.fold) free_slot(tile);
                     }
-                    if (u.more && u.t < u.end[x] && ok) qk(u, x, k_slot);
+                    if (u.more && u.j < u.n[x] && ok) qk(u, x);
                 }
-                ptx::mma_commit(&tail->kv_empty[v_slot]);
-                if (u.more) ptx::mma_commit(&tail->kv_empty[k_slot]);
+                if (!now.fold) free_slot(now.at + 1);
+                if (u.more && !u.fold) free_slot(u.at);
             }
             if (!ok) {                    // MMAs still running must end before shared memory and TMEM go away
                 ptx::mma_commit(&tail->drain);
@@ -616,8 +639,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             ok = items.ok;
             if (!items.more) break;
             const TileItem it = items.item();
-            const int t_end = max(it.end[0], it.end[1]);
-            for (int t = it.t0; t < t_end; ++t) {
+            for (int i = 0; i < it.tiles; ++i) {
+                const int t = unit_of(it, i);
                 const int valid = it.len - t * kTileKeys;
                 if (valid < kTileKeys) {
                     if (!wait(&tail->raw_full[slot], phases >> slot & 1u)) break;
@@ -648,15 +671,26 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + 256 + x * D;
         uint32_t s_phase = 0;                                      // parity of the unit whose S is waited for
+        // the two row tiles' warps that share lanes of TMEM meet where they work on the same rows
+        uint32_t meet_phase = 0;
+        auto meet = [&] {
+            ptx::tc_fence_before_sync();
+            ptx::mbar_arrive(&tail->meet[quad]);
+            if (!wait(&tail->meet[quad], meet_phase)) return false;
+            meet_phase ^= 1u;
+            ptx::tc_fence_after_sync();
+            return true;
+        };
         ItemReader items{tail, p, 0, true, false};
         for (; ok; items.template leave<true>(lane == 0)) {
             items.template fetch<true>();
             ok = items.ok;
             if (!items.more) break;
             const TileItem& it = items.item();
-            const int t0 = it.t0, t_end = it.end[x];
+            const bool fold = it.fold != 0;
+            const int t0 = it.begin[x], t_end = it.end[x];
             const bool any = t0 < t_end;                           // this row tile sees keys of this block's units
-            const int item_row = it.first_row + x * half + row;    // among the sequence's rows
+            const int item_row = it.first_row + (fold ? 0 : x * half) + row;      // among the sequence's rows
             const bool valid = row < half && item_row < it.rows;
             int row_limit = it.limit;
             if (p.causal && valid) row_limit = it.before + item_row / p.group + 1;
@@ -754,19 +788,42 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ptx::tc_fence_after_sync();
             }
             const float2 sums = unpack2(sum2);
-            const float sum = m == -INFINITY ? 0.0f : sums.x + sums.y;   // no key: exp2_poly is not quite 0 at -inf
+            float sum = m == -INFINITY ? 0.0f : sums.x + sums.y;   // no key: exp2_poly is not quite 0 at -inf
+            float f0 = 1.0f, f1 = 0.0f;                            // weights of the two row tiles' O
+            if (fold) {
+                if (x == 1) tail->other[row] = make_float2(m, sum);
+                if (!meet()) break;                                // both O are complete
+                if (x == 1) {
+                    if (!meet()) break;                            // and have been read
+                    continue;
+                }
+                const float2 o = tail->other[row];
+                const float m_new = fmaxf(m, o.x), ref = m_new == -INFINITY ? 0.0f : m_new;
+                f0 = exp2_approx(m - ref);
+                f1 = exp2_approx(o.x - ref);
+                m = m_new;
+                sum = sum * f0 + o.y * f1;
+            }
             const bool whole = it.whole;
             const float inv = sum > 0.0f ? (INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f) / sum : 0.0f;
             const int tok = item_row / p.group;
             const int head = it.h * p.group + item_row - tok * p.group;
             const long long token = it.first_token + tok;
-            const long long part_row = (long long)(2 * blockIdx.x + (t0 == 0 ? 1 : 0)) * 256 + x * 128 + row;
+            const long long part_row = (long long)(2 * blockIdx.x + (it.t0 == 0 ? 1 : 0)) * 256 + x * 128 + row;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 uint32_t o[32];
                 if (any) {
                     ptx::tmem_ld_32x32(o_addr + c, o);
                     ptx::tmem_ld_wait();
+                    if (fold) {
+                        uint32_t o1[32];
+                        ptx::tmem_ld_32x32(o_addr + D + c, o1);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            o[e] = __float_as_uint(__uint_as_float(o[e]) * f0 + __uint_as_float(o1[e]) * f1);
+                    }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0;
@@ -790,7 +847,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (valid && whole && p.lse != nullptr)
                 p.lse[token * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             if (valid && !whole) p.part_ml[part_row] = make_float2(m, sum);
-            if (!whole && t0 == 0 && tid == 0) {
+            if (!whole && it.t0 == 0 && tid == 0) {
                 PartItem pi;
                 pi.last = it.last;
                 pi.h = it.h;
@@ -801,6 +858,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 p.part_items[blockIdx.x] = pi;
             }
             ptx::tc_fence_before_sync();                           // O has been read: the next item's first PV may overwrite it
+            if (fold && !meet()) break;
         }
     }
 
