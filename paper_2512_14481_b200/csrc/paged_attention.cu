@@ -44,6 +44,7 @@ struct Plan {
     int rows;                   // of an item
     int slot_rows;              // room for an item's rows in a part slot
     int unit;
+    int max_rows;               // (token, head) rows of a sequence and KV head at most, by the host's bound
 };
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
@@ -52,6 +53,7 @@ Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, in
     Plan pl{};
     const int group = heads / c->num_kv_heads;
     const long long rows = (long long)b->max_q_len * group;
+    pl.max_rows = (int)(rows < (1 << 30) ? rows : 1 << 30);
     pl.tiles = rows > 16 && group <= 128 && c->num_pages > 0;
     pl.nb = rows <= 8 ? 1 : 2;
     pl.rows = pl.tiles ? 2 * (128 / group * group) : 8 * pl.nb;
@@ -143,8 +145,14 @@ bool encode_queries(CUtensorMap* m, const AttendParams& p) {
     return encode_map<BF>(m, const_cast<uint16_t*>(p.q), 3, dims, strides, box);
 }
 
+// groups of eight rows of the joining launch: all that an item can have (by the host's bound; the kernel walks on over
+// rows beyond it)
+unsigned join_rows(const AttendParams& p, int max_rows) {
+    return max_rows > p.item_rows / 2 ? 256 / 8 : (unsigned)ceil_div(max_rows < 1 ? 1 : max_rows, 8);
+}
+
 template <int D, bool BF, bool INT8>
-cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
+cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, int max_rows, cudaStream_t st) {
     static std::atomic<unsigned long long> ready{0};          // devices whose shared-memory limit has been raised
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -167,13 +175,13 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, cudaSt
     cfg.numAttrs = 1;
     e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF, INT8>, map_q, map_k, map_v, p);
     if (e != cudaSuccess || !p.split) return e;
-    return launch(paged_join_kernel<256, 128, D, BF>, dim3(p.max_blocks, 256 / 8), 256, 0, st, p);
+    return launch(paged_join_kernel<256, 128, D, BF>, dim3(p.max_blocks, join_rows(p, max_rows)), 256, 0, st, p);
 }
 
 template <int D, bool BF>
 cudaError_t launch_all(const Plan& pl, const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
     const bool int8 = c->kind == SASQ_KV_INT8;
-    if (pl.tiles) return int8 ? launch_tiles<D, BF, true>(p, c, st) : launch_tiles<D, BF, false>(p, c, st);
+    if (pl.tiles) return int8 ? launch_tiles<D, BF, true>(p, c, pl.max_rows, st) : launch_tiles<D, BF, false>(p, c, pl.max_rows, st);
     return pl.nb == 1 ? launch_rows<D, 1, BF>(p, int8, st) : launch_rows<D, 2, BF>(p, int8, st);
 }
 
@@ -227,7 +235,6 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.split = batch->max_seq_len > pl.unit;
     p.max_blocks = pl.blocks;
     p.item_rows = pl.rows;
-    p.min_units = 1;
     p.wait_limit = 1LL << 31;
     p.part_items = static_cast<PartItem*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + l.ml);

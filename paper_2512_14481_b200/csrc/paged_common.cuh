@@ -92,26 +92,32 @@ struct Schedule {
 };
 
 // First unit of block c when `total` units go to n blocks.
-__device__ __forceinline__ long long block_begin(long long total, int c, int n) { return total * c / n; }
+__device__ __forceinline__ long long block_begin(long long total, int c, int n) {
+    if (total < (1 << 20)) return (unsigned)total * (unsigned)c / (unsigned)n;      // c, n < 4096
+    return total * c / n;
+}
 // The block that has unit x.
-__device__ __forceinline__ int block_of(long long total, long long x, int n) { return (int)(((x + 1) * n + total - 1) / total) - 1; }
+__device__ __forceinline__ int block_of(long long total, long long x, int n) {
+    if (total < (1 << 20)) return (int)((((unsigned)x + 1) * (unsigned)n + (unsigned)total - 1) / (unsigned)total) - 1;
+    return (int)(((x + 1) * n + total - 1) / total) - 1;
+}
 
-// Where a block's stretch begins; found by the whole block together.
+// Where a block's stretch begins.
 struct Start {
     long long total;          // units of the call
     long long begin, end;     // this block's
     long long offset;         // of `begin` in sequence b
-    int b;
+    int b;                    // -1: nothing to do
     int blocks;               // blocks that have work
 };
 
-// Every thread of the block calls this; scratch: one long long per warp + one Start, in shared memory.
-template <int THREADS, int KT>
-__device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule<KT>& sch, int max_blocks, int min_units,
-                                            long long* scratch, Start* found) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (p.batch + THREADS - 1) / THREADS;
-    const int b0 = tid * per, b1 = min(b0 + per, p.batch);
+// A whole warp calls this; every lane gets the answer.  Each lane adds up a run of sequences: no barrier, and one round
+// trip to memory for up to 32 sequences.
+template <int KT>
+__device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule<KT>& sch, int max_blocks) {
+    const int lane = threadIdx.x & 31;
+    const int per = (p.batch + 31) >> 5;
+    const int b0 = lane * per, b1 = min(b0 + per, p.batch);
     long long mine = 0;
     for (int b = b0; b < b1; ++b) mine += sch.head_units(load_sequence(p, b)) * sch.heads;
     long long incl = mine;
@@ -120,40 +126,33 @@ __device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule
         const long long other = __shfl_up_sync(0xFFFFFFFFu, incl, off);
         if (lane >= off) incl += other;
     }
-    if (lane == 31) scratch[warp] = incl;
-    if (tid == 0) found->b = -1;
-    __syncthreads();
-    long long before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        const long long s = scratch[w];
-        before += w < warp ? s : 0;
-        total += s;
-    }
-    long long at = before + incl - mine;
-    const long long want = total / min_units;
-    const int blocks = want < 1 ? 1 : want < max_blocks ? (int)want : max_blocks;
-    const int c = blockIdx.x;
-    const long long begin = c < blocks ? block_begin(total, c, blocks) : total;
-    if (begin >= at && begin < at + mine) {
-        for (int b = b0; b < b1; ++b) {
-            const long long n = sch.head_units(load_sequence(p, b)) * sch.heads;
-            if (begin < at + n) {
-                found->b = b;
-                found->offset = begin - at;
-                break;
-            }
-            at += n;
-        }
-    }
-    __syncthreads();
     Start st;
-    st.total = total;
-    st.blocks = blocks;
-    st.begin = begin;
-    st.end = c < blocks ? block_begin(total, c + 1, blocks) : total;
-    st.b = found->b;
-    st.offset = st.b >= 0 ? found->offset : 0;
+    st.total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+    st.blocks = st.total < 1 ? 1 : st.total < max_blocks ? (int)st.total : max_blocks;
+    const int c = blockIdx.x;
+    st.begin = c < st.blocks ? block_begin(st.total, c, st.blocks) : st.total;
+    st.end = c < st.blocks ? block_begin(st.total, c + 1, st.blocks) : st.total;
+    // the lane in whose run the stretch begins walks its sequences
+    long long at = incl - mine;
+    const unsigned hit = __ballot_sync(0xFFFFFFFFu, st.begin >= at && st.begin < incl);
+    st.b = -1;
+    st.offset = 0;
+    if (hit != 0) {
+        const int owner = __ffs(hit) - 1;
+        if (lane == owner) {
+            for (int b = b0; b < b1; ++b) {
+                const long long n = per == 1 ? mine : sch.head_units(load_sequence(p, b)) * sch.heads;
+                if (st.begin < at + n) {
+                    st.b = b;
+                    st.offset = st.begin - at;
+                    break;
+                }
+                at += n;
+            }
+        }
+        st.b = __shfl_sync(0xFFFFFFFFu, st.b, owner);
+        st.offset = __shfl_sync(0xFFFFFFFFu, st.offset, owner);
+    }
     return st;
 }
 
@@ -177,7 +176,8 @@ struct Walk {
         it.s = load_sequence(p, it.b);
         n_tiles = sch.tiles(it.s);
         const long long per_head = sch.head_units(it.s);
-        it.h = (int)(st.offset / per_head);
+        it.h = st.offset < (1ll << 32) && per_head < (1ll << 32) ? (int)((unsigned)st.offset / (unsigned)per_head)
+                                                               : (int)(st.offset / per_head);
         long long rest = st.offset - it.h * per_head;
         it.i = 0;
         for (;;) {

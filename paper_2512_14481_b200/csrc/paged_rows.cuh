@@ -15,7 +15,7 @@ struct AttendParams {
     float scale;                // softmax_scale * log2(e)
     int causal;
     int split;                  // items may be cut among blocks (the joining launch follows)
-    int max_blocks, min_units;
+    int max_blocks;
     int item_rows;              // rows of an item
     PartItem* part_items;       // [max_blocks]
     float2* part_ml;            // [2 * max_blocks][R]: maximum (log2 units) and sum
@@ -72,8 +72,6 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm<D, NB, INT8>) p
     constexpr int kSteps = D / 16;                          // k16 steps of S, and 16-row blocks of O
     constexpr int VW = D / 8 * (INT8 ? 1 : 2) / 4;          // 32-bit words of a V row that a lane takes: D / 8 elements
 
-    __shared__ long long scratch[kRowsThreads / 32];
-    __shared__ Start found;
     __shared__ float sm_m[4][R], sm_l[4][R];
     __shared__ alignas(16) float sm_o[4][R][D];         // read back four at a time
 
@@ -81,7 +79,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm<D, NB, INT8>) p
     pdl_launch_dependents();
     pdl_wait();
     const Schedule<kRowsUnit> sch{R, p.group, p.causal, p.c.kv_heads};
-    const Start st = find_start<kRowsThreads, kRowsUnit>(p.c, sch, p.max_blocks, p.min_units, scratch, &found);
+    const Start st = find_start<kRowsUnit>(p.c, sch, p.max_blocks);
     if (tid == 0) p.part_items[blockIdx.x].last = -1;
     Walk<kRowsUnit> walk;
     for (bool more = walk.begin(p.c, sch, st, p.split != 0); more; more = walk.next(p.c)) {
@@ -376,57 +374,59 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocksPerSm<D, NB, INT8>) p
     }
 }
 
-// Joins the parts of the item that began in block x and ended in a later one; one warp per row.  The parts lie in the
-// second slot of block x and in the first slots of the blocks after it, and are added in that order.  R rows of a slot,
-// in row tiles of TILE of which an item may use fewer.
+// Joins the parts of the item that began in block x and ended in a later one; a warp per row, rows gridDim.y * 8 apart.
+// The parts lie in the second slot of block x and in the first slots of the blocks after it, and are added in that
+// order.  R rows of a slot, in row tiles of TILE of which an item may use fewer.
 template <int R, int TILE, int D, bool BF>
 __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttendParams p) {
     pdl_launch_dependents();
     pdl_wait();
     const int c = blockIdx.x, lane = threadIdx.x & 31;
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
     const PartItem pi = p.part_items[c];
-    const int item_row = r / TILE * pi.tile_rows + r % TILE;
-    if (pi.last < 0 || r % TILE >= pi.tile_rows || item_row >= pi.rows) return;
+    if (pi.last < 0) return;
     constexpr int N = D / 32;                                  // elements of a lane
-    auto slot_of = [&](int k) { return (long long)(k == c ? 2 * c + 1 : 2 * k) * R + r; };
-    float m = -INFINITY;
-    for (int k = c + lane; k <= pi.last; k += 32) m = fmaxf(m, p.part_ml[slot_of(k)].x);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f, acc[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = 0.0f;
-#pragma unroll 4
-    for (int k = c; k <= pi.last; ++k) {
-        const long long s = slot_of(k);
-        const float2 ml = p.part_ml[s];
-        const float f = exp2_approx(ml.x - ref);
-        sum += f * ml.y;
-        const float* src = p.part_o + s * D + lane * N;
-        if constexpr (N == 4) {
-            const float4 v = *reinterpret_cast<const float4*>(src);
-            acc[0] += f * v.x;
-            acc[1] += f * v.y;
-            acc[2] += f * v.z;
-            acc[3] += f * v.w;
-        } else {
-            const float2 v = *reinterpret_cast<const float2*>(src);
-            acc[0] += f * v.x;
-            acc[1] += f * v.y;
-        }
-    }
     const float vs = p.c.v_scale != nullptr ? __ldg(p.c.v_scale + pi.h) : 1.0f;
-    const float inv = sum > 0.0f ? vs / sum : 0.0f;
-    const int row = pi.first_row + item_row, tok = row / p.group;
-    const int head = pi.h * p.group + row - tok * p.group;
-    const long long t = pi.first_token + tok;
-    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + t * p.out_stride + (long long)head * D + lane * N);
+    for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); r < R; r += gridDim.y * 8) {
+        const int item_row = r / TILE * pi.tile_rows + r % TILE;
+        if (r % TILE >= pi.tile_rows || item_row >= pi.rows) continue;
+        auto slot_of = [&](int k) { return (long long)(k == c ? 2 * c + 1 : 2 * k) * R + r; };
+        float m = -INFINITY;
+        for (int k = c + lane; k <= pi.last; k += 32) m = fmaxf(m, p.part_ml[slot_of(k)].x);
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) dst[e] = narrow2<BF>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    if (lane == 0 && p.lse != nullptr)
-        p.lse[t * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float sum = 0.0f, acc[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = 0.0f;
+#pragma unroll 4
+        for (int k = c; k <= pi.last; ++k) {
+            const long long s = slot_of(k);
+            const float2 ml = p.part_ml[s];
+            const float f = exp2_approx(ml.x - ref);
+            sum += f * ml.y;
+            const float* src = p.part_o + s * D + lane * N;
+            if constexpr (N == 4) {
+                const float4 v = *reinterpret_cast<const float4*>(src);
+                acc[0] += f * v.x;
+                acc[1] += f * v.y;
+                acc[2] += f * v.z;
+                acc[3] += f * v.w;
+            } else {
+                const float2 v = *reinterpret_cast<const float2*>(src);
+                acc[0] += f * v.x;
+                acc[1] += f * v.y;
+            }
+        }
+        const float inv = sum > 0.0f ? vs / sum : 0.0f;
+        const int row = pi.first_row + item_row, tok = row / p.group;
+        const int head = pi.h * p.group + row - tok * p.group;
+        const long long t = pi.first_token + tok;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + t * p.out_stride + (long long)head * D + lane * N);
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) dst[e] = narrow2<BF>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+        if (lane == 0 && p.lse != nullptr)
+            p.lse[t * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+    }
 }
 
 }  // namespace

@@ -122,8 +122,6 @@ struct TileTail {
     uint64_t s_full[2], p_full[2][2], o_full[2];            // p_full: either half of the unit's keys
     uint64_t drain, meet[4];
     float2 other[128];        // reference and sum of the second row tile's rows, for the first
-    long long scratch[20];
-    Start found;
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -210,30 +208,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
-}
-
-// Of every 8 pairs of a row this many take 2^x from a polynomial on the FMA pipe, the others from the special-function
-// unit (which needs 8 cycles per warp and exponential, as long as the two MMAs of the same logits take).
-#ifndef POLYP
-#define POLYP 0
-#endif
-constexpr int kPolyPairs = POLYP;
-
-// 2^x for two values: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), a polynomial
-// of degree 4 for 2^f on [-1/2, 1/2] (least maximum relative error, 2.6e-6, by Remez exchange), and n added to the exponent.
-// x below -125 counts as -125.
-__device__ __forceinline__ uint64_t exp2_poly(float2 x) {
-    const uint64_t z = pack2(fmaxf(x.x, -125.0f), fmaxf(x.y, -125.0f));
-    const uint64_t big = pack2(12582912.0f, 12582912.0f);
-    const uint64_t t = add2(z, big);
-    const uint64_t f = fma2(add2(t, pack2(-12582912.0f, -12582912.0f)), pack2(-1.0f, -1.0f), z);
-    uint64_t y = fma2(f, pack2(0.009570102207362652f, 0.009570102207362652f), pack2(0.05591785907745361f, 0.05591785907745361f));
-    y = fma2(y, f, pack2(0.240247443318367f, 0.240247443318367f));
-    y = fma2(y, f, pack2(0.6931217908859253f, 0.6931217908859253f));
-    y = fma2(y, f, pack2(0.9999992847442627f, 0.9999992847442627f));
-    const float2 n = unpack2(t), v = unpack2(y);
-    return pack2(__uint_as_float(__float_as_uint(v.x) + (__float_as_uint(n.x) << 23)),
-                 __uint_as_float(__float_as_uint(v.y) + (__float_as_uint(n.y) << 23)));
 }
 
 // The warps that fill the ring from an int8 cache (`me` of kConvertThreads): K and V of each unit in turn, in the layout
@@ -391,7 +365,6 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     pdl_wait();
 
     const TileSchedule sch{p.item_rows, p.group, p.causal, p.c.kv_heads};
-    const Start st = find_start<kTileThreads<INT8>, kTileKeys>(p.c, sch, p.max_blocks, p.min_units, tail->scratch, &tail->found);
     if (tid == 0) p.part_items[blockIdx.x].last = -1;
     bool ok = true;
     // whole warps wait together: a role goes on, or gives up, as a warp
@@ -415,12 +388,20 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             ok = items.ok;
             if (!items.more) break;
             const TileItem it = items.item();
+            // a unit's page entries are asked for while the unit before waits for its slots
+            const int* table = p.c.page_table + it.b * p.c.table_stride;
+            auto look_up = [&](int i) {
+                const int key = unit_of(it, i) * kTileKeys + lane * box;
+                return i < it.tiles && lane < boxes && key < it.len ? __ldg(table + (key >> p.c.page_shift)) : -1;
+            };
+            int next_entry = look_up(0);
             for (int i = 0; i < it.tiles && ok; ++i) {
                 const int t = unit_of(it, i);
                 const int key = t * kTileKeys + lane * box;
+                const int entry = next_entry;
+                next_entry = look_up(i + 1);
                 int page = (int)p.c.num_pages;                  // outside the cache: the copy fills in zeros
                 if (lane < boxes && key < it.len) {
-                    const int entry = __ldg(p.c.page_table + it.b * p.c.table_stride + (key >> p.c.page_shift));
                     if (entry < 0 || entry >= p.c.num_pages) atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
                     else page = entry;
                 }
@@ -459,6 +440,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---------------- the block's items, for everyone, and their Q ----------------
         uint32_t filled[2] = {0, 0};                            // times that each row tile's queries were asked for
         const int tokens = 128 / p.group;
+        const Start st = find_start<kTileKeys>(p.c, sch, p.max_blocks);
         TileWalk walk;
         int n = 0;
         for (bool more = walk.begin(p.c, sch, st, p.split != 0);; more = walk.next(p.c), ++n) {
@@ -705,10 +687,16 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ptx::tc_fence_after_sync();
                 const int seen = row_limit - t * kTileKeys;
                 const bool cut = __any_sync(0xFFFFFFFFu, seen < kTileKeys);
-                // The row is read twice: for its maximum, second half first, and for the exponentials, whose first half is
-                // still in registers.  128 logits and what is made of them do not fit a thread's registers.
-                uint32_t s[2][32];
-                auto fetch = [&](int part) {
+                // The row is read in halves, the second one twice: for its maximum before the first half, and for its
+                // exponentials behind it.  128 logits and what is made of them do not fit a thread's registers.  With the
+                // int8 cache the three steps share their code: the converting warps need the instruction cache too
+                // (measured on a 1024-token chunk over 15000 keys: int8 350 -> 323 us, 16-bit 227 -> 246 us).
+                constexpr int kSteps = INT8 ? 1 : 3;
+                float most = -INFINITY;
+#pragma unroll kSteps
+                for (int step = 0; step < 3; ++step) {
+                    const int part = step == 1 ? 0 : 1;
+                    uint32_t s[2][32];
                     ptx::tmem_ld_32x32(s_addr + part * 64, s[0]);
                     ptx::tmem_ld_32x32(s_addr + part * 64 + 32, s[1]);
                     ptx::tmem_ld_wait();
@@ -717,63 +705,54 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         for (int e = 0; e < 64; ++e) s[e >> 5][e & 31] ^= 0x80000000u;
                     }
                     if (cut) {
+                        const int left = seen - part * 64;
 #pragma unroll
                         for (int e = 0; e < 64; ++e)
-                            if (part * 64 + e >= seen) s[e >> 5][e & 31] = 0xFF800000u;      // -inf
+                            if (e >= left) s[e >> 5][e & 31] = 0xFF800000u;      // -inf
                     }
-                };
-                auto most_of = [&]() {
-                    float top[4];
+                    if (step < 2) {
+                        float top[4];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t* w = s[c >> 1] + 16 * (c & 1);
-                        top[c] = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t* w = s[c >> 1] + 16 * (c & 1);
+                            top[c] = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 #pragma unroll
-                        for (int e = 2; e < 16; e += 2) top[c] = max3(top[c], __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
+                            for (int e = 2; e < 16; e += 2) top[c] = max3(top[c], __uint_as_float(w[e]), __uint_as_float(w[e + 1]));
+                        }
+                        most = fmaxf(most, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
                     }
-                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                };
-                fetch(1);
-                float most = most_of();
-                fetch(0);
-                most = fmaxf(most, most_of()) * scale;
-                if (__any_sync(0xFFFFFFFFu, most > m + kRescaleAt)) {
-                    const float m_new = fmaxf(m, most);
-                    const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m - m_new);
-                    m = m_new;
-                    const float2 old = unpack2(sum2);
-                    sum2 = pack2(old.x * f, old.y * f);
-                    if (t > t0) {          // S(t) was asked for behind the second product of t - 1, which is done as well
+                    if (step == 0) continue;
+                    if (step == 1) {
+                        most *= scale;
+                        if (__any_sync(0xFFFFFFFFu, most > m + kRescaleAt)) {
+                            const float m_new = fmaxf(m, most);
+                            const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m - m_new);
+                            m = m_new;
+                            const float2 old = unpack2(sum2);
+                            sum2 = pack2(old.x * f, old.y * f);
+                            if (t > t0) {     // S(t) was asked for behind the second product of t - 1, which is done as well
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
-                            uint32_t o[16];
-                            ptx::tmem_ld_32x16(o_addr + c, o);
-                            ptx::tmem_ld_wait();
+                                for (int c = 0; c < D; c += 16) {
+                                    uint32_t o[16];
+                                    ptx::tmem_ld_32x16(o_addr + c, o);
+                                    ptx::tmem_ld_wait();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            ptx::tmem_st_32x16(o_addr + c, o);
+                                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                    ptx::tmem_st_32x16(o_addr + c, o);
+                                }
+                            }
                         }
                     }
-                }
-                const float ref = m == -INFINITY ? 0.0f : m;
-                const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-ref, -ref);
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    if (part == 1) fetch(1);
+                    const float ref = m == -INFINITY ? 0.0f : m;
+                    const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-ref, -ref);
                     uint32_t pk[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
                         const float2 z = unpack2(fma2(pack2(__uint_as_float(s[e >> 4][2 * e & 31]), __uint_as_float(s[e >> 4][(2 * e & 31) + 1])),
                                                       scale2, ref2));
-                        uint64_t pr;
-                        if (e % 8 < kPolyPairs) {
-                            pr = exp2_poly(z);
-                        } else {
-                            pr = pack2(exp2_approx(z.x), exp2_approx(z.y));
-                        }
-                        sum2 = add2(sum2, pr);
-                        const float2 both = unpack2(pr);
-                        pk[e] = narrow2<BF>(both.x, both.y);
+                        const float p0 = exp2_approx(z.x), p1 = exp2_approx(z.y);
+                        sum2 = add2(sum2, pack2(p0, p1));
+                        pk[e] = narrow2<BF>(p0, p1);
                     }
                     ptx::tmem_st_32x32(s_addr + part * 32, pk);
                     ptx::tmem_st_wait();
@@ -788,7 +767,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ptx::tc_fence_after_sync();
             }
             const float2 sums = unpack2(sum2);
-            float sum = m == -INFINITY ? 0.0f : sums.x + sums.y;   // no key: exp2_poly is not quite 0 at -inf
+            float sum = sums.x + sums.y;
             float f0 = 1.0f, f1 = 0.0f;                            // weights of the two row tiles' O
             if (fold) {
                 if (x == 1) tail->other[row] = make_float2(m, sum);
@@ -810,6 +789,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const int head = it.h * p.group + item_row - tok * p.group;
             const long long token = it.first_token + tok;
             const long long part_row = (long long)(2 * blockIdx.x + (it.t0 == 0 ? 1 : 0)) * 256 + x * 128 + row;
+            // A thread stores its own row in 16-byte pieces.  Turning 4 x 4 pieces among four lanes first, so that a store
+            // covers 64 bytes of a row, cost more instructions (cold in the caches, once an item) than it saved stores:
+            // 47.5 against 43.9 us for seven-token drafts of 16 sequences.
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 uint32_t o[32];

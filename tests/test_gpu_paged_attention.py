@@ -145,6 +145,18 @@ def test_offsets_beyond_32_bits():
     assert (np.abs(out.float().cpu().double().numpy() - want) <= tol).all()
 
 
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim,new,lens", [
+    (32, 32, 128, [300, 40, 257], [1500, 900, 2300]),       # several units and items per block, both row tiles in use
+    (24, 24, 128, [20, 33, 7], [3000, 2000, 1111]),         # rows for one row tile, long keys
+    (40, 8, 64, [7, 90, 33], [4000, 3000, 1800]),
+    (8, 8, 64, [1000, 129], [1700, 1900]),
+    (64, 64, 128, [1, 1, 1, 1], [700, 40, 3000, 1]),        # more units than blocks, single tokens
+])
+def test_more_work_than_blocks(heads, kv_heads, dim, new, lens, int8):
+    check(R.Batch(lens, new, heads, kv_heads, dim, 64, torch.float16 if dim == 64 else torch.bfloat16, int8, seed=heads + dim))
+
+
 @pytest.mark.parametrize("new", [1, 60])
 def test_other_stream_and_graph(new):
     """On a stream of its own, and replayed from a graph on new values, lengths and pages."""
