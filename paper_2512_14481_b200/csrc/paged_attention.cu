@@ -25,6 +25,7 @@ int* paged_status_ptr() {
 namespace {
 
 constexpr int kMaxSms = 256;
+constexpr int kClusterKeysPerWarp = 1536;
 
 struct Layout {
     size_t ml, o, total;        // byte offsets behind the part items
@@ -39,6 +40,8 @@ Layout layout_of(int blocks, int R, int D) {
 
 struct Plan {
     bool tiles;                 // the tensor-core kernel for many rows; else the few-row kernel
+    int cluster;                // few-row kernel: warps of the blocks of an item's cluster, or 0
+    int tile_bound;
     int nb;                     // few-row kernel: blocks of 8 rows
     int blocks;
     int rows;                   // of an item
@@ -67,6 +70,14 @@ Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, in
                                   : kRowsBlocksPerSm<128, 2, false>;
     const long long fill = (long long)sms * per_sm;
     pl.blocks = (int)(most < fill ? (most < 1 ? 1 : most) : fill);
+    pl.tile_bound = rows < 1 ? 1 : ceil_div(rows, pl.rows);
+    // Few items: a cluster each, if all clusters are resident at once and a block's eighth of the keys is not long.  One
+    // token, 32 heads over 1000 keys: 8.2 us in clusters, 15.0 us in equal stretches with a joining launch; over 4000 keys
+    // 19.1 and 22.8 us; over 16000 keys 58.5 and 51.7 us.  Where there is no more than a block for each SM its warps are
+    // eight (8 heads over 4000 keys: 10.3 us; with four 13.4 us), and the keys may be twice as many.
+    const int warps = items * kClusterBlocks <= sms && pl.nb * c->head_dim <= 128 ? 8 : 4;
+    if (!pl.tiles && items > 0 && items * kClusterBlocks <= fill && b->max_seq_len <= kClusterKeysPerWarp * warps) pl.cluster = warps;
+    if (pl.cluster != 0) pl.blocks = (int)items * kClusterBlocks;
     return pl;
 }
 
@@ -80,24 +91,37 @@ int attend_check(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, int
 }
 
 template <typename Kernel>
-cudaError_t launch(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, const AttendParams& p) {
+cudaError_t launch(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, const AttendParams& p, int cluster = 1) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr = pdl_attribute();
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0] = pdl_attribute();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 template <int D, int NB, bool BF>
-cudaError_t launch_rows(const AttendParams& p, bool int8, cudaStream_t st) {
-    const cudaError_t e = int8 ? launch(paged_rows_kernel<D, NB, BF, true>, dim3(p.max_blocks), kRowsThreads, 0, st, p)
-                               : launch(paged_rows_kernel<D, NB, BF, false>, dim3(p.max_blocks), kRowsThreads, 0, st, p);
+cudaError_t launch_rows(const Plan& pl, const AttendParams& p, bool int8, cudaStream_t st) {
+    const dim3 grid((unsigned)p.max_blocks);
+    if constexpr (NB * D <= 128) {             // eight warps' sums fit 48 KB of shared memory
+        if (pl.cluster == 8)
+            return int8 ? launch(paged_rows_kernel<D, NB, BF, true, true, 8>, grid, 256, 0, st, p, kClusterBlocks)
+                        : launch(paged_rows_kernel<D, NB, BF, false, true, 8>, grid, 256, 0, st, p, kClusterBlocks);
+    }
+    if (pl.cluster != 0)
+        return int8 ? launch(paged_rows_kernel<D, NB, BF, true, true, 4>, grid, 128, 0, st, p, kClusterBlocks)
+                    : launch(paged_rows_kernel<D, NB, BF, false, true, 4>, grid, 128, 0, st, p, kClusterBlocks);
+    const cudaError_t e = int8 ? launch(paged_rows_kernel<D, NB, BF, true, false, 4>, grid, 128, 0, st, p)
+                               : launch(paged_rows_kernel<D, NB, BF, false, false, 4>, grid, 128, 0, st, p);
     if (e != cudaSuccess || !p.split) return e;
-    return launch(paged_join_kernel<8 * NB, 8 * NB, D, BF>, dim3(p.max_blocks, NB), 256, 0, st, p);
+    return launch(paged_join_kernel<8 * NB, 8 * NB, D, BF, true>, dim3(p.max_blocks, 8 * NB), 256, 0, st, p);
 }
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -175,14 +199,14 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, int ma
     cfg.numAttrs = 1;
     e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF, INT8>, map_q, map_k, map_v, p);
     if (e != cudaSuccess || !p.split) return e;
-    return launch(paged_join_kernel<256, 128, D, BF>, dim3(p.max_blocks, join_rows(p, max_rows)), 256, 0, st, p);
+    return launch(paged_join_kernel<256, 128, D, BF, false>, dim3(p.max_blocks, join_rows(p, max_rows)), 256, 0, st, p);
 }
 
 template <int D, bool BF>
 cudaError_t launch_all(const Plan& pl, const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
     const bool int8 = c->kind == SASQ_KV_INT8;
     if (pl.tiles) return int8 ? launch_tiles<D, BF, true>(p, c, pl.max_rows, st) : launch_tiles<D, BF, false>(p, c, pl.max_rows, st);
-    return pl.nb == 1 ? launch_rows<D, 1, BF>(p, int8, st) : launch_rows<D, 2, BF>(p, int8, st);
+    return pl.nb == 1 ? launch_rows<D, 1, BF>(pl, p, int8, st) : launch_rows<D, 2, BF>(pl, p, int8, st);
 }
 
 }  // namespace
@@ -235,6 +259,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.split = batch->max_seq_len > pl.unit;
     p.max_blocks = pl.blocks;
     p.item_rows = pl.rows;
+    p.tile_bound = pl.tile_bound;
     p.wait_limit = 1LL << 31;
     p.part_items = static_cast<PartItem*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + l.ml);
