@@ -789,31 +789,38 @@ def _heads(t, name: str, dtype, total: int, heads: int | None, dim: int):
     return shape[1], (stride[0] if total > 1 else max(stride[0], shape[1] * dim))
 
 
+def _stream_of(t, stream) -> int:
+    """As _stream, for calls whose tensors are known to lie on one device: the raw handle of its current stream."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(t.get_device())
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
 def sasq_rope_kv_append(cache: KVCache, batch: PagedBatch, q, k, v, q_out, cos_sin, interleaved: bool = False,
                         stream=None) -> None:
     """Appends k, v [total_q, num_kv_heads, head_dim] to the cache with the rotation of cos_sin [max_positions, rot_dim]
     fp32 (None: no rotation) applied to k, and to q [total_q, num_q_heads, head_dim] -> q_out (both None: skip)."""
     T, K, D = batch.total_q, cache.num_kv_heads, cache.head_dim
-    dt = _dt(k)
-    if cache.dtype is not torch.int8 and cache.dtype != k.dtype:
+    dt = k.dtype
+    if cache.dtype is not torch.int8 and cache.dtype != dt:
         raise TypeError(f"k must have the cache's dtype {cache.dtype}")
-    _, ks = _heads(k, "k", k.dtype, T, K, D)
-    _, vs = _heads(v, "v", k.dtype, T, K, D)
+    _, ks = _heads(k, "k", dt, T, K, D)
+    _, vs = _heads(v, "v", dt, T, K, D)
     H = qs = qos = 0
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     if q is not None:
-        H, qs = _heads(q, "q", k.dtype, T, None, D)
-        _, qos = _heads(q_out, "q_out", k.dtype, T, H, D)
+        H, qs = _heads(q, "q", dt, T, None, D)
+        _, qos = _heads(q_out, "q_out", dt, T, H, D)
     positions = rot = 0
     if cos_sin is not None:
         _dev(cos_sin, "cos_sin", torch.float32)
         if cos_sin.dim() != 2:
             raise ValueError("cos_sin must be [max_positions, rot_dim]")
         positions, rot = cos_sin.shape
-    _check(load_library().sasq_rope_kv_append(cache.ref, batch.ref, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), qs, ks, vs, qos,
-                                              H, _ptr(cos_sin), positions, rot, int(bool(interleaved)), dt,
-                                              _stream(stream)), "sasq_rope_kv_append")
+    _check((_lib or load_library()).sasq_rope_kv_append(
+        cache.ref, batch.ref, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_out), qs, ks, vs, qos, H, _ptr(cos_sin), positions,
+        rot, 1 if interleaved else 0, _dt(k), _stream_of(k, stream)), "sasq_rope_kv_append")
 
 
 def sasq_paged_attention_workspace(cache: KVCache, batch: PagedBatch, num_q_heads: int) -> int:
@@ -825,17 +832,16 @@ def sasq_paged_attention(cache: KVCache, batch: PagedBatch, q, out, workspace, l
     """Attention of q [total_q, num_q_heads, head_dim] over the cache -> out of the same shape, lse [total_q, num_q_heads]
     fp32 or None; scale defaults to head_dim ** -0.5."""
     T, D = batch.total_q, cache.head_dim
-    dt = _dt(q)
-    if cache.dtype is not torch.int8 and cache.dtype != q.dtype:
+    dt = q.dtype
+    if cache.dtype is not torch.int8 and cache.dtype != dt:
         raise TypeError(f"q must have the cache's dtype {cache.dtype}")
-    H, qs = _heads(q, "q", q.dtype, T, None, D)
-    _, os_ = _heads(out, "out", q.dtype, T, H, D)
+    H, qs = _heads(q, "q", dt, T, None, D)
+    _, os_ = _heads(out, "out", dt, T, H, D)
     if lse is not None:
         _dev(lse, "lse", torch.float32)
-        if tuple(lse.shape) != (T, H):
+        if lse.shape != (T, H):
             raise ValueError("lse must be [total_q, num_q_heads]")
     _dev(workspace, "workspace")
-    _check(load_library().sasq_paged_attention(cache.ref, batch.ref, _ptr(q), _ptr(out), _ptr(lse), qs, os_, H,
-                                               D ** -0.5 if scale is None else float(scale), int(bool(causal)), dt,
-                                               _ptr(workspace), _nbytes(workspace), _stream(stream)),
-           "sasq_paged_attention")
+    _check((_lib or load_library()).sasq_paged_attention(
+        cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _ptr(lse), qs, os_, H, D ** -0.5 if scale is None else scale,
+        1 if causal else 0, _dt(q), workspace.data_ptr(), workspace.nbytes, _stream_of(q, stream)), "sasq_paged_attention")
