@@ -484,7 +484,7 @@ SASQ_API int sasq_adamw_scales(float* scales_dev, const float* grad_scales_dev, 
  * The paper has no counterpart. */
 SASQ_API int sasq_set_gang_launch(int on);
 
-/* Test hook.  Every wait inside the GEMM kernels (on an mbarrier, on the activation quantizer's counters) gives up
+/* Test hook.  Every wait inside the GEMM and attention kernels (on an mbarrier, on the activation quantizer's counters) gives up
  * after this many SM clock cycles, raises SASQ_ERR_TIMEOUT in the status word and lets the kernel finish in an
  * orderly way (outputs are then unspecified).  The default is 2^31 cycles, about a second; a negative value restores
  * it.  Returns the previous limit.  Applies to launches made afterwards.  sasq_device_status clears the library's

@@ -745,7 +745,9 @@ class KVCache:
                     raise ValueError(f"{name} must hold one factor per KV head")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.num_kv_heads, self.head_dim, self.dtype = k.shape[2], k.shape[3], k.dtype
-        self.struct = KVCacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.stride(0), k.stride(1), k.stride(2),
+        # a dimension of one entry may have any stride in torch; the library wants whole 16-byte words
+        page_stride, token_stride, head_stride, _ = (s if n > 1 else k.shape[3] for s, n in zip(k.stride(), k.shape))
+        self.struct = KVCacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), page_stride, token_stride, head_stride,
                                     k.shape[0], k.shape[1], k.shape[2], k.shape[3],
                                     SASQ_KV_INT8 if int8 else SASQ_KV_16BIT)
         self.ref = ctypes.byref(self.struct)

@@ -6,6 +6,8 @@
 
 namespace sasq {
 
+long long debug_wait_limit();       // sasq_debug_set_wait_limit's setting
+
 SASQ_DEFINE_STATUS_WORD(g_paged_status)
 
 int paged_status_read_and_clear(cudaStream_t st) { return g_paged_status_read_and_clear(st); }
@@ -47,38 +49,80 @@ struct Plan {
     int rows;                   // of an item
     int slot_rows;              // room for an item's rows in a part slot
     int unit;
+    long long items;            // by the host's bounds
+    int fill;                   // blocks that are resident at once
     int max_rows;               // (token, head) rows of a sequence and KV head at most, by the host's bound
 };
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
+// The equal-stretch plan of the few-row kernel, and of the tensor-core kernel.
+Plan rows_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
     Plan pl{};
-    const int group = heads / c->num_kv_heads;
-    const long long rows = (long long)b->max_q_len * group;
-    pl.max_rows = (int)(rows < (1 << 30) ? rows : 1 << 30);
-    pl.tiles = rows > 16 && group <= 128 && c->num_pages > 0;
-    pl.nb = rows <= 8 ? 1 : 2;
-    pl.rows = pl.tiles ? 2 * (128 / group * group) : 8 * pl.nb;
-    pl.slot_rows = pl.tiles ? 256 : pl.rows;
-    pl.unit = pl.tiles ? kTileKeys : kRowsUnit;
-    const long long items = (long long)b->batch * c->num_kv_heads * (rows < 1 ? 1 : ceil_div(rows, pl.rows));
-    const long long most = items * (b->max_seq_len < 1 ? 1 : ceil_div(b->max_seq_len, pl.unit));
+    const long long rows = (long long)b->max_q_len * (heads / c->num_kv_heads);
     const bool int8 = c->kind == SASQ_KV_INT8, d128 = c->head_dim == 128;
-    const int per_sm = pl.tiles ? 1 : pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
+    pl.nb = rows <= 8 ? 1 : 2;
+    pl.rows = pl.slot_rows = 8 * pl.nb;
+    pl.unit = kRowsUnit;
+    pl.tile_bound = rows < 1 ? 1 : ceil_div(rows, pl.rows);
+    const int per_sm = pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
                                           : (int8 ? kRowsBlocksPerSm<64, 1, true> : kRowsBlocksPerSm<64, 1, false>))
                                   : kRowsBlocksPerSm<128, 2, false>;
-    const long long fill = (long long)sms * per_sm;
-    pl.blocks = (int)(most < fill ? (most < 1 ? 1 : most) : fill);
-    pl.tile_bound = rows < 1 ? 1 : ceil_div(rows, pl.rows);
+    pl.items = (long long)b->batch * c->num_kv_heads * pl.tile_bound;
+    pl.fill = sms * per_sm;
+    return pl;
+}
+Plan tiles_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
+    Plan pl{};
+    const int group = heads / c->num_kv_heads;
+    pl.tiles = true;
+    pl.rows = 2 * (128 / group * group);
+    pl.slot_rows = 256;
+    pl.unit = kTileKeys;
+    pl.items = (long long)b->batch * c->num_kv_heads * ceil_div((long long)b->max_q_len * group, pl.rows);
+    pl.fill = sms;
+    return pl;
+}
+void set_blocks(Plan* pl, const sasq_kv_batch_t* b) {
+    const long long most = pl->items * (b->max_seq_len < 1 ? 1 : ceil_div(b->max_seq_len, pl->unit));
+    pl->blocks = (int)(most < pl->fill ? (most < 1 ? 1 : most) : pl->fill);
+}
+bool tiles_possible(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads) {
+    const int group = heads / c->num_kv_heads;
+    return (long long)b->max_q_len * group > 16 && group <= 128 && c->num_pages > 0;
+}
+
+Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
+    Plan pl = rows_plan(c, b, heads, sms);
+    const long long rows = (long long)b->max_q_len * (heads / c->num_kv_heads);
     // Few items: a cluster each, if all clusters are resident at once and a block's eighth of the keys is not long.  One
     // token, 32 heads over 1000 keys: 8.2 us in clusters, 15.0 us in equal stretches with a joining launch; over 4000 keys
     // 19.1 and 22.8 us; over 16000 keys 58.5 and 51.7 us.  Where there is no more than a block for each SM its warps are
     // eight (8 heads over 4000 keys: 10.3 us; with four 13.4 us), and the keys may be twice as many.
-    const int warps = items * kClusterBlocks <= sms && pl.nb * c->head_dim <= 128 ? 8 : 4;
-    if (!pl.tiles && items > 0 && items * kClusterBlocks <= fill && b->max_seq_len <= kClusterKeysPerWarp * warps) pl.cluster = warps;
-    if (pl.cluster != 0) pl.blocks = (int)items * kClusterBlocks;
+    const int warps = pl.items * kClusterBlocks <= sms && pl.nb * c->head_dim <= 128 ? 8 : 4;
+    if (pl.items > 0 && pl.items * kClusterBlocks <= pl.fill && b->max_seq_len <= kClusterKeysPerWarp * warps) pl.cluster = warps;
+    // More rows than one item of the few-row kernel holds: the tensor-core kernel, except for up to 64 rows in clusters
+    // (8 KV heads with 20, 32 and 64 rows over 1000 keys: 9.0, 9.6 and 9.8 us, on the tensor cores 14.4, 14.4 and 15.0 us;
+    // 128 rows: 22.5 and 17.8 us; 16 sequences with 20 rows, not in clusters: 35.0 and 28.3 us).
+    if (tiles_possible(c, b, heads) && (pl.cluster == 0 || rows > 64)) pl = tiles_plan(c, b, heads, sms);
+    if (pl.cluster != 0) pl.blocks = (int)pl.items * kClusterBlocks;
+    else set_blocks(&pl, b);
+    pl.max_rows = (int)(rows < (1 << 30) ? rows : 1 << 30);
     return pl;
+}
+
+// What any plan can need, whatever the device's number of SMs.
+size_t most_workspace(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads) {
+    Plan few = rows_plan(c, b, heads, kMaxSms);
+    set_blocks(&few, b);
+    size_t bytes = layout_of(few.blocks, few.slot_rows, c->head_dim).total;
+    if (tiles_possible(c, b, heads)) {
+        Plan many = tiles_plan(c, b, heads, kMaxSms);
+        set_blocks(&many, b);
+        const size_t m = layout_of(many.blocks, many.slot_rows, c->head_dim).total;
+        bytes = m > bytes ? m : bytes;
+    }
+    return bytes;
 }
 
 int attend_check(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, int num_q_heads, int dt, PagedParams* p) {
@@ -218,8 +262,7 @@ size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, const sasq_k
     using namespace sasq;
     PagedParams p{};
     if (attend_check(cache, batch, num_q_heads, SASQ_BF16, &p) != SASQ_OK) return 0;
-    const Plan pl = make_plan(cache, batch, num_q_heads, kMaxSms);
-    return layout_of(pl.blocks, pl.slot_rows, cache->head_dim).total;
+    return most_workspace(cache, batch, num_q_heads);
 }
 
 int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, const void* q, void* out, float* lse,
@@ -245,6 +288,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     if (p.c.status == nullptr) return SASQ_ERR_CUDA;
     const Plan pl = make_plan(cache, batch, num_q_heads, sms);
     const Layout l = layout_of(pl.blocks, pl.slot_rows, cache->head_dim);
+    if (pl.cluster == 0 && l.total > ws_bytes) return SASQ_ERR_WORKSPACE;      // most_workspace covers every plan
     p.q = static_cast<const uint16_t*>(q);
     p.out = static_cast<uint16_t*>(out);
     p.lse = lse;
@@ -260,7 +304,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.max_blocks = pl.blocks;
     p.item_rows = pl.rows;
     p.tile_bound = pl.tile_bound;
-    p.wait_limit = 1LL << 31;
+    p.wait_limit = debug_wait_limit();
     p.part_items = static_cast<PartItem*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + l.ml);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.o);

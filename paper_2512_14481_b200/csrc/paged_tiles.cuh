@@ -424,9 +424,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
             }
         }
-        // gave up: copies still in flight must land before the block's shared memory goes away
-        // (a tile with a tail to clear may never be announced; the limit is far above a copy's flight)
-        if (!ok && lane == 0) {
+        // Copies still in flight must land before the block's shared memory goes away: at once, unless a role gave up.
+        // (A tile with a tail to clear may then never be announced; the limit is far above a copy's flight.)
+        if (lane == 0) {
             for (int s = 0; s < Shape::kSlots; ++s) {
                 const long long t0 = clock64();
                 const uint32_t par = s < slot ? phase : (phase ^ 1u);
@@ -494,7 +494,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             if (!ok) break;
         }
-        if (!ok && lane == 0) {
+        if (lane == 0) {
             for (int x = 0; x < 2; ++x) {
                 const long long t0 = clock64();
                 while (filled[x] != 0 && !ptx::mbar_try_wait(&tail->q_full[x], (filled[x] & 1u) ^ 1u))
@@ -600,12 +600,11 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (!now.fold) free_slot(now.at + 1);
                 if (u.more && !u.fold) free_slot(u.at);
             }
-            if (!ok) {                    // MMAs still running must end before shared memory and TMEM go away
-                ptx::mma_commit(&tail->drain);
-                const long long t0 = clock64();
-                while (!ptx::mbar_try_wait(&tail->drain, 0))
-                    if (clock64() - t0 > (1LL << 24)) break;
-            }
+            // MMAs still running must end before shared memory and TMEM go away
+            ptx::mma_commit(&tail->drain);
+            const long long t0 = clock64();
+            while (!ptx::mbar_try_wait(&tail->drain, 0))
+                if (clock64() - t0 > (1LL << 24)) break;
         }
         __syncwarp();
     } else if (warp == kTailWarp) {

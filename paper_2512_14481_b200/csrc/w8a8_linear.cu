@@ -345,6 +345,9 @@ bool single_kernel_ready(bool bf) {
 }
 
 }  // namespace
+
+long long debug_wait_limit() { return g_wait_limit.load(std::memory_order_relaxed); }
+
 }  // namespace sasq
 
 extern "C" {

@@ -208,3 +208,37 @@ def test_pages_outside_the_cache_are_reported():
         bt.seq_lens[0] = 5000                                        # more keys than its table has room for
         attend(bt)
         assert P.sasq_device_status() == 7
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean(int8):
+    """The many-row kernel with a wait limit of zero cycles: it winds down in order, and the status word says so."""
+    bt = R.Batch([1500, 900], [200, 300], 8, 8, 128, 64, int8=int8, seed=7)
+    assert P.sasq_device_status() == 0
+    old = P.sasq_debug_set_wait_limit(0)
+    try:
+        attend(bt)
+        status = P.sasq_device_status()
+    finally:
+        P.sasq_debug_set_wait_limit(-1)
+    assert old == 1 << 31
+    assert status == 5
+    check(bt)
+
+
+def test_a_view_of_one_head_or_one_page():
+    """Dimensions of one entry have strides that say nothing."""
+    for heads, n_pages in ((1, 3), (2, 1)):
+        k = torch.randn((n_pages, 16, heads, 64), device="cuda").to(torch.bfloat16)
+        odd = torch.as_strided(k, k.shape, [s if n > 1 else 3 for s, n in zip(k.stride(), k.shape)])
+        i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+        q = torch.randn((20, heads, 64), device="cuda").to(torch.bfloat16)
+        outs = []
+        for cache_k in (k, odd):
+            cache = P.KVCache(cache_k, cache_k)
+            batch = P.PagedBatch(i32([[n_pages - 1]]), i32([16]), i32([0, 20]), 20, 20, 16)
+            out = torch.empty_like(q)
+            ws = torch.empty(P.sasq_paged_attention_workspace(cache, batch, heads), dtype=torch.uint8, device="cuda")
+            P.sasq_paged_attention(cache, batch, q, out, ws)
+            outs.append(out)
+        assert P.sasq_device_status() == 0 and torch.equal(outs[0], outs[1]) and (outs[0][:4] == 0).all()
