@@ -546,10 +546,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const uint32_t tile = u.at + (u.fold ? 2 * x : 0);
                 if (u.j == 0) {
                     ok = ok && tile_wait(&tail->q_full[x], q_phase >> x & 1u, tail, p);
+                    if (!ok) return;
                     q_phase ^= 1u << x;
+                    ptx::tc_fence_after_sync();
                 }
-                if (!arrived(tile)) return;
-                ptx::tc_fence_after_sync();
                 const uint64_t a = q_desc + (uint64_t)(x * (Shape::kQBytes >> 4));
                 const uint64_t b = k_desc + (uint64_t)(tile % Shape::kSlots * (Shape::kSlotBytes >> 4));
 #pragma unroll
@@ -567,7 +567,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (u.more) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
-                    if (u.j < u.n[x] && ok) qk(u, x);
+                    if (u.j < u.n[x] && arrived(u.at + (u.fold ? 2 * x : 0))) {
+                        ptx::tc_fence_after_sync();
+                        qk(u, x);
+                    }
                 if (!u.fold) free_slot(u.at);
             }
             while (u.more && ok) {
@@ -576,9 +579,15 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (++u.j == u.steps) enter(u);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    if (now.j < now.n[x] && ok) {
+                    // the tiles that this row tile needs (the second row tile's are the first's, unless folded), before P: then
+                    // nothing stands between PV and the next QK
+                    const bool k_next = u.more && u.j < u.n[x];
+                    if (now.j < now.n[x] && (x == 0 || now.fold || now.j >= now.n[0])) arrived(now.at + (now.fold ? 2 * x : 0) + 1);
+                    if (k_next && (x == 0 || u.fold || u.j >= u.n[0])) arrived(u.at + (u.fold ? 2 * x : 0));
+                    if (!ok) break;
+                    ptx::tc_fence_after_sync();
+                    if (now.j < now.n[x]) {
                         const uint32_t tile = now.at + (now.fold ? 2 * x : 0) + 1;
-                        if (!arrived(tile)) break;
                         // the first half's keys are multiplied while the softmax warps work on the second's
                         const uint64_t b = v_desc + (uint64_t)(tile % Shape::kSlots * (Shape::kSlotBytes >> 4));
 #pragma unroll
@@ -595,7 +604,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         ptx::mma_commit(&tail->o_full[x]);
                         if (now.fold) free_slot(tile);
                     }
-                    if (u.more && u.j < u.n[x] && ok) qk(u, x);
+                    if (k_next && ok) qk(u, x);
                 }
                 if (!now.fold) free_slot(now.at + 1);
                 if (u.more && !u.fold) free_slot(u.at);
