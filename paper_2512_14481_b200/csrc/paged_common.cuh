@@ -50,10 +50,12 @@ __device__ __forceinline__ Sequence load_sequence(const PagedParams& p, int b) {
 
 // ---------------------------------------------------------------------------------------------------------------------
 // Work of an attention call.  The rows of one KV head are (new token, query head of the group) pairs, token first; a
-// fixed number of consecutive rows of a sequence and KV head are an item, and an item's keys are walked in units of KT.  The units of
-// all items, laid end to end (sequence, KV head, item, key), are cut into equal stretches, one per thread block: every
-// block has the same number of units whatever the lengths are, a block walks whole items in the middle of its stretch
-// and at most two part items at its ends.  Part items leave (O, m, l) in the workspace, and a second launch joins them.
+// fixed number of consecutive rows of a sequence and KV head are an item, and an item's keys are walked in units of KT.
+// The units of all items, laid end to end (sequence, KV head, item, key), are cut into equal stretches, one per thread
+// block: every block has the same amount of work whatever the lengths are, a block walks whole items in the middle of its stretch
+// and at most two part items at its ends.  Beginning and ending an item costs as much as COST units, which stand before
+// the item's own in the row: without them a block that gets many short items is the tail.  Part items leave (O, m, l) in
+// the workspace, and a second launch joins them.
 // A split by whole items alone would leave most SMs idle for few long sequences, and a fixed number of splits per item
 // makes the longest sequence of a ragged batch the tail.
 // ---------------------------------------------------------------------------------------------------------------------
@@ -62,10 +64,10 @@ struct Item {
     Sequence s;
     int units;                // of the whole item
     int t0, t1;               // this block's units
-    long long first_unit;     // of the item, in the whole call
+    long long first;          // where the item begins in the row of all
 };
 
-template <int KT>
+template <int KT, int COST>
 struct Schedule {
     int rows;                 // of an item
     int group, causal, heads;
@@ -81,17 +83,19 @@ struct Schedule {
         const int n = (key_limit(s, i) + KT - 1) / KT;
         return n < 1 ? 1 : n;
     }
-    __device__ __forceinline__ long long head_units(const Sequence& s) const {
+    // length of an item, and of a sequence's items of one KV head, in the row
+    __device__ __forceinline__ int cost(const Sequence& s, int i) const { return units(s, i) + COST; }
+    __device__ __forceinline__ long long head_cost(const Sequence& s) const {
         const int n = tiles(s);
         if (n == 0) return 0;
-        if (!causal) return (long long)n * units(s, 0);
+        if (!causal) return (long long)n * cost(s, 0);
         long long sum = 0;
-        for (int i = 0; i < n; ++i) sum += units(s, i);
+        for (int i = 0; i < n; ++i) sum += cost(s, i);
         return sum;
     }
 };
 
-// First unit of block c when `total` units go to n blocks.
+// Where block c's stretch begins when a row of `total` units goes to n blocks.
 __device__ __forceinline__ long long block_begin(long long total, int c, int n) {
     if (total < (1 << 20)) return (unsigned)total * (unsigned)c / (unsigned)n;      // c, n < 4096
     return total * c / n;
@@ -104,7 +108,7 @@ __device__ __forceinline__ int block_of(long long total, long long x, int n) {
 
 // Where a block's stretch begins.
 struct Start {
-    long long total;          // units of the call
+    long long total;          // length of the row of all items
     long long begin, end;     // this block's
     long long offset;         // of `begin` in sequence b
     int b;                    // -1: nothing to do
@@ -113,13 +117,13 @@ struct Start {
 
 // A whole warp calls this; every lane gets the answer.  Each lane adds up a run of sequences: no barrier, and one round
 // trip to memory for up to 32 sequences.
-template <int KT>
-__device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule<KT>& sch, int max_blocks) {
+template <int KT, int COST>
+__device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule<KT, COST>& sch, int max_blocks) {
     const int lane = threadIdx.x & 31;
     const int per = (p.batch + 31) >> 5;
     const int b0 = lane * per, b1 = min(b0 + per, p.batch);
     long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += sch.head_units(load_sequence(p, b)) * sch.heads;
+    for (int b = b0; b < b1; ++b) mine += sch.head_cost(load_sequence(p, b)) * sch.heads;
     long long incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -141,7 +145,7 @@ __device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule
         const int owner = __ffs(hit) - 1;
         if (lane == owner) {
             for (int b = b0; b < b1; ++b) {
-                const long long n = per == 1 ? mine : sch.head_units(load_sequence(p, b)) * sch.heads;
+                const long long n = per == 1 ? mine : sch.head_cost(load_sequence(p, b)) * sch.heads;
                 if (st.begin < at + n) {
                     st.b = b;
                     st.offset = st.begin - at;
@@ -157,16 +161,25 @@ __device__ __forceinline__ Start find_start(const PagedParams& p, const Schedule
 }
 
 // Walks the items of a block's stretch; every thread keeps its own copy.
-template <int KT>
+template <int KT, int COST>
 struct Walk {
-    Schedule<KT> sch;
+    Schedule<KT, COST> sch;
     Item it;
-    long long at, end;
+    long long at, end;        // where the walk stands in the row, and the stretch's end
     int n_tiles;
     bool split;
 
+    // The item's units in [at, end), which begins `rest` behind the item's begin: false when there are none.
+    __device__ __forceinline__ bool cut(int rest) {
+        it.units = sch.units(it.s, it.i);
+        it.first = at - rest;
+        it.t0 = max(rest - COST, 0);
+        it.t1 = it.units;
+        if (split) it.t1 = max((int)min((long long)it.units, end - it.first - COST), 0);
+        return it.t1 > it.t0 && (split || rest == 0);
+    }
     // split == false: items are not cut, an item belongs to the block in whose stretch it begins
-    __device__ __forceinline__ bool begin(const PagedParams& p, const Schedule<KT>& s, const Start& st, bool may_split) {
+    __device__ __forceinline__ bool begin(const PagedParams& p, const Schedule<KT, COST>& s, const Start& st, bool may_split) {
         sch = s;
         split = may_split;
         at = st.begin;
@@ -175,41 +188,40 @@ struct Walk {
         it.b = st.b;
         it.s = load_sequence(p, it.b);
         n_tiles = sch.tiles(it.s);
-        const long long per_head = sch.head_units(it.s);
+        const long long per_head = sch.head_cost(it.s);
         it.h = st.offset < (1ll << 32) && per_head < (1ll << 32) ? (int)((unsigned)st.offset / (unsigned)per_head)
                                                                : (int)(st.offset / per_head);
         long long rest = st.offset - it.h * per_head;
         it.i = 0;
         for (;;) {
-            it.units = sch.units(it.s, it.i);
-            if (rest < it.units) break;
-            rest -= it.units;
+            const int n = sch.cost(it.s, it.i);
+            if (rest < n) break;
+            rest -= n;
             ++it.i;
         }
-        it.first_unit = at - rest;
-        it.t0 = (int)rest;
-        it.t1 = split ? (int)min((long long)it.units, rest + (end - at)) : it.units;
-        return (split || rest == 0) ? true : next(p);
+        return cut((int)rest) || next(p);
     }
     __device__ __forceinline__ bool next(const PagedParams& p) {
-        at += it.t1 - it.t0;
-        if (at >= end) return false;
-        if (++it.i == n_tiles) {
-            it.i = 0;
-            if (++it.h == sch.heads) {
-                it.h = 0;
-                do {
-                    if (++it.b >= p.batch) return false;      // cannot happen while at < end
-                    it.s = load_sequence(p, it.b);
-                    n_tiles = sch.tiles(it.s);
-                } while (n_tiles == 0);
+        do {
+            at = it.first + it.units + COST;
+            if (at >= end) return false;
+            if (++it.i == n_tiles) {
+                it.i = 0;
+                if (++it.h == sch.heads) {
+                    it.h = 0;
+                    do {
+                        if (++it.b >= p.batch) return false;  // cannot happen while at < end
+                        it.s = load_sequence(p, it.b);
+                        n_tiles = sch.tiles(it.s);
+                    } while (n_tiles == 0);
+                }
             }
-        }
-        it.units = sch.units(it.s, it.i);
-        it.first_unit = at;
-        it.t0 = 0;
-        it.t1 = split ? (int)min((long long)it.units, end - at) : it.units;
+        } while (!cut(0));
         return true;
+    }
+    // the block that has the item's last unit
+    __device__ __forceinline__ int last_block(const Start& st) const {
+        return block_of(st.total, it.first + COST + it.units - 1, st.blocks);
     }
 };
 

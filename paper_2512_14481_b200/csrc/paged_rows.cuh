@@ -28,6 +28,9 @@ namespace {
 
 constexpr int kRowsUnit = 64;             // keys of a unit
 constexpr int kClusterBlocks = 8;
+// units that beginning and ending an item costs (64 ragged sequences of 30 to 4500 keys, 32/8 heads: 112.4 us with 0,
+// 101.9 with 2, 103.8 with 4, 107.0 with 6)
+constexpr int kRowsItemCost = 2;
 constexpr float kRescaleAt = 8.0f;        // a row's reference moves once a logit passes it by this many powers of two
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool bf) {
@@ -107,9 +110,9 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
     pdl_launch_dependents();
     pdl_wait();
-    const Schedule<kRowsUnit> sch{R, p.group, p.causal, p.c.kv_heads};
+    const Schedule<kRowsUnit, kRowsItemCost> sch{R, p.group, p.causal, p.c.kv_heads};
     const int rank = blockIdx.x % kClusterBlocks;             // CLUSTER: of the block in its cluster
-    Walk<kRowsUnit> walk;
+    Walk<kRowsUnit, kRowsItemCost> walk;
     Start st;
     bool more;
     if constexpr (CLUSTER) {
@@ -122,7 +125,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         walk.n_tiles = sch.tiles(walk.it.s);
         more = walk.it.i < walk.n_tiles;
     } else {
-        st = find_start<kRowsUnit>(p.c, sch, p.max_blocks);
+        st = find_start(p.c, sch, p.max_blocks);
         if (tid == 0) p.part_items[blockIdx.x].last = -1;
         more = walk.begin(p.c, sch, st, p.split != 0);
     }
@@ -478,7 +481,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         }
         if (!whole && it.t0 == 0 && tid == 0) {
             PartItem pi;
-            pi.last = block_of(st.total, it.first_unit + it.units - 1, st.blocks);
+            pi.last = walk.last_block(st);
             pi.h = it.h;
             pi.first_row = first_row;
             pi.rows = rows;

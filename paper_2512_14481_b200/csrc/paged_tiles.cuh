@@ -148,8 +148,11 @@ __device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, TileTa
     return true;
 }
 
-using TileSchedule = Schedule<kTileKeys>;
-using TileWalk = Walk<kTileKeys>;
+// units that beginning and ending an item costs (12 sequences of 1 to 300 new tokens over up to 2500 keys, 40 heads: 159.7 us
+// with 0, 128.4 with 1, 124.7 with 2, 125.7 with 4, 130.0 with 6)
+constexpr int kTileItemCost = 2;
+using TileSchedule = Schedule<kTileKeys, kTileItemCost>;
+using TileWalk = Walk<kTileKeys, kTileItemCost>;
 
 // end of the units of an item, in this block, that row tile x takes part in (it.t0 or less: none)
 __device__ __forceinline__ int tile_end(const TileSchedule& sch, const Item& it, int x) {
@@ -440,7 +443,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---------------- the block's items, for everyone, and their Q ----------------
         uint32_t filled[2] = {0, 0};                            // times that each row tile's queries were asked for
         const int tokens = 128 / p.group;
-        const Start st = find_start<kTileKeys>(p.c, sch, p.max_blocks);
+        const Start st = find_start(p.c, sch, p.max_blocks);
         TileWalk walk;
         int n = 0;
         for (bool more = walk.begin(p.c, sch, st, p.split != 0);; more = walk.next(p.c), ++n) {
@@ -470,7 +473,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     it.end[0] = it.begin[1];
                 }
                 it.whole = w.t0 == 0 && w.t1 == w.units;
-                it.last = block_of(st.total, w.first_unit + w.units - 1, st.blocks);
+                it.last = walk.last_block(st);
             }
             if (lane == 0) {
                 tail->items[at] = it;
