@@ -63,7 +63,7 @@ Plan rows_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, in
     const bool int8 = c->kind == SASQ_KV_INT8, d128 = c->head_dim == 128;
     pl.nb = rows <= 8 ? 1 : 2;
     pl.rows = pl.slot_rows = 8 * pl.nb;
-    pl.unit = kRowsUnit;
+    pl.unit = pl.nb == 1 ? (int8 ? kRowsUnit<1, true> : kRowsUnit<1, false>) : kRowsUnit<2, false>;
     pl.tile_bound = rows < 1 ? 1 : ceil_div(rows, pl.rows);
     const int per_sm = pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
                                           : (int8 ? kRowsBlocksPerSm<64, 1, true> : kRowsBlocksPerSm<64, 1, false>))

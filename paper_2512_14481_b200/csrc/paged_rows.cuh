@@ -26,7 +26,12 @@ struct AttendParams {
 
 namespace {
 
-constexpr int kRowsUnit = 64;             // keys of a unit
+// Blocks of 16 keys of a warp's step: with 8 rows as many bytes are under way whatever the cache holds (16 rows' sums leave
+// no registers for that), and keys of a unit: a step of four warps.
+template <int NB, bool INT8>
+constexpr int kRowsSub = INT8 && NB == 1 ? 2 : 1;
+template <int NB, bool INT8>
+constexpr int kRowsUnit = 64 * kRowsSub<NB, INT8>;
 constexpr int kClusterBlocks = 8;
 // units that beginning and ending an item costs (64 ragged sequences of 30 to 4500 keys, 32/8 heads: 112.4 us with 0,
 // 101.9 with 2, 103.8 with 4, 107.0 with 6)
@@ -80,7 +85,7 @@ __device__ __forceinline__ uint2 ldg_stream8(const void* p) {
 
 // blocks that an SM holds: as many as the registers of the fragments leave room for without spilling
 template <int D, int NB, bool INT8>
-constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : (D == 128 && !INT8) ? 3 : 4;
+constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
 
 // Both products are taken transposed, keys (then dimensions) on the 16-row side of m16n8k16 and query rows on its
 // 8-column side, so that one query row wastes 7/8 of the instruction and not 15/16, and neither K nor V passes through
@@ -98,7 +103,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
     // both products are f16.  A bf16 query row is brought into f16's range by a power of two; elements below 2^-14 of the
     // row's largest then lose bits that are worth less than 2^-25 of it.
     constexpr bool PBF = BF && !INT8;
-    constexpr int kStride = 16 * WARPS;                     // keys from a warp's step to its next
+    constexpr int SUB = kRowsSub<NB, INT8>, kUnit = kRowsUnit<NB, INT8>;
+    constexpr int kStride = 16 * SUB * WARPS;               // keys from a warp's step to its next
     constexpr int kWords = INT8 ? D / 64 : D / 32;          // 16-byte words of a key that a lane takes
     constexpr int kSteps = D / 16;                          // k16 steps of S, and 16-row blocks of O
     constexpr int VW = D / 8 * (INT8 ? 1 : 2) / 4;          // 32-bit words of a V row that a lane takes: D / 8 elements
@@ -110,9 +116,9 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
     pdl_launch_dependents();
     pdl_wait();
-    const Schedule<kRowsUnit, kRowsItemCost> sch{R, p.group, p.causal, p.c.kv_heads};
+    const Schedule<kUnit, kRowsItemCost> sch{R, p.group, p.causal, p.c.kv_heads};
     const int rank = blockIdx.x % kClusterBlocks;             // CLUSTER: of the block in its cluster
-    Walk<kRowsUnit, kRowsItemCost> walk;
+    Walk<kUnit, kRowsItemCost> walk;
     Start st;
     bool more;
     if constexpr (CLUSTER) {
@@ -213,11 +219,12 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         const char* kbase = static_cast<const char*>(p.c.k) + it.h * p.c.head_stride * elem;
         const char* vbase = static_cast<const char*>(p.c.v) + it.h * p.c.head_stride * elem;
         const int page_mask = (1 << p.c.page_shift) - 1;
-        const int last_key = min(it.t1 * kRowsUnit, limit);
-        int key = it.t0 * kRowsUnit + warp * 16;             // of this warp's step
+        const int last_key = min(it.t1 * kUnit, limit);
+        int key = it.t0 * kUnit + warp * 16 * SUB;           // of this warp's step
 
-        // byte offset of key `at` of the sequence, or -1 when its page lies outside the cache
+        // byte offset of key `at` of the sequence, or -1 when there is none or its page lies outside the cache
         auto place = [&](int at) -> long long {
+            if (at >= last_key) return -1;
             const int page = __ldg(table + (at >> p.c.page_shift));
             if (page < 0 || page >= p.c.num_pages) {
                 atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
@@ -225,8 +232,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
             return (page * p.c.page_stride + (at & page_mask) * p.c.token_stride) * elem;
         };
-        uint4 kw[2][kWords];                                  // keys g and g + 8
-        auto load_k = [&](int at, long long off) {
+        uint4 kws[SUB][2][kWords];                            // keys g and g + 8
+        auto load_k = [&](int at, long long off, uint4 (&kw)[2][kWords]) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const bool in = off >= 0 && at + g + 8 * r < last_key;
@@ -236,8 +243,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     kw[r][w] = in ? ldg_stream16(row + 16 * (j + 4 * w)) : make_uint4(0, 0, 0, 0);
             }
         };
-        uint32_t vw[4][VW];                                   // keys 2j, 2j + 1, 2j + 8, 2j + 9
-        auto load_v = [&](int at, long long off) {
+        uint32_t vws[SUB][4][VW];                             // keys 2j, 2j + 1, 2j + 8, 2j + 9
+        auto load_v = [&](int at, long long off, uint32_t (&vw)[4][VW]) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int kk = 2 * j + (r & 1) + 8 * (r >> 1);
@@ -260,70 +267,79 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
         };
 
-        long long off = -1, off_next = -1;
-        if (key < last_key) {
-            off = place(key);
-            load_k(key, off);
-            load_v(key, off);
-            if (key + kStride < last_key) off_next = place(key + kStride);
+        long long off[SUB], off_next[SUB];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            off[u] = place(key + 16 * u);
+            load_k(key + 16 * u, off[u], kws[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            load_v(key + 16 * u, off[u], vws[u]);
+            off_next[u] = place(key + kStride + 16 * u);
         }
         while (key < last_key) {
-            // S^T of 16 keys: rows are keys, columns query rows
-            float s[NB][4];
+            // S^T of the step's keys: rows are keys, columns query rows
+            float s[SUB][NB][4];
+            const int key_now = key, key_next = key + kStride;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+            for (int u = 0; u < SUB; ++u) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[nb][e] = 0.0f;
+                for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int w = 0; w < kWords; ++w) {
-                const uint32_t k0[4] = {kw[0][w].x, kw[0][w].y, kw[0][w].z, kw[0][w].w};
-                const uint32_t k1[4] = {kw[1][w].x, kw[1][w].y, kw[1][w].z, kw[1][w].w};
-                if constexpr (INT8) {
+                    for (int e = 0; e < 4; ++e) s[u][nb][e] = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t a[4] = {codes_to_pair<false, 0>(k0[e]), codes_to_pair<false, 0>(k1[e]),
-                                               codes_to_pair<false, 1>(k0[e]), codes_to_pair<false, 1>(k1[e])};
+                for (int w = 0; w < kWords; ++w) {
+                    const uint32_t k0[4] = {kws[u][0][w].x, kws[u][0][w].y, kws[u][0][w].z, kws[u][0][w].w};
+                    const uint32_t k1[4] = {kws[u][1][w].x, kws[u][1][w].y, kws[u][1][w].z, kws[u][1][w].w};
+                    if constexpr (INT8) {
 #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb)
-                            mma_16816(s[nb], a, qf[nb][8 * w + 2 * e], qf[nb][8 * w + 2 * e + 1], PBF);
-                    }
-                } else {
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t a[4] = {codes_to_pair<false, 0>(k0[e]), codes_to_pair<false, 0>(k1[e]),
+                                                   codes_to_pair<false, 1>(k0[e]), codes_to_pair<false, 1>(k1[e])};
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t a[4] = {k0[2 * e], k1[2 * e], k0[2 * e + 1], k1[2 * e + 1]};
+                            for (int nb = 0; nb < NB; ++nb)
+                                mma_16816(s[u][nb], a, qf[nb][8 * w + 2 * e], qf[nb][8 * w + 2 * e + 1], PBF);
+                        }
+                    } else {
 #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb)
-                            mma_16816(s[nb], a, qf[nb][4 * w + 2 * e], qf[nb][4 * w + 2 * e + 1], PBF);
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t a[4] = {k0[2 * e], k1[2 * e], k0[2 * e + 1], k1[2 * e + 1]};
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb)
+                                mma_16816(s[u][nb], a, qf[nb][4 * w + 2 * e], qf[nb][4 * w + 2 * e + 1], PBF);
+                        }
                     }
                 }
-            }
-            const int key_now = key;
-            const int key_next = key + kStride;
-            const long long off_now = off_next;
-            if (key_next < last_key) {
-                load_k(key_next, off_now);                    // the next step's keys travel under this step's softmax
-                if (key_next + kStride < last_key) off_next = place(key_next + kStride);
+                // the next step's keys travel under this step's softmax
+                off[u] = off_next[u];
+                load_k(key_next + 16 * u, off[u], kws[u]);
+                off_next[u] = place(key_next + kStride + 16 * u);
             }
 
             // running maximum and sum in powers of two; a row's reference m only moves when a logit passes it by
             // kRescaleAt, so that most steps need neither the shuffles nor the rescaling (P stays below 2^kRescaleAt)
             bool moves = false;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int at = key_now + g + 8 * (e >> 1);
-                    s[nb][e] = at < row_limit[nb][e & 1] ? s[nb][e] * row_scale[nb][e & 1] : -INFINITY;
+                for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int at = key_now + 16 * u + g + 8 * (e >> 1);
+                        s[u][nb][e] = at < row_limit[nb][e & 1] ? s[u][nb][e] * row_scale[nb][e & 1] : -INFINITY;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) moves |= fmaxf(s[u][nb][e], s[u][nb][e + 2]) > m[nb][e] + kRescaleAt;
                 }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) moves |= fmaxf(s[nb][e], s[nb][e + 2]) > m[nb][e] + kRescaleAt;
-            }
             if (__any_sync(0xFFFFFFFFu, moves)) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float t = fmaxf(s[nb][e], s[nb][e + 2]);
+                        float t = fmaxf(s[0][nb][e], s[0][nb][e + 2]);
+#pragma unroll
+                        for (int u = 1; u < SUB; ++u) t = fmaxf(t, fmaxf(s[u][nb][e], s[u][nb][e + 2]));
                         t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 4));
                         t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 8));
                         t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 16));
@@ -338,46 +354,50 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                         }
                     }
             }
-            uint32_t pf[NB][2];
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                float pr[4];
+            for (int u = 0; u < SUB; ++u) {
+                uint32_t pf[NB][2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float ref = m[nb][e & 1] == -INFINITY ? 0.0f : m[nb][e & 1];
-                    pr[e] = exp2_approx(s[nb][e] - ref);
-                    l[nb][e & 1] += pr[e];
+                for (int nb = 0; nb < NB; ++nb) {
+                    float pr[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ref = m[nb][e & 1] == -INFINITY ? 0.0f : m[nb][e & 1];
+                        pr[e] = exp2_approx(s[u][nb][e] - ref);
+                        l[nb][e & 1] += pr[e];
+                    }
+                    pf[nb][0] = transpose_8x8(narrow2<PBF>(pr[0], pr[1]));
+                    pf[nb][1] = transpose_8x8(narrow2<PBF>(pr[2], pr[3]));
                 }
-                pf[nb][0] = transpose_8x8(narrow2<PBF>(pr[0], pr[1]));
-                pf[nb][1] = transpose_8x8(narrow2<PBF>(pr[2], pr[3]));
-            }
 
-            // O^T += V^T P^T: rows are dimensions, the contraction is over the 16 keys
-            if constexpr (INT8) {
+                // O^T += V^T P^T: rows are dimensions, the contraction is over 16 keys
+                const uint32_t (&vw)[4][VW] = vws[u];
+                if constexpr (INT8) {
 #pragma unroll
-                for (int w = 0; w < VW; ++w) {
-                    const uint32_t x0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), x1 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
-                    const uint32_t y0 = __byte_perm(vw[2][w], vw[3][w], 0x5140), y1 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
-                    const uint32_t a0[4] = {codes_to_pair<false, 0>(x0), codes_to_pair<false, 1>(x0), codes_to_pair<false, 0>(y0),
-                                            codes_to_pair<false, 1>(y0)};
-                    const uint32_t a1[4] = {codes_to_pair<false, 0>(x1), codes_to_pair<false, 1>(x1), codes_to_pair<false, 0>(y1),
-                                            codes_to_pair<false, 1>(y1)};
+                    for (int w = 0; w < VW; ++w) {
+                        const uint32_t x0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), x1 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
+                        const uint32_t y0 = __byte_perm(vw[2][w], vw[3][w], 0x5140), y1 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
+                        const uint32_t a0[4] = {codes_to_pair<false, 0>(x0), codes_to_pair<false, 1>(x0), codes_to_pair<false, 0>(y0),
+                                                codes_to_pair<false, 1>(y0)};
+                        const uint32_t a1[4] = {codes_to_pair<false, 0>(x1), codes_to_pair<false, 1>(x1), codes_to_pair<false, 0>(y1),
+                                                codes_to_pair<false, 1>(y1)};
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        mma_16816(o[2 * w][nb], a0, pf[nb][0], pf[nb][1], PBF);
-                        mma_16816(o[2 * w + 1][nb], a1, pf[nb][0], pf[nb][1], PBF);
+                        for (int nb = 0; nb < NB; ++nb) {
+                            mma_16816(o[2 * w][nb], a0, pf[nb][0], pf[nb][1], PBF);
+                            mma_16816(o[2 * w + 1][nb], a1, pf[nb][0], pf[nb][1], PBF);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) {
+                        const uint32_t a[4] = {__byte_perm(vw[0][w], vw[1][w], 0x5410), __byte_perm(vw[0][w], vw[1][w], 0x7632),
+                                               __byte_perm(vw[2][w], vw[3][w], 0x5410), __byte_perm(vw[2][w], vw[3][w], 0x7632)};
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) mma_16816(o[w][nb], a, pf[nb][0], pf[nb][1], PBF);
                     }
                 }
-            } else {
-#pragma unroll
-                for (int w = 0; w < VW; ++w) {
-                    const uint32_t a[4] = {__byte_perm(vw[0][w], vw[1][w], 0x5410), __byte_perm(vw[0][w], vw[1][w], 0x7632),
-                                           __byte_perm(vw[2][w], vw[3][w], 0x5410), __byte_perm(vw[2][w], vw[3][w], 0x7632)};
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mma_16816(o[w][nb], a, pf[nb][0], pf[nb][1], PBF);
-                }
+                load_v(key_next + 16 * u, off[u], vws[u]);
             }
-            if (key_next < last_key) load_v(key_next, off_now);
             key = key_next;
         }
 
