@@ -213,6 +213,19 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+// 16 codes of a key as 16-bit floats into row r of a swizzled tile: two chunks of 8, of which lanes with `turn` store the
+// second first.  V meets P in f16 whatever the queries' type is (five instructions for four codes, to bf16 eight).
+template <bool BF>
+__device__ __forceinline__ void store_codes(uint8_t* tile, int r, int chunk, int turn, const uint4& v) {
+    uint8_t* const row = tile + r * 128;
+    const uint2 lo = turn ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y);
+    const uint2 hi = turn ? make_uint2(v.x, v.y) : make_uint2(v.z, v.w);
+    *reinterpret_cast<uint4*>(row + (((chunk + turn) ^ (r & 7)) << 4)) =
+        make_uint4(codes_to_pair<BF, 0>(lo.x), codes_to_pair<BF, 1>(lo.x), codes_to_pair<BF, 0>(lo.y), codes_to_pair<BF, 1>(lo.y));
+    *reinterpret_cast<uint4*>(row + (((chunk + (turn ^ 1)) ^ (r & 7)) << 4)) =
+        make_uint4(codes_to_pair<BF, 0>(hi.x), codes_to_pair<BF, 1>(hi.x), codes_to_pair<BF, 0>(hi.y), codes_to_pair<BF, 1>(hi.y));
+}
+
 // The warps that fill the ring from an int8 cache (`me` of kConvertThreads): K and V of each unit in turn, in the layout
 // that the 16-bit copies leave: keys along the rows, 128-byte swizzle.  Keys behind the sequence's last are zeros.
 template <int D, bool BF>
@@ -264,20 +277,15 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
     };
     int slot = 0;
     uint32_t phase = 0;
-    auto store = [&](const uint4 (&v)[kSteps]) {
+    auto store = [&](const uint4 (&v)[kSteps], bool values) {
         ok = ok && tile_wait(&tail->kv_empty[slot], phase ^ 1u, tail, p);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) return;
+        uint8_t* const tile = column + (size_t)slot * Shape::kSlotBytes;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const int r = i * kKeys + first;
-            uint8_t* row = column + (size_t)slot * Shape::kSlotBytes + r * 128;
-            const uint4 lo = make_uint4(codes_to_pair<BF, 0>(v[i].x), codes_to_pair<BF, 1>(v[i].x), codes_to_pair<BF, 0>(v[i].y),
-                                        codes_to_pair<BF, 1>(v[i].y));
-            const uint4 hi = make_uint4(codes_to_pair<BF, 0>(v[i].z), codes_to_pair<BF, 1>(v[i].z), codes_to_pair<BF, 0>(v[i].w),
-                                        codes_to_pair<BF, 1>(v[i].w));
-            *reinterpret_cast<uint4*>(row + (((chunk + turn) ^ (r & 7)) << 4)) = turn ? hi : lo;
-            *reinterpret_cast<uint4*>(row + (((chunk + (turn ^ 1)) ^ (r & 7)) << 4)) = turn ? lo : hi;
+            if (values) store_codes<false>(tile, i * kKeys + first, chunk, turn, v[i]);
+            else store_codes<BF>(tile, i * kKeys + first, chunk, turn, v[i]);
         }
         ptx::fence_proxy_async_smem();
         ptx::mbar_arrive(&tail->kv_full[slot]);
@@ -295,9 +303,9 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
         load(p.c.v, entry, v);
         next();
         entry = look_up();
-        store(k);
+        store(k, false);
         if (more) load(p.c.k, entry, k);
-        if (ok) store(v);
+        if (ok) store(v, true);
     }
 }
 
@@ -510,7 +518,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---------------- MMAs, all by one lane (which lets the descriptors live in uniform registers) ----------------
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, BF);
-            constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF) | ptx::kIdescBTransposed;
+            constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF && !INT8) | ptx::kIdescBTransposed;
             uint32_t q_phase = 0, p_phase = 0;                        // a bit per row tile
             const uint64_t q_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(q_smem));
             const uint64_t k_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(ring));
@@ -763,7 +771,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                                       scale2, ref2));
                         const float p0 = exp2_approx(z.x), p1 = exp2_approx(z.y);
                         sum2 = add2(sum2, pack2(p0, p1));
-                        pk[e] = narrow2<BF>(p0, p1);
+                        pk[e] = narrow2<BF && !INT8>(p0, p1);
                     }
                     ptx::tmem_st_32x32(s_addr + part * 32, pk);
                     ptx::tmem_st_wait();
