@@ -416,7 +416,7 @@ SASQ_API size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, con
  *   s_j = softmax_scale * <q, k_j>,   lse = log sum_j exp(s_j),   out = sum_j exp(s_j - lse) v_j
  * (for an int8 cache k_j, v_j are code * factor).  A token that sees no key gets out = +0 and lse = -inf.  What the
  * cache holds past a sequence's keys (NaN included) does not matter.  Logits, maxima, sums and accumulators are fp32;
- * the probabilities are rounded once to `dt` as operands of the second product.  Bit-identical from run to run.
+ * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 cache to f16.  Bit-identical from run to run.
  * q: as for sasq_rope_kv_append (already rotated); out: [total_q, num_q_heads, head_dim] of `dt`, rows at out_stride;
  * must not alias q.  lse: [total_q, num_q_heads] fp32 (natural logarithm) or NULL.  head_dim: 64 or 128.
  * workspace: >= sasq_paged_attention_workspace() bytes, 16-byte aligned, contents need no initialisation; calls that
