@@ -416,12 +416,14 @@ SASQ_API size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, con
  *   s_j = softmax_scale * <q, k_j>,   lse = log sum_j exp(s_j),   out = sum_j exp(s_j - lse) v_j
  * (for an int8 cache k_j, v_j are code * factor).  A token that sees no key gets out = +0 and lse = -inf.  What the
  * cache holds past a sequence's keys (NaN included) does not matter.  Logits, maxima, sums and accumulators are fp32;
- * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 cache to f16.  Bit-identical from run to run.
+ * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 cache to f16.
+ * Bit-identical from run to run.  Infinities or NaN among a sequence's OWN values are outside the contract: they may
+ * reach any row of that sequence, rows that do not see them included.
  * q: as for sasq_rope_kv_append (already rotated); out: [total_q, num_q_heads, head_dim] of `dt`, rows at out_stride;
  * must not alias q.  lse: [total_q, num_q_heads] fp32 (natural logarithm) or NULL.  head_dim: 64 or 128.
  * workspace: >= sasq_paged_attention_workspace() bytes, 16-byte aligned, contents need no initialisation; calls that
  * share one must be ordered on the stream.  A page or length outside its range sets SASQ_ERR_BAD_INDEX (out
- * unspecified for that sequence). */
+ * unspecified for that sequence), a factor that Eq. 1 cannot use SASQ_ERR_BAD_SCALE (for that head). */
 SASQ_API int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, const void* q,
                                   void* out, float* lse, int64_t q_stride, int64_t out_stride, int num_q_heads,
                                   float softmax_scale, int causal, int dt, void* workspace, size_t ws_bytes,

@@ -242,3 +242,36 @@ def test_a_view_of_one_head_or_one_page():
             P.sasq_paged_attention(cache, batch, q, out, ws)
             outs.append(out)
         assert P.sasq_device_status() == 0 and torch.equal(outs[0], outs[1]) and (outs[0][:4] == 0).all()
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_bad_factors_are_reported(new):
+    for which in ("k_scale", "v_scale"):
+        for wrong in (0.0, float("nan"), float("inf")):
+            bt = R.Batch([200], [new], 4, 4, 64, 16, int8=True, seed=3)
+            getattr(bt, which)[2] = wrong
+            attend(bt)
+            assert P.sasq_device_status() == 4
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_negative_factors(new):
+    bt = R.Batch([300, 200], [new] * 2, 4, 2, 128, 32, int8=True, seed=4)
+    bt.k_scale[0] *= -1
+    bt.v_scale[1] *= -1
+    check(bt)
+
+
+@pytest.mark.parametrize("new", [2, 150])
+def test_loud_keys_out_of_sight(new):
+    """Keys that a row must not see have logits far above all others (and are NaN for K): only the mask keeps them out."""
+    bt = R.Batch([new + 40], [new], 4, 4, 128, 64, seed=5, tokens_first=True)
+    last = new + 39
+    page, row = int(bt.table[0, last // 64]), last % 64
+    bt.k_host[page, row] = float("nan")
+    bt.k.copy_(bt.k_host)
+    out, lse = attend(bt)
+    short = R.Batch([new + 40], [new], 4, 4, 128, 64, seed=5, tokens_first=True)
+    want, want_lse, tol, lse_tol = R.attention(short, 128 ** -0.5, True)
+    assert (np.abs(out.float().cpu().double().numpy() - want) <= tol)[:-1].all()
+    assert (np.abs(lse.cpu().double().numpy() - want_lse) <= lse_tol)[:-1].all()
