@@ -71,11 +71,11 @@ namespace {
 // An item is two row tiles, each the tokens whose heads fit 128 MMA rows: 128 / group tokens, so that a row tile is one
 // box of q (of a group of five heads 125 rows are used).
 constexpr int kTileKeys = 128;            // keys of a unit
-// Warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q; 11: V's tails.  With an int8 cache warps
-// 12-19 fetch and convert K and V, and 9 and 11 are idle.
-// readers of the item queue: the softmax warps, the MMA lane, and whoever fetches K and V
+// Readers of the item queue: the softmax warps, the MMA lane, and whoever fetches K and V
 template <bool INT8>
 constexpr int kReaders = 8 + 1 + (INT8 ? 8 : 2);
+// Warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q and the items; 11: V's tails.  With an int8 cache warps
+// 12-19 fetch and convert K and V, and 9 and 11 are idle.
 template <bool INT8>
 constexpr int kTileThreads = INT8 ? 640 : 384;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11, kConvertWarp = 12;

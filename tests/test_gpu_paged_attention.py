@@ -275,3 +275,27 @@ def test_loud_keys_out_of_sight(new):
     want, want_lse, tol, lse_tol = R.attention(short, 128 ** -0.5, True)
     assert (np.abs(out.float().cpu().double().numpy() - want) <= tol)[:-1].all()
     assert (np.abs(lse.cpu().double().numpy() - want_lse) <= lse_tol)[:-1].all()
+
+
+@pytest.mark.parametrize("new", [1, 3])
+def test_more_heads_per_key_head_than_a_row_tile(new):
+    for int8 in (False, True):
+        check(R.Batch([90, 400], [new] * 2, 130, 1, 64, 16, int8=int8, seed=2))
+
+
+@pytest.mark.parametrize("heads", [24, 48, 100, 128])
+def test_groups_that_do_not_divide_a_row_tile(heads):
+    check(R.Batch([500, 260], [40, 33], heads, 1, 64, 32, torch.float16, seed=heads))
+
+
+def test_a_cache_without_pages():
+    k = torch.empty((0, 16, 2, 64), dtype=torch.bfloat16, device="cuda")
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    for new in (1, 30):
+        cache = P.KVCache(k, k)
+        batch = P.PagedBatch(torch.zeros((2, 1), dtype=torch.int32, device="cuda"), i32([0, 0]), i32([0, new, 2 * new]), 2 * new, new, 0)
+        q = torch.randn((2 * new, 4, 64), device="cuda").to(torch.bfloat16)
+        out, lse = torch.full_like(q, 7.0), torch.zeros((2 * new, 4), device="cuda")
+        ws = torch.empty(P.sasq_paged_attention_workspace(cache, batch, 4), dtype=torch.uint8, device="cuda")
+        P.sasq_paged_attention(cache, batch, q, out, ws, lse=lse)
+        assert P.sasq_device_status() == 0 and (out == 0).all() and torch.isneginf(lse).all()
