@@ -78,8 +78,10 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
     if (b >= p.c.batch || idle) return;          // padding behind the last sequence
     const Sequence s = load_sequence(p.c, b);
     if (t < s.first || t >= s.first + s.new_len) return;
-    const int pos = s.len - s.new_len + (t - s.first);
-    bool there = pos >= 0;
+    // from the length as given: a token that the table has no room for is skipped, it does not move to another's place
+    const long long place = (long long)s.given_len - s.new_len + (t - s.first);
+    bool there = place >= 0 && place < (long long)p.c.max_pages << p.c.page_shift;      // (reported by load_sequence)
+    const int pos = (int)place;
     if (there && p.rot > 0 && pos >= p.max_positions) {
         atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
         there = false;

@@ -34,6 +34,7 @@ namespace {
 // A sequence's new tokens and keys as the device arrays give them, cut to what is safe to touch.
 struct Sequence {
     int first, new_len, len;
+    int given_len;              // seq_lens' own value: positions follow from it, not from the cut length
 };
 __device__ __forceinline__ Sequence load_sequence(const PagedParams& p, int b) {
     Sequence s;
@@ -45,6 +46,7 @@ __device__ __forceinline__ Sequence load_sequence(const PagedParams& p, int b) {
     s.first = q0;
     s.new_len = (q0 < 0 || q1 < q0 || q1 > p.total_q) ? 0 : q1 - q0;
     s.len = len < 0 ? 0 : (len > room ? (int)room : len);
+    s.given_len = len;
     return s;
 }
 
