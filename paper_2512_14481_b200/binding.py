@@ -764,6 +764,8 @@ class PagedBatch:
             raise TypeError("page_table must be an int32 CUDA tensor")
         if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be [batch, max_pages] with contiguous rows")
+        if page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]:
+            raise ValueError("the rows of page_table must not overlap (an expanded table needs a copy)")
         _dev(seq_lens, "seq_lens", torch.int32); _dev(q_starts, "q_starts", torch.int32)
         B, max_pages = page_table.shape
         if seq_lens.numel() != B or q_starts.numel() != B + 1:
@@ -771,7 +773,7 @@ class PagedBatch:
         self.page_table, self.seq_lens, self.q_starts = page_table, seq_lens, q_starts
         self.total_q = int(total_q)
         longest = 0x7FFFFFFF if max_seq_len is None else int(max_seq_len)
-        self.struct = KVBatchStruct(_ptr(page_table), _ptr(seq_lens), _ptr(q_starts), max(page_table.stride(0), max_pages),
+        self.struct = KVBatchStruct(_ptr(page_table), _ptr(seq_lens), _ptr(q_starts), page_table.stride(0) if B > 1 else max_pages,
                                     B, max_pages, self.total_q, self.total_q if max_q_len is None else int(max_q_len),
                                     longest, 0)
         self.ref = ctypes.byref(self.struct)
