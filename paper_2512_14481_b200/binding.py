@@ -719,6 +719,36 @@ def sasq_fakequant_fwd_bwd_static(x, grad_y, y, grad_x, grad_scale, scale, bits:
 # ---------------------------------------------------------------------------
 # paged key/value cache
 # ---------------------------------------------------------------------------
+_current_device = torch._C._cuda_getDevice
+
+
+def _elsewhere(device: int, t, name: str):
+    """Says why a tensor that does not lie on `device` is refused."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    raise ValueError(f"{name} lies on cuda:{t.get_device()}, the other tensors of the call on cuda:{device}")
+
+
+def _flat(t, name: str, device: int, dtype=None) -> None:
+    """As _dev, for a tensor that goes with others of `device`."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.get_device() != device:                       # a host tensor says -1
+        _elsewhere(device, t, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _wrong_device(cache, batch):
+    """Says why a call is refused whose handles do not lie on the current device, where the library launches."""
+    if batch.device != cache.device:
+        raise ValueError(f"the batch lies on cuda:{batch.device}, the cache on cuda:{cache.device}")
+    raise ValueError(f"the cache lies on cuda:{cache.device}, the current device is cuda:{_current_device()} (enter "
+                     f"torch.cuda.device({cache.device}))")
+
+
 class KVCache:
     """A paged cache, marshalled once (see LinearProblems).  k, v: [num_pages, page_size, num_kv_heads, head_dim] views
     of one stride pattern, last dimension contiguous (a pool stored heads first is passed as its .transpose(1, 2));
@@ -733,14 +763,15 @@ class KVCache:
                                  "dimension")
             if t.dtype not in (torch.int8, torch.float16, torch.bfloat16):
                 raise TypeError(f"{name} must be int8, float16 or bfloat16, got {t.dtype}")
-        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.get_device() != v.get_device():
             raise ValueError("k and v must share shape, strides, dtype and device")
         int8 = k.dtype == torch.int8
+        self.device = k.get_device()
         for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
             if int8 != (t is not None):
                 raise ValueError(f"{name} goes with an int8 cache, and only with it")
             if t is not None:
-                _dev(t, name, torch.float32)
+                _flat(t, name, self.device, torch.float32)
                 if t.numel() != k.shape[2]:
                     raise ValueError(f"{name} must hold one factor per KV head")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
@@ -766,7 +797,8 @@ class PagedBatch:
             raise ValueError("page_table must be [batch, max_pages] with contiguous rows")
         if page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]:
             raise ValueError("the rows of page_table must not overlap (an expanded table needs a copy)")
-        _dev(seq_lens, "seq_lens", torch.int32); _dev(q_starts, "q_starts", torch.int32)
+        self.device = page_table.get_device()
+        _flat(seq_lens, "seq_lens", self.device, torch.int32); _flat(q_starts, "q_starts", self.device, torch.int32)
         B, max_pages = page_table.shape
         if seq_lens.numel() != B or q_starts.numel() != B + 1:
             raise ValueError("seq_lens must be [batch] and q_starts [batch + 1]")
@@ -779,10 +811,12 @@ class PagedBatch:
         self.ref = ctypes.byref(self.struct)
 
 
-def _heads(t, name: str, dtype, total: int, heads: int | None, dim: int):
+def _heads(t, name: str, dtype, total: int, heads: int | None, dim: int, device: int):
     """[total, heads, dim] with each row's heads contiguous; returns (heads, row stride)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a CUDA tensor")
+    if t.get_device() != device:
+        _elsewhere(device, t, name)
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     shape, stride = t.shape, t.stride()
@@ -790,13 +824,13 @@ def _heads(t, name: str, dtype, total: int, heads: int | None, dim: int):
         raise ValueError(f"{name} must be [{total}, {'heads' if heads is None else heads}, {dim}]")
     if stride[2] != 1 or (shape[1] > 1 and stride[1] != dim):
         raise ValueError(f"the heads of a row of {name} must be contiguous")
-    return shape[1], (stride[0] if total > 1 else max(stride[0], shape[1] * dim))
+    return shape[1], (stride[0] if total > 1 else shape[1] * dim)      # one row may have any stride in torch
 
 
-def _stream_of(t, stream) -> int:
+def _stream_of(device: int, stream) -> int:
     """As _stream, for calls whose tensors are known to lie on one device: the raw handle of its current stream."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(t.get_device())
+        return torch._C._cuda_getCurrentRawStream(device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -805,26 +839,31 @@ def sasq_rope_kv_append(cache: KVCache, batch: PagedBatch, q, k, v, q_out, cos_s
     """Appends k, v [total_q, num_kv_heads, head_dim] to the cache with the rotation of cos_sin [max_positions, rot_dim]
     fp32 (None: no rotation) applied to k, and to q [total_q, num_q_heads, head_dim] -> q_out (both None: skip)."""
     T, K, D = batch.total_q, cache.num_kv_heads, cache.head_dim
+    device = cache.device
+    if batch.device != device or _current_device() != device:
+        _wrong_device(cache, batch)
     dt = k.dtype
     if cache.dtype is not torch.int8 and cache.dtype != dt:
         raise TypeError(f"k must have the cache's dtype {cache.dtype}")
-    _, ks = _heads(k, "k", dt, T, K, D)
-    _, vs = _heads(v, "v", dt, T, K, D)
+    _, ks = _heads(k, "k", dt, T, K, D, device)
+    _, vs = _heads(v, "v", dt, T, K, D, device)
     H = qs = qos = 0
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     if q is not None:
-        H, qs = _heads(q, "q", dt, T, None, D)
-        _, qos = _heads(q_out, "q_out", dt, T, H, D)
+        H, qs = _heads(q, "q", dt, T, None, D, device)
+        _, qos = _heads(q_out, "q_out", dt, T, H, D, device)
     positions = rot = 0
     if cos_sin is not None:
-        _dev(cos_sin, "cos_sin", torch.float32)
+        _flat(cos_sin, "cos_sin", device, torch.float32)
         if cos_sin.dim() != 2:
             raise ValueError("cos_sin must be [max_positions, rot_dim]")
         positions, rot = cos_sin.shape
-    _check((_lib or load_library()).sasq_rope_kv_append(
+    status = (_lib or load_library()).sasq_rope_kv_append(
         cache.ref, batch.ref, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_out), qs, ks, vs, qos, H, _ptr(cos_sin), positions,
-        rot, 1 if interleaved else 0, _dt(k), _stream_of(k, stream)), "sasq_rope_kv_append")
+        rot, 1 if interleaved else 0, _dt(k), _stream_of(device, stream))
+    if status != 0 or _DEBUG_STATUS:
+        _check(status, "sasq_rope_kv_append")
 
 
 def sasq_paged_attention_workspace(cache: KVCache, batch: PagedBatch, num_q_heads: int) -> int:
@@ -836,16 +875,21 @@ def sasq_paged_attention(cache: KVCache, batch: PagedBatch, q, out, workspace, l
     """Attention of q [total_q, num_q_heads, head_dim] over the cache -> out of the same shape, lse [total_q, num_q_heads]
     fp32 or None; scale defaults to head_dim ** -0.5."""
     T, D = batch.total_q, cache.head_dim
+    device = cache.device
+    if batch.device != device or _current_device() != device:
+        _wrong_device(cache, batch)
     dt = q.dtype
     if cache.dtype is not torch.int8 and cache.dtype != dt:
         raise TypeError(f"q must have the cache's dtype {cache.dtype}")
-    H, qs = _heads(q, "q", dt, T, None, D)
-    _, os_ = _heads(out, "out", dt, T, H, D)
+    H, qs = _heads(q, "q", dt, T, None, D, device)
+    _, os_ = _heads(out, "out", dt, T, H, D, device)
     if lse is not None:
-        _dev(lse, "lse", torch.float32)
+        _flat(lse, "lse", device, torch.float32)
         if lse.shape != (T, H):
             raise ValueError("lse must be [total_q, num_q_heads]")
-    _dev(workspace, "workspace")
-    _check((_lib or load_library()).sasq_paged_attention(
+    _flat(workspace, "workspace", device)
+    status = (_lib or load_library()).sasq_paged_attention(
         cache.ref, batch.ref, q.data_ptr(), out.data_ptr(), _ptr(lse), qs, os_, H, D ** -0.5 if scale is None else scale,
-        1 if causal else 0, _dt(q), workspace.data_ptr(), workspace.nbytes, _stream_of(q, stream)), "sasq_paged_attention")
+        1 if causal else 0, _dt(q), workspace.data_ptr(), workspace.nbytes, _stream_of(device, stream))
+    if status != 0 or _DEBUG_STATUS:
+        _check(status, "sasq_paged_attention")
