@@ -13,15 +13,15 @@ SASQ_DEFINE_STATUS_WORD(g_paged_status)
 int paged_status_read_and_clear(cudaStream_t st) { return g_paged_status_read_and_clear(st); }
 
 int* paged_status_ptr() {
-    static int* cache[64] = {nullptr};
+    static std::atomic<int*> cache[64];      // any host thread may make the first call on a device
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-    if (cache[dev] == nullptr) {
-        int* p = nullptr;
+    int* p = cache[dev].load(std::memory_order_acquire);
+    if (p == nullptr) {
         if (cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_paged_status) != cudaSuccess) return nullptr;
-        cache[dev] = p;
+        cache[dev].store(p, std::memory_order_release);
     }
-    return cache[dev];
+    return p;
 }
 
 namespace {
