@@ -36,7 +36,14 @@ constexpr int kClusterBlocks = 8;
 // units that beginning and ending an item costs (64 ragged sequences of 30 to 4500 keys, 32/8 heads: 112.4 us with 0,
 // 101.9 with 2, 103.8 with 4, 107.0 with 6)
 constexpr int kRowsItemCost = 2;
-constexpr float kRescaleAt = 8.0f;        // a row's reference moves once a logit passes it by this many powers of two
+// A row's reference moves once a logit passes what it was set for by this many powers of two.
+constexpr float kRescaleAt = 8.0f;
+// It is set this many powers of two below the row's maximum.  Probabilities that the second product takes as f16 then use
+// that type's range: at most 2^15, and off by 2^-32 of the row's maximum where they are too small for f16's normal numbers
+// (2^-25 with a reference at the maximum: of 2^20 faint keys beside a loud one, together 3 % of the row's sum, nothing
+// would be left).  bf16 has fp32's range.
+template <bool F16>
+constexpr float kHeadroom = F16 ? 7.0f : 0.0f;
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool bf) {
     if (bf)
@@ -321,8 +328,9 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                 off_next[u] = place(key_next + kStride + 16 * u);
             }
 
-            // running maximum and sum in powers of two; a row's reference m only moves when a logit passes it by
-            // kRescaleAt, so that most steps need neither the shuffles nor the rescaling (P stays below 2^kRescaleAt)
+            // running reference and sum in powers of two; a row's reference m only moves when a logit has passed it by
+            // enough, so that most steps need neither the shuffles nor the rescaling (P stays below
+            // 2^(kRescaleAt + kHeadroom))
             bool moves = false;
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
@@ -334,7 +342,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                         s[u][nb][e] = at < row_limit[nb][e & 1] ? s[u][nb][e] * row_scale[nb][e & 1] : -INFINITY;
                     }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) moves |= fmaxf(s[u][nb][e], s[u][nb][e + 2]) > m[nb][e] + kRescaleAt;
+                    for (int e = 0; e < 2; ++e) moves |= fmaxf(s[u][nb][e], s[u][nb][e + 2]) > m[nb][e] + (kRescaleAt + kHeadroom<!PBF>);
                 }
             if (__any_sync(0xFFFFFFFFu, moves)) {
 #pragma unroll
@@ -347,7 +355,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                         t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 4));
                         t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 8));
                         t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 16));
-                        const float m_new = fmaxf(m[nb][e], t);
+                        const float m_new = fmaxf(m[nb][e], t - kHeadroom<!PBF>);
                         const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m[nb][e] - m_new);
                         m[nb][e] = m_new;
                         l[nb][e] *= f;

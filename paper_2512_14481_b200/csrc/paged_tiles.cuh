@@ -331,6 +331,7 @@ __global__ void __launch_bounds__(kTileThreads<INT8>, 1)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendParams p) {
     using Shape = TileShape<D>;
+    constexpr bool PBF = BF && !INT8;                          // the second product's type; else f16
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* q_smem = smem;
@@ -522,7 +523,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---------------- MMAs, all by one lane (which lets the descriptors live in uniform registers) ----------------
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, BF);
-            constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, BF && !INT8) | ptx::kIdescBTransposed;
+            constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, PBF) | ptx::kIdescBTransposed;
             uint32_t q_phase = 0, p_phase = 0;                        // a bit per row tile
             const uint64_t q_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(q_smem));
             const uint64_t k_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(ring));
@@ -747,8 +748,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (step == 0) continue;
                     if (step == 1) {
                         most *= scale;
-                        if (__any_sync(0xFFFFFFFFu, most > m + kRescaleAt)) {
-                            const float m_new = fmaxf(m, most);
+                        if (__any_sync(0xFFFFFFFFu, most > m + (kRescaleAt + kHeadroom<!PBF>))) {
+                            const float m_new = fmaxf(m, most - kHeadroom<!PBF>);
                             const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m - m_new);
                             m = m_new;
                             const float2 old = unpack2(sum2);
@@ -775,7 +776,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                                       scale2, ref2));
                         const float p0 = exp2_approx(z.x), p1 = exp2_approx(z.y);
                         sum2 = add2(sum2, pack2(p0, p1));
-                        pk[e] = narrow2<BF && !INT8>(p0, p1);
+                        pk[e] = narrow2<PBF>(p0, p1);
                     }
                     ptx::tmem_st_32x32(s_addr + part * 32, pk);
                     ptx::tmem_st_wait();
