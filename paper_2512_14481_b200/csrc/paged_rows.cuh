@@ -440,14 +440,14 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         const float vs = INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f;
         // four elements of the item's result
         auto write = [&](int r, int d, float m, float sum, const float (&acc)[4]) {
-            const float inv = sum > 0.0f ? vs / sum : 0.0f;
+            const float inv = sum != 0.0f ? vs / sum : 0.0f;      // 0: a row without keys; NaN is not one
             const int row = first_row + r, tok = row / p.group;
             const int head = it.h * p.group + row - tok * p.group;
             const long long t = it.s.first + tok;
             *reinterpret_cast<uint2*>(p.out + t * p.out_stride + (long long)head * D + d) =
                 make_uint2(narrow2<BF>(acc[0] * inv, acc[1] * inv), narrow2<BF>(acc[2] * inv, acc[3] * inv));
             if (d == 0 && p.lse != nullptr)
-                p.lse[t * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                p.lse[t * p.heads + head] = sum != 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
         };
         for (int x = tid * 4; x < rows * D; x += kThreads * 4) {
             const int r = x / D, d = x % D;
@@ -597,7 +597,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
             __syncthreads();
             if (warp != 0) continue;
         }
-        const float inv = sum > 0.0f ? vs / sum : 0.0f;
+        const float inv = sum != 0.0f ? vs / sum : 0.0f;
         const int row = pi.first_row + item_row, tok = row / p.group;
         const int head = pi.h * p.group + row - tok * p.group;
         const long long t = pi.first_token + tok;
@@ -605,7 +605,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
 #pragma unroll
         for (int e = 0; e < N / 2; ++e) dst[e] = narrow2<BF>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
         if (lane == 0 && p.lse != nullptr)
-            p.lse[t * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            p.lse[t * p.heads + head] = sum != 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
     }
 }
 

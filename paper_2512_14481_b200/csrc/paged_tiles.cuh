@@ -808,7 +808,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 sum = sum * f0 + o.y * f1;
             }
             const bool whole = it.whole;
-            const float inv = sum > 0.0f ? (INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f) / sum : 0.0f;
+            const float inv = sum != 0.0f ? (INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f) / sum : 0.0f;
             const int tok = item_row / p.group;
             const int head = it.h * p.group + item_row - tok * p.group;
             const long long token = it.first_token + tok;
@@ -841,7 +841,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         uint32_t w[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            w[k] = sum > 0.0f ? narrow2<BF>(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv) : 0u;
+                            w[k] = sum != 0.0f ? narrow2<BF>(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv) : 0u;
                         dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 } else if (valid) {
@@ -851,7 +851,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
             }
             if (valid && whole && p.lse != nullptr)
-                p.lse[token * p.heads + head] = sum > 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                p.lse[token * p.heads + head] = sum != 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             if (valid && !whole) p.part_ml[part_row] = make_float2(m, sum);
             if (!whole && it.t0 == 0 && tid == 0) {
                 PartItem pi;

@@ -1,4 +1,4 @@
-"""Numbers at the ends of their ranges: keys that count for little one by one."""
+"""Numbers at the ends of their ranges: keys that count for little one by one, NaN in a query."""
 import numpy as np
 import pytest
 import torch
@@ -60,3 +60,21 @@ def test_one_loud_key_and_many_faint_ones(new, count, dtype, int8, below):
     assert (np.abs(want) > 0).all()
     assert (np.abs(out - want) <= tail_bounds(bt, tol)).all()
     assert (np.abs(lse - want_lse) <= lse_tol).all()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("new,count", [(1, 2), (1, 60), (12, 2), (12, 60), (70, 2), (70, 60)])
+def test_nan_in_a_query_shows_in_its_own_row_only(new, count, dtype, int8):
+    """A NaN is not a row without keys: out and lse of that (token, head) are NaN, all others are what they were."""
+    lens = [new + 9 * i for i in range(count)]
+    bt = R.Batch(lens, [new] * count, 4, 2, 64, 16, dtype, int8, seed=count)
+    want, want_lse, tol, lse_tol = R.attention(bt, 0.125, True)
+    hit = np.zeros((bt.T, 4), dtype=bool)
+    for t, h in ((0, 1), (bt.T // 2, 3), (bt.T - 1, 0)):
+        hit[t, h] = True
+        bt.q[t, h, 5 * h] = float("nan")
+    out, lse = attend(bt)
+    assert np.isnan(out[hit]).all() and np.isnan(lse[hit]).all()
+    assert (np.abs(out - want) <= tol)[~hit].all()
+    assert (np.abs(lse - want_lse) <= lse_tol)[~hit].all()
