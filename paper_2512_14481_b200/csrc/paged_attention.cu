@@ -296,8 +296,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.out_stride = out_stride;
     p.heads = num_q_heads;
     p.group = num_q_heads / cache->num_kv_heads;
-    // A zero scale would turn masked logits, -inf, into NaN; one this small gives the same equal weights.
-    p.scale = softmax_scale == 0.0f ? 1e-30f : softmax_scale * 1.4426950408889634f;
+    p.scale = softmax_scale * 1.4426950408889634f;
     p.causal = causal != 0;
     // no item has more than one unit when the host's bound says so: nothing to cut, no joining launch
     p.split = batch->max_seq_len > pl.unit;

@@ -701,7 +701,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             int row_limit = it.limit;
             if (p.causal && valid) row_limit = it.before + item_row / p.group + 1;
             const float signed_scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
-            const float scale = fabsf(signed_scale);
+            // A scale of zero, or one that vanished in the product with the factor, would turn masked logits, -inf, into NaN; the
+            // smallest number there is gives the same equal weights.
+            const float scale = signed_scale == 0.0f ? __uint_as_float(1u) : fabsf(signed_scale);
             const uint32_t flip = signed_scale < 0.0f ? 0x80000000u : 0u;    // maxima are then of the negated logits
             float m = -INFINITY;                                   // reference, in powers of two
             uint64_t sum2 = 0;                                     // two partial sums of P

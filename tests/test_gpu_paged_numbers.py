@@ -1,4 +1,4 @@
-"""Numbers at the ends of their ranges: keys that count for little one by one, NaN in a query."""
+"""Numbers at the ends of their ranges: keys that count for little one by one, NaN in a query, factors that vanish."""
 import numpy as np
 import pytest
 import torch
@@ -78,3 +78,15 @@ def test_nan_in_a_query_shows_in_its_own_row_only(new, count, dtype, int8):
     assert np.isnan(out[hit]).all() and np.isnan(lse[hit]).all()
     assert (np.abs(out - want) <= tol)[~hit].all()
     assert (np.abs(lse - want_lse) <= lse_tol)[~hit].all()
+
+
+@pytest.mark.parametrize("factor", [1e-20, 1e-30, -1e-30])
+@pytest.mark.parametrize("new", [1, 12, 70])
+def test_a_scale_and_a_factor_whose_product_vanishes(new, factor):
+    """All logits are zero to fp32: every key that a row sees counts the same."""
+    bt = R.Batch([new, 300], [new] * 2, 4, 4, 64, 16, int8=True, seed=new)
+    bt.k_scale[:] = factor
+    out, lse = attend(bt, scale=0.0)
+    want, want_lse, tol, lse_tol = R.attention(bt, 0.0, True)
+    assert (np.abs(out - want) <= tol).all()
+    assert (np.abs(lse - want_lse) <= lse_tol).all()
