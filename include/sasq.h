@@ -384,8 +384,9 @@ typedef struct {
     int32_t batch;
     int32_t max_pages;          /* usable entries of a row of page_table */
     int32_t total_q;            /* rows of q / k / v / out */
-    int32_t max_q_len;          /* upper bounds of the new tokens and of the keys of a sequence, known to the host: */
-    int32_t max_seq_len;        /* they choose launch shapes only; results do not depend on them */
+    int32_t max_q_len;          /* upper bounds of the new tokens and of the keys of a sequence, known to the host. */
+    int32_t max_seq_len;        /* They choose kernels and launch shapes: with other bounds, results agree to rounding. */
+                                /* Cut to total_q and to the room of the page table; too small a bound costs time only. */
     int32_t reserved;           /* must be 0 */
 } sasq_kv_batch_t;
 
@@ -417,9 +418,9 @@ SASQ_API size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, con
  * (for an int8 cache k_j, v_j are code * factor).  A token that sees no key gets out = +0 and lse = -inf.  What the
  * cache holds past a sequence's keys (NaN included) does not matter.  Logits, maxima, sums and accumulators are fp32;
  * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 cache to f16.
- * Bit-identical from run to run.  Infinities or NaN among a sequence's OWN keys and values are outside the contract: they
- * may reach any row of that sequence, rows that do not see them included.  A NaN in q makes its own (token, head) NaN, out
- * and lse, unless that sees no key.
+ * Bit-identical from run to run for equal host bounds.  Infinities or NaN among a sequence's OWN keys and values are
+ * outside the contract: they may reach any row of that sequence, rows that do not see them included.  A NaN in q makes
+ * its own (token, head) NaN, out and lse, unless that sees no key.
  * q: as for sasq_rope_kv_append (already rotated); out: [total_q, num_q_heads, head_dim] of `dt`, rows at out_stride;
  * must not alias q.  lse: [total_q, num_q_heads] fp32 (natural logarithm) or NULL.  head_dim: 64 or 128.
  * workspace: >= sasq_paged_attention_workspace() bytes, 16-byte aligned, contents need no initialisation; calls that

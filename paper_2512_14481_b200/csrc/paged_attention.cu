@@ -92,6 +92,16 @@ bool tiles_possible(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int head
     return (long long)b->max_q_len * group > 16 && group <= 128 && c->num_pages > 0;
 }
 
+// The batch with its bounds cut to what q and the page table can hold (the device cuts lengths to the same), so that a
+// caller who leaves a bound wide open gets the plan, and the workspace, of one who gives it.
+sasq_kv_batch_t with_cut_bounds(const sasq_kv_batch_t* b, const PagedParams& p) {
+    sasq_kv_batch_t cut = *b;
+    const long long room = (long long)p.max_pages << p.page_shift;
+    if (cut.max_seq_len > room) cut.max_seq_len = (int32_t)room;
+    if (cut.max_q_len > cut.total_q) cut.max_q_len = cut.total_q;
+    return cut;
+}
+
 Plan make_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
     Plan pl = rows_plan(c, b, heads, sms);
     const long long rows = (long long)b->max_q_len * (heads / c->num_kv_heads);
@@ -262,7 +272,8 @@ size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, const sasq_k
     using namespace sasq;
     PagedParams p{};
     if (attend_check(cache, batch, num_q_heads, SASQ_BF16, &p) != SASQ_OK) return 0;
-    return most_workspace(cache, batch, num_q_heads);
+    const sasq_kv_batch_t cut = with_cut_bounds(batch, p);
+    return most_workspace(cache, &cut, num_q_heads);
 }
 
 int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* batch, const void* q, void* out, float* lse,
@@ -286,7 +297,8 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     if (sms <= 0 || sms > kMaxSms) return SASQ_ERR_UNSUPPORTED;
     p.c.status = paged_status_ptr();
     if (p.c.status == nullptr) return SASQ_ERR_CUDA;
-    const Plan pl = make_plan(cache, batch, num_q_heads, sms);
+    const sasq_kv_batch_t cut = with_cut_bounds(batch, p.c);
+    const Plan pl = make_plan(cache, &cut, num_q_heads, sms);
     const Layout l = layout_of(pl.blocks, pl.slot_rows, cache->head_dim);
     if (pl.cluster == 0 && l.total > ws_bytes) return SASQ_ERR_WORKSPACE;      // most_workspace covers every plan
     p.q = static_cast<const uint16_t*>(q);
@@ -299,7 +311,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.scale = softmax_scale * 1.4426950408889634f;
     p.causal = causal != 0;
     // no item has more than one unit when the host's bound says so: nothing to cut, no joining launch
-    p.split = batch->max_seq_len > pl.unit;
+    p.split = cut.max_seq_len > pl.unit;
     p.max_blocks = pl.blocks;
     p.item_rows = pl.rows;
     p.tile_bound = pl.tile_bound;
