@@ -237,6 +237,8 @@ extern "C" int sasq_rope_kv_append(const sasq_kv_cache_t* cache, const sasq_kv_b
         if (k_stride < row_kv || v_stride < row_kv || k_stride % 8 != 0 || v_stride % 8 != 0) return SASQ_ERR_INVALID_ARG;
         if (has_q && (q_stride < row_q || q_out_stride < row_q || q_stride % 8 != 0 || q_out_stride % 8 != 0))
             return SASQ_ERR_INVALID_ARG;
+        // in place a row has to stay where it is: with another stride rows would be written that are still to be read
+        if (has_q && q == q_out && q_stride != q_out_stride && batch->total_q > 1) return SASQ_ERR_INVALID_ARG;
         if (rot_dim > 0 && (cos_sin == nullptr || !aligned16(cos_sin))) return SASQ_ERR_INVALID_ARG;
     }
     if (cache->head_dim % 16 != 0 || cache->head_dim > 256 || rot_dim % 16 != 0 || rot_dim > cache->head_dim)
