@@ -398,7 +398,8 @@ typedef struct {
  * the code of Eq. 1 of the fp32 value, with s = k_scale[head] or v_scale[head].
  * q: [total_q, num_q_heads, head_dim] of `dt`, row t at q + t * q_stride elements, heads contiguous; k, v: the same
  * with num_kv_heads.  q_out: the rotated q (rows at q_out_stride); may be q itself, with the same stride, but must not
- * overlap it otherwise.  q == q_out == NULL: keys and values only.  cos_sin: [max_positions, rot_dim] fp32.  Strides are multiples of 8 elements, pointers 16-byte aligned.
+ * overlap it otherwise.  q == q_out == NULL: keys and values only.  cos_sin: [max_positions, rot_dim] fp32.  Strides are
+ * multiples of 8 elements, pointers 16-byte aligned.
  * head_dim: a multiple of 16 up to 256.  rot_dim: a multiple of 16 up to head_dim (0: no rotation, cos_sin unused).
  * A position outside cos_sin or the page table, or a page outside the cache, is not written (its q_out rows become
  * +0) and sets SASQ_ERR_BAD_INDEX; a factor that Eq. 1 cannot use sets SASQ_ERR_BAD_SCALE.  Two new tokens of one call
