@@ -359,8 +359,8 @@ typedef enum { SASQ_KV_16BIT = 0,   /* elements of the activations' dtype */
 typedef struct {
     void* k;
     void* v;
-    const float* k_scale;       /* [num_kv_heads] factors of the codes (SASQ_KV_INT8), else NULL */
-    const float* v_scale;
+    const float* k_scale;       /* [num_kv_heads] factors of the codes (SASQ_KV_INT8), else NULL; k's are those of */
+    const float* v_scale;       /* the ROTATED keys, which the cache holds */
     int64_t page_stride, token_stride, head_stride;
     int64_t num_pages;
     int32_t page_size;          /* positions per page: 16, 32, 64, 128 or 256 */
@@ -400,7 +400,8 @@ typedef struct {
  * with num_kv_heads.  q_out: the rotated q (rows at q_out_stride); may be q itself, with the same stride, but must not
  * overlap it otherwise.  q == q_out == NULL: keys and values only.  cos_sin: [max_positions, rot_dim] fp32.  Strides are
  * multiples of 8 elements, pointers 16-byte aligned.
- * head_dim: a multiple of 16 up to 256.  rot_dim: a multiple of 16 up to head_dim (0: no rotation, cos_sin unused).
+ * head_dim: a multiple of 16 up to 256 (sasq_paged_attention reads caches of 64 and 128).  rot_dim: a multiple of 16 up
+ * to head_dim (0: no rotation, cos_sin unused).
  * A position outside cos_sin or the page table, or a page outside the cache, is not written (its q_out rows become
  * +0) and sets SASQ_ERR_BAD_INDEX; a factor that Eq. 1 cannot use sets SASQ_ERR_BAD_SCALE.  Two new tokens of one call
  * must not share a cache row. */

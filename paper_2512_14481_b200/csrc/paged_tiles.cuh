@@ -325,7 +325,8 @@ __device__ __forceinline__ void registers_to() {
 // the PV that frees it, across items too: the next item's queries are fetched as soon as the last QK has read the old
 // ones, so that its first S is there when the softmax warps have stored the old item's rows.
 // Bound by that alternation: 256 rows x 128 keys take 2050 clocks of MMAs and 2048 of exponentials, and a step takes about
-// 3500 (8192 causal tokens, 32 heads of 128, bf16: 516 us, 1065 TFLOP/s at 1.5 to 1.65 GHz; the power cap is near).
+// 3500 (8192 causal tokens, 32 heads of 128, bf16: 511 us, 1076 TFLOP/s in short bursts; 619 us, 888 TFLOP/s, one call after
+// another under the power cap, at 1.4 to 1.65 GHz).
 template <int D, bool BF, bool INT8>
 __global__ void __launch_bounds__(kTileThreads<INT8>, 1)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
