@@ -719,7 +719,7 @@ def sasq_fakequant_fwd_bwd_static(x, grad_y, y, grad_x, grad_scale, scale, bits:
 # ---------------------------------------------------------------------------
 # paged key/value cache
 # ---------------------------------------------------------------------------
-_current_device = torch._C._cuda_getDevice
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _elsewhere(device: int, t, name: str):
