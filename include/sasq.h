@@ -349,18 +349,22 @@ SASQ_API int sasq_static_w8a8_linear_tiles(int64_t T, int64_t N, int num_pairs, 
  *
  * A cache is a pool of pages; a page holds `page_size` consecutive positions of ONE sequence, for every KV head.
  * Element (page, row, head, d) of K or V lies at
- *   base + page * page_stride + row * token_stride + head * head_stride + d                (strides in elements)
+ *   base + page * page_stride + row * token_stride + head * head_stride + d                (strides in elements; the
+ *                                                                                    byte of a 4-bit one: half of that)
  * so both orders of a page, tokens first and heads first, are expressed by the strides.  K and V share the strides. */
 typedef enum { SASQ_KV_16BIT = 0,   /* elements of the activations' dtype */
-               SASQ_KV_INT8 = 1     /* int8 codes (Eq. 1, b = 8) under one static factor per KV head */
+               SASQ_KV_INT8 = 1,    /* int8 codes (Eq. 1, b = 8) under one static factor per KV head */
+               SASQ_KV_INT4 = 2     /* 4-bit codes (Eq. 1, b = 4), two to a byte, the even channel's in the low half (two's
+                                       complement), under one static factor per KV head and channel.  A factor is used
+                                       rounded to bfloat16 (to nearest even), here written s: a code times s then fits f16 */
 } sasq_kv_kind_t;
 
 /* The cache (host struct; the pointers are device pointers, 16-byte aligned; the strides are multiples of 16 bytes). */
 typedef struct {
     void* k;
     void* v;
-    const float* k_scale;       /* [num_kv_heads] factors of the codes (SASQ_KV_INT8), else NULL; k's are those of */
-    const float* v_scale;       /* the ROTATED keys, which the cache holds */
+    const float* k_scale;       /* factors of the codes, of the ROTATED keys, which the cache holds: [num_kv_heads] for */
+    const float* v_scale;       /* SASQ_KV_INT8, [num_kv_heads][head_dim] (16-byte aligned) for SASQ_KV_INT4, else NULL */
     int64_t page_stride, token_stride, head_stride;
     int64_t num_pages;
     int32_t page_size;          /* positions per page: 16, 32, 64, 128 or 256 */
@@ -395,13 +399,14 @@ typedef struct {
  * c = cos_sin[p][j], s = cos_sin[p][rot_dim / 2 + j], j < rot_dim / 2:
  *   a' = fl32(fl32(a c) - fl32(b s)),   b' = fl32(fl32(b c) + fl32(a s))         (fp32, no fused multiply-add)
  * Elements from rot_dim on, and all of v, pass unchanged.  16-bit destinations get one narrowing; an int8 cache gets
- * the code of Eq. 1 of the fp32 value, with s = k_scale[head] or v_scale[head].
+ * the code of Eq. 1 of the fp32 value, with s = k_scale[head] or v_scale[head]; a 4-bit cache the code with b = 4 and the
+ * channel's own s.
  * q: [total_q, num_q_heads, head_dim] of `dt`, row t at q + t * q_stride elements, heads contiguous; k, v: the same
  * with num_kv_heads.  q_out: the rotated q (rows at q_out_stride); may be q itself, with the same stride, but must not
  * overlap it otherwise.  q == q_out == NULL: keys and values only.  cos_sin: [max_positions, rot_dim] fp32.  Strides are
  * multiples of 8 elements, pointers 16-byte aligned.
- * head_dim: a multiple of 16 up to 256 (sasq_paged_attention reads caches of 64 and 128).  rot_dim: a multiple of 16 up
- * to head_dim (0: no rotation, cos_sin unused).
+ * head_dim: a multiple of 16 (4-bit cache: of 32) up to 256 (sasq_paged_attention reads caches of 64 and 128).  rot_dim:
+ * a multiple of 16 up to head_dim (0: no rotation, cos_sin unused).
  * A position outside cos_sin or the page table, or a page outside the cache, is not written (its q_out rows become
  * +0) and sets SASQ_ERR_BAD_INDEX; a factor that Eq. 1 cannot use sets SASQ_ERR_BAD_SCALE.  Two new tokens of one call
  * must not share a cache row. */
@@ -417,9 +422,9 @@ SASQ_API size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, con
 /* Attention of the new tokens over their sequences' cached keys.  Query head c reads KV head c / (num_q_heads /
  * num_kv_heads).  Token i of sequence b sees the first  causal ? p + 1 : seq_lens[b]  keys:
  *   s_j = softmax_scale * <q, k_j>,   lse = log sum_j exp(s_j),   out = sum_j exp(s_j - lse) v_j
- * (for an int8 cache k_j, v_j are code * factor).  A token that sees no key gets out = +0 and lse = -inf.  What the
+ * (for an int8 or 4-bit cache k_j, v_j are code * factor).  A token that sees no key gets out = +0 and lse = -inf.  What the
  * cache holds past a sequence's keys (NaN included) does not matter.  Logits, maxima, sums and accumulators are fp32;
- * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 cache to f16.
+ * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 or 4-bit cache to f16.
  * Bit-identical from run to run for equal host bounds.  Infinities or NaN among a sequence's OWN keys and values are
  * outside the contract: they may reach any row of that sequence, rows that do not see them included.  A NaN in q makes
  * its own (token, head) NaN, out and lse, unless that sees no key.

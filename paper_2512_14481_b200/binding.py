@@ -28,7 +28,7 @@ __all__ = [
     "sasq_fakequant_linear_fp_weights", "sasq_absmax_scale_per_channel", "sasq_running_mean", "LinearDesc", "sasq_static_w8a8_linear_multi_workspace",
     "sasq_static_w8a8_linear_multi", "sasq_static_w8a8_linear_multi_launches", "sasq_set_gang_launch",
     "sasq_debug_int8_issue_rate", "LinearProblems", "QuantTensors",
-    "SASQ_KV_16BIT", "SASQ_KV_INT8", "KVCacheStruct", "KVBatchStruct", "KVCache", "PagedBatch", "sasq_rope_kv_append",
+    "SASQ_KV_16BIT", "SASQ_KV_INT8", "SASQ_KV_INT4", "KVCacheStruct", "KVBatchStruct", "KVCache", "PagedBatch", "sasq_rope_kv_append",
     "sasq_paged_attention_workspace", "sasq_paged_attention",
 ]
 
@@ -39,6 +39,7 @@ SASQ_WITHOUT_ROUND = 1
 SASQ_WITHOUT_CLAMP = 2
 SASQ_KV_16BIT = 0
 SASQ_KV_INT8 = 1
+SASQ_KV_INT4 = 2
 
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -752,7 +753,8 @@ def _wrong_device(cache, batch):
 class KVCache:
     """A paged cache, marshalled once (see LinearProblems).  k, v: [num_pages, page_size, num_kv_heads, head_dim] views
     of one stride pattern, last dimension contiguous (a pool stored heads first is passed as its .transpose(1, 2));
-    fp16 / bf16, or int8 with k_scale, v_scale: [num_kv_heads] fp32 factors.  Holds references to the tensors."""
+    fp16 / bf16, or int8 with k_scale, v_scale: [num_kv_heads] fp32 factors, or uint8 for 4-bit codes, two to a byte (the
+    last dimension is head_dim / 2), with k_scale, v_scale: [num_kv_heads, head_dim].  Holds references to the tensors."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         for name, t in (("k", k), ("v", v)):
@@ -761,26 +763,31 @@ class KVCache:
             if t.dim() != 4 or t.stride(3) != 1:
                 raise ValueError(f"{name} must be [num_pages, page_size, num_kv_heads, head_dim] with a contiguous last "
                                  "dimension")
-            if t.dtype not in (torch.int8, torch.float16, torch.bfloat16):
-                raise TypeError(f"{name} must be int8, float16 or bfloat16, got {t.dtype}")
+            if t.dtype not in (torch.uint8, torch.int8, torch.float16, torch.bfloat16):
+                raise TypeError(f"{name} must be uint8 (4-bit codes), int8, float16 or bfloat16, got {t.dtype}")
         if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.get_device() != v.get_device():
             raise ValueError("k and v must share shape, strides, dtype and device")
-        int8 = k.dtype == torch.int8
+        int8, int4 = k.dtype == torch.int8, k.dtype == torch.uint8
         self.device = k.get_device()
+        self.num_kv_heads, self.head_dim = k.shape[2], k.shape[3] * 2 if int4 else k.shape[3]
         for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-            if int8 != (t is not None):
-                raise ValueError(f"{name} goes with an int8 cache, and only with it")
+            if (int8 or int4) != (t is not None):
+                raise ValueError(f"{name} goes with an int8 or 4-bit cache, and only with it")
             if t is not None:
                 _flat(t, name, self.device, torch.float32)
-                if t.numel() != k.shape[2]:
+                if int8 and t.numel() != k.shape[2]:
                     raise ValueError(f"{name} must hold one factor per KV head")
+                if int4 and t.shape != (self.num_kv_heads, self.head_dim):
+                    raise ValueError(f"{name} must be [num_kv_heads, head_dim]")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.num_kv_heads, self.head_dim, self.dtype = k.shape[2], k.shape[3], k.dtype
+        self.dtype = k.dtype
+        self.token_dtype = None if int8 or int4 else k.dtype    # of the tokens that go in and come out; None: either
         # a dimension of one entry may have any stride in torch; the library wants whole 16-byte words
-        page_stride, token_stride, head_stride, _ = (s if n > 1 else k.shape[3] for s, n in zip(k.stride(), k.shape))
+        strides = [s if n > 1 else k.shape[3] for s, n in zip(k.stride()[:3], k.shape)]
+        page_stride, token_stride, head_stride = (2 * s for s in strides) if int4 else strides
         self.struct = KVCacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), page_stride, token_stride, head_stride,
-                                    k.shape[0], k.shape[1], k.shape[2], k.shape[3],
-                                    SASQ_KV_INT8 if int8 else SASQ_KV_16BIT)
+                                    k.shape[0], k.shape[1], k.shape[2], self.head_dim,
+                                    SASQ_KV_INT4 if int4 else SASQ_KV_INT8 if int8 else SASQ_KV_16BIT)
         self.ref = ctypes.byref(self.struct)
 
 
@@ -843,7 +850,7 @@ def sasq_rope_kv_append(cache: KVCache, batch: PagedBatch, q, k, v, q_out, cos_s
     if batch.device != device or _current_device() != device:
         _wrong_device(cache, batch)
     dt = k.dtype
-    if cache.dtype is not torch.int8 and cache.dtype != dt:
+    if cache.token_dtype is not None and cache.token_dtype != dt:
         raise TypeError(f"k must have the cache's dtype {cache.dtype}")
     _, ks = _heads(k, "k", dt, T, K, D, device)
     _, vs = _heads(v, "v", dt, T, K, D, device)
@@ -879,7 +886,7 @@ def sasq_paged_attention(cache: KVCache, batch: PagedBatch, q, out, workspace, l
     if batch.device != device or _current_device() != device:
         _wrong_device(cache, batch)
     dt = q.dtype
-    if cache.dtype is not torch.int8 and cache.dtype != dt:
+    if cache.token_dtype is not None and cache.token_dtype != dt:
         raise TypeError(f"q must have the cache's dtype {cache.dtype}")
     H, qs = _heads(q, "q", dt, T, None, D, device)
     _, os_ = _heads(out, "out", dt, T, H, D, device)

@@ -53,11 +53,31 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float inv) {
     return make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
 }
 
+// the same with b = 4, and eight of them in a word, the first in its low bits
+__device__ __forceinline__ uint32_t code4(float x, float inv) {
+    const float r = rintf(__fmul_rn(x, inv));
+    return (uint32_t)(int)fminf(fmaxf(r, -8.0f), 7.0f) & 15u;
+}
+// Codes of eight channels with a factor each; `bad` collects whether Eq. 1 can use them.
+__device__ __forceinline__ uint32_t codes4(const float (&f)[8], const float* scale, bool* bad) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(scale)), b = __ldg(reinterpret_cast<const float4*>(scale) + 1);
+    const float s[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = factor4(s[i]);
+        *bad |= scale_is_bad(t);
+        w |= code4(f[i], __fdiv_rn(1.0f, t)) << (4 * i);
+    }
+    return w;
+}
+
 // A thread owns a "unit" of a head, two 8-element words that the rotation mixes: words u and u + rot / 16 for half-split
 // pairs, 2u and 2u + 1 for interleaved ones and behind the rotated part.  Its cosines and sines serve every head that
 // it walks (heads h, h + head_step, ...), so they are read once per token and block.  A block has one token.
-template <bool BF, bool INT8>
+template <bool BF, int KIND>
 __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __grid_constant__ AppendParams p) {
+    constexpr bool INT8 = KIND == SASQ_KV_INT8, INT4 = KIND == SASQ_KV_INT4;
     const int units = p.dim >> 4;
     const int u = threadIdx.x % units, slot = threadIdx.x / units;
     pdl_launch_dependents();
@@ -121,7 +141,7 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
         uint4 x0 = words[a0], x1 = words[a1];
         if (which != 0 && !there) continue;
         float f0[8], f1[8];
-        if (turn || (INT8 && which != 0)) {
+        if (turn || (KIND != SASQ_KV_16BIT && which != 0)) {
             widen8<BF>(x0, f0);
             widen8<BF>(x1, f1);
         }
@@ -142,7 +162,7 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
                     f[2 * (i & 3) + 1] = __fadd_rn(__fmul_rn(c, co[i]), __fmul_rn(a, si[i]));
                 }
             }
-            if (!INT8 || which == 0) {
+            if (KIND == SASQ_KV_16BIT || which == 0) {
                 x0 = narrow8<BF>(f0);
                 x1 = narrow8<BF>(f1);
             }
@@ -162,6 +182,13 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
                 uint2* dst = reinterpret_cast<uint2*>(static_cast<int8_t*>(base) + at);
                 dst[a0] = codes8(f0, inv);
                 dst[a1] = codes8(f1, inv);
+            } else if constexpr (INT4) {
+                const float* sc = (which == 1 ? p.c.k_scale : p.c.v_scale) + hh * p.dim;
+                uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(base) + (at >> 1));
+                bool bad = false;
+                dst[a0] = codes4(f0, sc + 8 * a0, &bad);
+                dst[a1] = codes4(f1, sc + 8 * a1, &bad);
+                if (bad) atomicMax(p.c.status, (int)SASQ_ERR_BAD_SCALE);
             } else {
                 uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at);
                 dst[a0] = x0;
@@ -175,7 +202,7 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
 
 int paged_check(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int dt, PagedParams* p) {
     if (c == nullptr || b == nullptr || (dt != SASQ_F16 && dt != SASQ_BF16)) return SASQ_ERR_INVALID_ARG;
-    if (c->kind != SASQ_KV_16BIT && c->kind != SASQ_KV_INT8) return SASQ_ERR_INVALID_ARG;
+    if (c->kind != SASQ_KV_16BIT && c->kind != SASQ_KV_INT8 && c->kind != SASQ_KV_INT4) return SASQ_ERR_INVALID_ARG;
     if (c->num_pages < 0 || c->num_kv_heads <= 0 || c->head_dim <= 0 || b->batch < 0 || b->total_q < 0 || b->max_pages < 0 ||
         b->max_q_len < 0 || b->max_seq_len < 0 || b->reserved != 0)
         return SASQ_ERR_INVALID_ARG;
@@ -187,13 +214,15 @@ int paged_check(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int dt, Page
     if (ints & 3u) return SASQ_ERR_INVALID_ARG;
     if (c->num_pages > 0 && (c->k == nullptr || c->v == nullptr || !aligned16(c->k) || !aligned16(c->v)))
         return SASQ_ERR_INVALID_ARG;
-    const int elem = c->kind == SASQ_KV_INT8 ? 1 : 2;
+    const int per_word = c->kind == SASQ_KV_INT4 ? 32 : c->kind == SASQ_KV_INT8 ? 16 : 8;      // elements in 16 bytes
     if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return SASQ_ERR_INVALID_ARG;
-    if (c->page_stride * elem % 16 != 0 || c->token_stride * elem % 16 != 0 || c->head_stride * elem % 16 != 0)
+    if (c->page_stride % per_word != 0 || c->token_stride % per_word != 0 || c->head_stride % per_word != 0)
         return SASQ_ERR_INVALID_ARG;
     const bool factors = c->k_scale != nullptr && c->v_scale != nullptr;
-    if (c->kind == SASQ_KV_INT8 ? !factors : (c->k_scale != nullptr || c->v_scale != nullptr)) return SASQ_ERR_INVALID_ARG;
-    if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3u) return SASQ_ERR_INVALID_ARG;
+    if (c->kind != SASQ_KV_16BIT ? !factors : (c->k_scale != nullptr || c->v_scale != nullptr)) return SASQ_ERR_INVALID_ARG;
+    // 4-bit: a factor per channel, read in 16-byte words
+    const uintptr_t odd = (reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale));
+    if (odd & (c->kind == SASQ_KV_INT4 ? 15u : 3u)) return SASQ_ERR_INVALID_ARG;
     int shift = 4;
     while (shift < 8 && (1 << shift) != c->page_size) ++shift;
     if ((1 << shift) != c->page_size) return SASQ_ERR_UNSUPPORTED;
@@ -215,6 +244,7 @@ int paged_check(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int dt, Page
     p->total_q = b->total_q;
     p->page_shift = shift;
     p->kv_heads = c->num_kv_heads;
+    p->kind = c->kind;
     return SASQ_OK;
 }
 
@@ -244,6 +274,7 @@ extern "C" int sasq_rope_kv_append(const sasq_kv_cache_t* cache, const sasq_kv_b
     }
     if (cache->head_dim % 16 != 0 || cache->head_dim > 256 || rot_dim % 16 != 0 || rot_dim > cache->head_dim)
         return SASQ_ERR_UNSUPPORTED;
+    if (cache->kind == SASQ_KV_INT4 && cache->head_dim % 32 != 0) return SASQ_ERR_UNSUPPORTED;
     if (batch->total_q == 0 || batch->batch == 0) return SASQ_OK;
     const int sms = device_sm_count_if_sm100();
     if (sms <= 0) return SASQ_ERR_UNSUPPORTED;
@@ -277,12 +308,9 @@ extern "C" int sasq_rope_kv_append(const sasq_kv_cache_t* cache, const sasq_kv_b
     cudaLaunchAttribute attr = pdl_attribute();
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    cudaError_t e;
-    if (cache->kind == SASQ_KV_INT8)
-        e = dt == SASQ_BF16 ? cudaLaunchKernelEx(&cfg, rope_kv_append_kernel<true, true>, p)
-                            : cudaLaunchKernelEx(&cfg, rope_kv_append_kernel<false, true>, p);
-    else
-        e = dt == SASQ_BF16 ? cudaLaunchKernelEx(&cfg, rope_kv_append_kernel<true, false>, p)
-                            : cudaLaunchKernelEx(&cfg, rope_kv_append_kernel<false, false>, p);
+    auto go = [&](auto* bf16_kernel, auto* f16_kernel) { return cudaLaunchKernelEx(&cfg, dt == SASQ_BF16 ? bf16_kernel : f16_kernel, p); };
+    const cudaError_t e = cache->kind == SASQ_KV_INT4 ? go(rope_kv_append_kernel<true, SASQ_KV_INT4>, rope_kv_append_kernel<false, SASQ_KV_INT4>)
+                          : cache->kind == SASQ_KV_INT8 ? go(rope_kv_append_kernel<true, SASQ_KV_INT8>, rope_kv_append_kernel<false, SASQ_KV_INT8>)
+                                                        : go(rope_kv_append_kernel<true, SASQ_KV_16BIT>, rope_kv_append_kernel<false, SASQ_KV_16BIT>);
     return e == cudaSuccess ? SASQ_OK : SASQ_ERR_CUDA;
 }

@@ -60,14 +60,15 @@ int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 Plan rows_plan(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads, int sms) {
     Plan pl{};
     const long long rows = (long long)b->max_q_len * (heads / c->num_kv_heads);
-    const bool int8 = c->kind == SASQ_KV_INT8, d128 = c->head_dim == 128;
+    const bool d128 = c->head_dim == 128;
     pl.nb = rows <= 8 ? 1 : 2;
     pl.rows = pl.slot_rows = 8 * pl.nb;
-    pl.unit = pl.nb == 1 ? (int8 ? kRowsUnit<1, true> : kRowsUnit<1, false>) : kRowsUnit<2, false>;
+    const int units[2][3] = {{kRowsUnit<1, 0>, kRowsUnit<1, 1>, kRowsUnit<1, 2>}, {kRowsUnit<2, 0>, kRowsUnit<2, 1>, kRowsUnit<2, 2>}};
+    pl.unit = units[pl.nb - 1][c->kind];
     pl.tile_bound = rows < 1 ? 1 : ceil_div(rows, pl.rows);
-    const int per_sm = pl.nb == 1 ? (d128 ? (int8 ? kRowsBlocksPerSm<128, 1, true> : kRowsBlocksPerSm<128, 1, false>)
-                                          : (int8 ? kRowsBlocksPerSm<64, 1, true> : kRowsBlocksPerSm<64, 1, false>))
-                                  : kRowsBlocksPerSm<128, 2, false>;
+    const int blocks[2][3] = {{kRowsBlocksPerSm<64, 1, 0>, kRowsBlocksPerSm<64, 1, 1>, kRowsBlocksPerSm<64, 1, 2>},
+                              {kRowsBlocksPerSm<128, 1, 0>, kRowsBlocksPerSm<128, 1, 1>, kRowsBlocksPerSm<128, 1, 2>}};
+    const int per_sm = pl.nb == 1 ? blocks[d128][c->kind] : kRowsBlocksPerSm<128, 2, 0>;
     pl.items = (long long)b->batch * c->num_kv_heads * pl.tile_bound;
     pl.fill = sms * per_sm;
     return pl;
@@ -89,7 +90,7 @@ void set_blocks(Plan* pl, const sasq_kv_batch_t* b) {
 }
 bool tiles_possible(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads) {
     const int group = heads / c->num_kv_heads;
-    return (long long)b->max_q_len * group > 16 && group <= 128 && c->num_pages > 0;
+    return (long long)b->max_q_len * group > 16 && group <= 128 && c->num_pages > 0 && c->kind != SASQ_KV_INT4;
 }
 
 // The batch with its bounds cut to what q and the page table can hold (the device cuts lengths to the same), so that a
@@ -161,21 +162,20 @@ cudaError_t launch(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStrea
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <int D, int NB, bool BF>
-cudaError_t launch_rows(const Plan& pl, const AttendParams& p, bool int8, cudaStream_t st) {
+template <int D, int NB, bool BF, int KIND>
+cudaError_t launch_rows(const Plan& pl, const AttendParams& p, cudaStream_t st) {
     const dim3 grid((unsigned)p.max_blocks);
     if constexpr (NB * D <= 128) {             // eight warps' sums fit 48 KB of shared memory
-        if (pl.cluster == 8)
-            return int8 ? launch(paged_rows_kernel<D, NB, BF, true, true, 8>, grid, 256, 0, st, p, kClusterBlocks)
-                        : launch(paged_rows_kernel<D, NB, BF, false, true, 8>, grid, 256, 0, st, p, kClusterBlocks);
+        if (pl.cluster == 8) return launch(paged_rows_kernel<D, NB, BF, KIND, true, 8>, grid, 256, 0, st, p, kClusterBlocks);
     }
-    if (pl.cluster != 0)
-        return int8 ? launch(paged_rows_kernel<D, NB, BF, true, true, 4>, grid, 128, 0, st, p, kClusterBlocks)
-                    : launch(paged_rows_kernel<D, NB, BF, false, true, 4>, grid, 128, 0, st, p, kClusterBlocks);
-    const cudaError_t e = int8 ? launch(paged_rows_kernel<D, NB, BF, true, false, 4>, grid, 128, 0, st, p)
-                               : launch(paged_rows_kernel<D, NB, BF, false, false, 4>, grid, 128, 0, st, p);
+    if (pl.cluster != 0) return launch(paged_rows_kernel<D, NB, BF, KIND, true, 4>, grid, 128, 0, st, p, kClusterBlocks);
+    const cudaError_t e = launch(paged_rows_kernel<D, NB, BF, KIND, false, 4>, grid, 128, 0, st, p);
     if (e != cudaSuccess || !p.split) return e;
     return launch(paged_join_kernel<8 * NB, 8 * NB, D, BF, true>, dim3(p.max_blocks, 8 * NB), 256, 0, st, p);
+}
+template <int D, bool BF, int KIND>
+cudaError_t launch_few(const Plan& pl, const AttendParams& p, cudaStream_t st) {
+    return pl.nb == 1 ? launch_rows<D, 1, BF, KIND>(pl, p, st) : launch_rows<D, 2, BF, KIND>(pl, p, st);
 }
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -258,9 +258,11 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, int ma
 
 template <int D, bool BF>
 cudaError_t launch_all(const Plan& pl, const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
-    const bool int8 = c->kind == SASQ_KV_INT8;
-    if (pl.tiles) return int8 ? launch_tiles<D, BF, true>(p, c, pl.max_rows, st) : launch_tiles<D, BF, false>(p, c, pl.max_rows, st);
-    return pl.nb == 1 ? launch_rows<D, 1, BF>(pl, p, int8, st) : launch_rows<D, 2, BF>(pl, p, int8, st);
+    if (pl.tiles)
+        return c->kind == SASQ_KV_INT8 ? launch_tiles<D, BF, true>(p, c, pl.max_rows, st) : launch_tiles<D, BF, false>(p, c, pl.max_rows, st);
+    return c->kind == SASQ_KV_INT4   ? launch_few<D, BF, SASQ_KV_INT4>(pl, p, st)
+           : c->kind == SASQ_KV_INT8 ? launch_few<D, BF, SASQ_KV_INT8>(pl, p, st)
+                                     : launch_few<D, BF, SASQ_KV_16BIT>(pl, p, st);
 }
 
 }  // namespace

@@ -1,5 +1,5 @@
 // Shared by the paged-cache kernels: the launch parameters, the lookup of a sequence, the division of an attention
-// call's work among its thread blocks, and the int8 codes' conversion.
+// call's work among its thread blocks, and the conversion of int8 and 4-bit codes.
 #pragma once
 
 #include "common.cuh"
@@ -23,6 +23,7 @@ struct PagedParams {
     int batch, max_pages, total_q;
     int page_shift;             // log2(page_size)
     int kv_heads;
+    int kind;                   // sasq_kv_kind_t
     int* status;
 };
 
@@ -259,6 +260,16 @@ __device__ __forceinline__ uint32_t codes_to_pair(uint32_t w) {
         return *reinterpret_cast<const uint32_t*>(&d);
     }
 }
+
+// A 4-bit cache's factor as it is used: rounded to bf16.  A code times it has at most 3 + 8 = 11 significant bits, which f16
+// holds, so that the tensor cores can take the product as an exact operand.
+__device__ __forceinline__ float factor4(float s) { return __bfloat162float(__float2bfloat16_rn(s)); }
+
+// 4-bit codes as f16, without arithmetic: a nibble that is alone in the low byte of a 16-bit half is a subnormal number, 2^-24
+// times the nibble (low nibble of the byte) or 2^-20 times (high nibble).  The code's sign bit is flipped on the way, so the
+// nibble stands for u = code + 8.
+__device__ __forceinline__ uint32_t nibbles_low(uint32_t w) { return (w & 0x000F000Fu) ^ 0x00080008u; }
+__device__ __forceinline__ uint32_t nibbles_high(uint32_t w) { return (w & 0x00F000F0u) ^ 0x00800080u; }
 
 // 2^x by the hardware's approximation (2^-inf = 0)
 __device__ __forceinline__ float exp2_approx(float x) {

@@ -28,10 +28,10 @@ namespace {
 
 // Blocks of 16 keys of a warp's step: with 8 rows as many bytes are under way whatever the cache holds (16 rows' sums leave
 // no registers for that), and keys of a unit: a step of four warps.
-template <int NB, bool INT8>
-constexpr int kRowsSub = INT8 && NB == 1 ? 2 : 1;
-template <int NB, bool INT8>
-constexpr int kRowsUnit = 64 * kRowsSub<NB, INT8>;
+template <int NB, int KIND>
+constexpr int kRowsSub = NB != 1 || KIND == SASQ_KV_16BIT ? 1 : 2;
+template <int NB, int KIND>
+constexpr int kRowsUnit = 64 * kRowsSub<NB, KIND>;
 constexpr int kClusterBlocks = 8;
 // units that beginning and ending an item costs (64 ragged sequences of 30 to 4500 keys, 32/8 heads: 112.4 us with 0,
 // 101.9 with 2, 103.8 with 4, 107.0 with 6)
@@ -90,9 +90,15 @@ __device__ __forceinline__ uint2 ldg_stream8(const void* p) {
     return v;
 }
 
+__device__ __forceinline__ uint32_t ldg_stream4(const void* p) {
+    uint32_t v;
+    asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
 // Blocks that an SM holds: as many as the registers of the fragments leave room for.  At this bound the variants for 8 rows
 // over int8 codes spill 4 to 20 bytes a thread, outside the loop over the keys (2072 local loads in a launch of 1776 warps).
-template <int D, int NB, bool INT8>
+template <int D, int NB, int KIND>
 constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
 
 // Both products are taken transposed, keys (then dimensions) on the 16-row side of m16n8k16 and query rows on its
@@ -106,18 +112,27 @@ constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
 //
 // CLUSTER: a cluster of eight blocks has an item to itself, each block an eighth of its units, and the blocks' sums meet
 // through distributed shared memory: no scan of the batch, no second launch.
-template <int D, int NB, bool BF, bool INT8, bool CLUSTER, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, NB, INT8> : 1) paged_rows_kernel(const __grid_constant__ AttendParams p) {
+//
+// 4-bit codes: a lane takes D / 4 neighbouring channels of a key and D / 8 of a value.  Masked in place, two of them are the
+// two halves of an f16 operand (nibbles_low, nibbles_high): five instructions for eight codes, where adding a bias and taking
+// it off again in f16 would need nine.  The nibble stands for code + 8; that product is a constant of the query row for S,
+// and for O eight times the sum of the rounded probabilities, which a product with a constant operand adds up.  A channel's
+// factor goes into the query for K and into the result for V.  Query times factor has up to 19 bits: it is taken as the sum of
+// two f16, each with its own product (exact; the tensor cores have the room).
+template <int D, int NB, bool BF, int KIND, bool CLUSTER, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, NB, KIND> : 1) paged_rows_kernel(const __grid_constant__ AttendParams p) {
     constexpr int R = 8 * NB, kThreads = 32 * WARPS;
     // The products' 16-bit type: codes become f16 in five instructions for four and bf16 in eight, so with an int8 cache
     // both products are f16.  A bf16 query row is brought into f16's range by a power of two; elements below 2^-14 of the
     // row's largest then lose bits that are worth less than 2^-25 of it.
-    constexpr bool PBF = BF && !INT8;
-    constexpr int SUB = kRowsSub<NB, INT8>, kUnit = kRowsUnit<NB, INT8>;
+    constexpr bool INT8 = KIND == SASQ_KV_INT8, INT4 = KIND == SASQ_KV_INT4;
+    constexpr bool PBF = BF && KIND == SASQ_KV_16BIT;
+    constexpr int SUB = kRowsSub<NB, KIND>, kUnit = kRowsUnit<NB, KIND>;
     constexpr int kStride = 16 * SUB * WARPS;               // keys from a warp's step to its next
-    constexpr int kWords = INT8 ? D / 64 : D / 32;          // 16-byte words of a key that a lane takes
+    constexpr int kWords = INT4 ? 1 : INT8 ? D / 64 : D / 32;   // 16-byte words of a key that a lane takes (INT4, D = 64: half of one)
     constexpr int kSteps = D / 16;                          // k16 steps of S, and 16-row blocks of O
-    constexpr int VW = D / 8 * (INT8 ? 1 : 2) / 4;          // 32-bit words of a V row that a lane takes: D / 8 elements
+    constexpr int VW = INT4 ? D / 64 : D / 8 * (INT8 ? 1 : 2) / 4;   // 32-bit words of a V row that a lane takes: D / 8 elements
+    constexpr int QL = INT4 ? 2 * kSteps : 1;                // registers of the queries' second parts
 
     __shared__ float sm_m[WARPS][R], sm_l[WARPS][R];
     __shared__ float2 block_ml[R];                            // CLUSTER: the block's references and sums
@@ -156,12 +171,18 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         const int first_row = it.i * R;
         const int rows = min(R, rows_all - first_row);
         const int limit = sch.key_limit(it.s, it.i);
-        const float scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
+        // (4-bit: the operands' 2^24 less the queries' 2^12)
+        const float scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : INT4 ? p.scale * 4096.0f : p.scale;
         if (INT8 && tid == 0 && (scale_is_bad(__ldg(p.c.k_scale + it.h)) || scale_is_bad(__ldg(p.c.v_scale + it.h))))
             atomicMax(p.c.status, (int)SASQ_ERR_BAD_SCALE);
+        if (INT4)
+            for (int d = tid; d < D; d += kThreads)
+                if (scale_is_bad(factor4(__ldg(p.c.k_scale + it.h * D + d))) || scale_is_bad(factor4(__ldg(p.c.v_scale + it.h * D + d))))
+                    atomicMax(p.c.status, (int)SASQ_ERR_BAD_SCALE);
 
         // queries: the fragment of row g of each block of 8 rows, in the order of the keys' words
-        uint32_t qf[NB][2 * kSteps];
+        uint32_t qf[NB][2 * kSteps], ql[NB][QL];
+        float row_off[NB][2];                                // INT4: what the nibbles' bias of 8 adds to their logits
         int row_limit[NB][2];                                // keys that rows 2j, 2j + 1 see
         float row_scale[NB][2];                              // and what turns their products into powers of two
 #pragma unroll
@@ -176,7 +197,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (valid) {
                     // int8: a lane's 16 codes of a key's word feed 16 elements, here in two halves
-                    const int at = INT8 ? 16 * (j + 4 * (w >> 1)) + 8 * (w & 1) : 8 * (j + 4 * w);
+                    const int at = INT4 ? D / 4 * j + 8 * w : INT8 ? 16 * (j + 4 * (w >> 1)) + 8 * (w & 1) : 8 * (j + 4 * w);
                     v = *reinterpret_cast<const uint4*>(qr + at);
                 }
                 qf[nb][4 * w] = v.x;
@@ -204,8 +225,54 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     qf[nb][w] = narrow2<false>(f.x * inv, f.y * inv);
                 }
             }
+            if constexpr (INT4) {
+                float f[4 * kSteps];                         // D / 4 channels, times their factors
+                float big = 0.0f, sum = 0.0f;
+                const float4* fk = reinterpret_cast<const float4*>(p.c.k_scale + it.h * D + D / 4 * j);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) row_scale[nb][e] = scale * __shfl_sync(0xFFFFFFFFu, unit, 4 * (2 * j + e));
+                for (int w = 0; w < kSteps; ++w) {
+                    const float4 s4 = __ldg(fk + w);
+                    const float2 a = widen2<BF>(qf[nb][2 * w]), b = widen2<BF>(qf[nb][2 * w + 1]);
+                    f[4 * w] = a.x * factor4(s4.x);
+                    f[4 * w + 1] = a.y * factor4(s4.y);
+                    f[4 * w + 2] = b.x * factor4(s4.z);
+                    f[4 * w + 3] = b.y * factor4(s4.w);
+                }
+#pragma unroll
+                for (int w = 0; w < 4 * kSteps; ++w) big = fmaxf(big, fabsf(f[w]));
+                big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
+                big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
+                // A power of two brings the row's largest to 2^12 ... 2^13: then the parts, a sixteenth of them included, keep
+                // 2^-33 of it, and what remains of 2^24 for the subnormal operands leaves fp32 its range.
+                const uint32_t top = min(max(__float_as_uint(big) & 0x7F800000u, 0x06800000u), 0x7E800000u);
+                const float inv = __uint_as_float(0x7F000000u + (12u << 23) - top);
+                unit = __uint_as_float(top);
+#pragma unroll
+                for (int w = 0; w < 4 * kSteps; ++w) {
+                    f[w] *= inv;
+                    sum += f[w];
+                    if (w & 1) f[w] *= 0.0625f;              // meets the high nibble
+                }
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                // of eight channels, the pairs that their nibbles stand in: (0, 4), (2, 6) and (1, 5), (3, 7)
+#pragma unroll
+                for (int w = 0; w < 2 * kSteps; ++w) {
+                    const int a = 8 * (w >> 2) + (w & 1) * 2 + (w >> 1 & 1);
+                    const uint32_t hi = narrow2<false>(f[a], f[a + 4]);
+                    const float2 h = widen2<false>(hi);
+                    qf[nb][w] = hi;
+                    ql[nb][w] = narrow2<false>(f[a] - h.x, f[a + 4] - h.y);
+                }
+                sum *= 8.0f * 5.9604644775390625e-8f;        // in the products' units
+#pragma unroll
+                for (int e = 0; e < 2; ++e) row_off[nb][e] = __shfl_sync(0xFFFFFFFFu, sum, 4 * (2 * j + e));
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                row_scale[nb][e] = scale * __shfl_sync(0xFFFFFFFFu, unit, 4 * (2 * j + e));
+                if (INT4) row_off[nb][e] *= row_scale[nb][e];
+            }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int rr = first_row + nb * 8 + 2 * j + e;
@@ -216,20 +283,22 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 
         float o[kSteps][NB][4];
         float m[NB][2], l[NB][2];
+        float lift[NB][4];                                   // INT4: the nibbles' bias in O
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             m[nb][0] = m[nb][1] = -INFINITY;
             l[nb][0] = l[nb][1] = 0.0f;
+            lift[nb][0] = lift[nb][1] = lift[nb][2] = lift[nb][3] = 0.0f;
 #pragma unroll
             for (int k = 0; k < kSteps; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[k][nb][e] = 0.0f;
         }
 
-        const int elem = INT8 ? 1 : 2;
+        auto bytes = [](long long elements) { return INT4 ? elements >> 1 : elements * (INT8 ? 1 : 2); };
         const int* table = p.c.page_table + it.b * p.c.table_stride;
-        const char* kbase = static_cast<const char*>(p.c.k) + it.h * p.c.head_stride * elem;
-        const char* vbase = static_cast<const char*>(p.c.v) + it.h * p.c.head_stride * elem;
+        const char* kbase = static_cast<const char*>(p.c.k) + bytes(it.h * p.c.head_stride);
+        const char* vbase = static_cast<const char*>(p.c.v) + bytes(it.h * p.c.head_stride);
         const int page_mask = (1 << p.c.page_shift) - 1;
         const int last_key = min(it.t1 * kUnit, limit);
         int key = it.t0 * kUnit + warp * 16 * SUB;           // of this warp's step
@@ -242,17 +311,22 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                 atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
                 return -1;
             }
-            return (page * p.c.page_stride + (at & page_mask) * p.c.token_stride) * elem;
+            return bytes(page * p.c.page_stride + (at & page_mask) * p.c.token_stride);
         };
         uint4 kws[SUB][2][kWords];                            // keys g and g + 8
         auto load_k = [&](int at, long long off, uint4 (&kw)[2][kWords]) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const bool in = off >= 0 && at + g + 8 * r < last_key;
-                const char* row = kbase + off + (long long)(g + 8 * r) * p.c.token_stride * elem;
+                const char* row = kbase + off + bytes((g + 8 * r) * p.c.token_stride);
+                if constexpr (INT4 && D == 64) {
+                    const uint2 v = in ? ldg_stream8(row + 8 * j) : make_uint2(0, 0);
+                    kw[r][0] = make_uint4(v.x, v.y, 0, 0);
+                } else {
 #pragma unroll
-                for (int w = 0; w < kWords; ++w)
-                    kw[r][w] = in ? ldg_stream16(row + 16 * (j + 4 * w)) : make_uint4(0, 0, 0, 0);
+                    for (int w = 0; w < kWords; ++w)
+                        kw[r][w] = in ? ldg_stream16(row + 16 * (j + 4 * w)) : make_uint4(0, 0, 0, 0);
+                }
             }
         };
         uint32_t vws[SUB][4][VW];                             // keys 2j, 2j + 1, 2j + 8, 2j + 9
@@ -261,8 +335,10 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             for (int r = 0; r < 4; ++r) {
                 const int kk = 2 * j + (r & 1) + 8 * (r >> 1);
                 const bool in = off >= 0 && at + kk < last_key;
-                const char* row = vbase + off + (long long)kk * p.c.token_stride * elem;
-                if constexpr (VW == 2) {
+                const char* row = vbase + off + bytes(kk * p.c.token_stride);
+                if constexpr (VW == 1) {
+                    vw[r][0] = in ? ldg_stream4(row + 4 * g) : 0u;
+                } else if constexpr (VW == 2) {
                     const uint2 v = in ? ldg_stream8(row + 8 * g) : make_uint2(0, 0);
                     vw[r][0] = v.x;
                     vw[r][1] = v.y;
@@ -304,7 +380,21 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                 for (int w = 0; w < kWords; ++w) {
                     const uint32_t k0[4] = {kws[u][0][w].x, kws[u][0][w].y, kws[u][0][w].z, kws[u][0][w].w};
                     const uint32_t k1[4] = {kws[u][1][w].x, kws[u][1][w].y, kws[u][1][w].z, kws[u][1][w].w};
-                    if constexpr (INT8) {
+                    if constexpr (INT4) {
+#pragma unroll
+                        for (int e = 0; e < D / 32; ++e) {
+                            const uint32_t x0 = k0[e], x1 = k1[e], y0 = x0 >> 8, y1 = x1 >> 8;
+                            const uint32_t low[4] = {nibbles_low(x0), nibbles_low(x1), nibbles_low(y0), nibbles_low(y1)};
+                            const uint32_t high[4] = {nibbles_high(x0), nibbles_high(x1), nibbles_high(y0), nibbles_high(y1)};
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) {
+                                mma_16816(s[u][nb], low, qf[nb][4 * e], qf[nb][4 * e + 1], false);
+                                mma_16816(s[u][nb], high, qf[nb][4 * e + 2], qf[nb][4 * e + 3], false);
+                                mma_16816(s[u][nb], low, ql[nb][4 * e], ql[nb][4 * e + 1], false);
+                                mma_16816(s[u][nb], high, ql[nb][4 * e + 2], ql[nb][4 * e + 3], false);
+                            }
+                        }
+                    } else if constexpr (INT8) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const uint32_t a[4] = {codes_to_pair<false, 0>(k0[e]), codes_to_pair<false, 0>(k1[e]),
@@ -340,7 +430,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int at = key_now + 16 * u + g + 8 * (e >> 1);
-                        s[u][nb][e] = at < row_limit[nb][e & 1] ? s[u][nb][e] * row_scale[nb][e & 1] : -INFINITY;
+                        const float logit = INT4 ? fmaf(s[u][nb][e], row_scale[nb][e & 1], -row_off[nb][e & 1]) : s[u][nb][e] * row_scale[nb][e & 1];
+                        s[u][nb][e] = at < row_limit[nb][e & 1] ? logit : -INFINITY;
                     }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) moves |= fmaxf(s[u][nb][e], s[u][nb][e + 2]) > m[nb][e] + (kRescaleAt + kHeadroom<!PBF>);
@@ -360,6 +451,10 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                         const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m[nb][e] - m_new);
                         m[nb][e] = m_new;
                         l[nb][e] *= f;
+                        if (INT4) {
+                            lift[nb][e] *= f;
+                            lift[nb][e + 2] *= f;
+                        }
 #pragma unroll
                         for (int k = 0; k < kSteps; ++k) {
                             o[k][nb][e] *= f;
@@ -385,7 +480,24 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 
                 // O^T += V^T P^T: rows are dimensions, the contraction is over 16 keys
                 const uint32_t (&vw)[4][VW] = vws[u];
-                if constexpr (INT8) {
+                if constexpr (INT4) {
+                    // eight times the sum of the rounded probabilities, in the units of the low nibbles
+                    const uint32_t eight[4] = {0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma_16816(lift[nb], eight, pf[nb][0], pf[nb][1], false);
+#pragma unroll
+                    for (int w = 0; w < 2 * VW; ++w) {       // four channels: a half of a word
+                        const uint32_t pick = w & 1 ? 0x7632 : 0x5410;
+                        const uint32_t x = __byte_perm(vw[0][w >> 1], vw[1][w >> 1], pick), y = __byte_perm(vw[2][w >> 1], vw[3][w >> 1], pick);
+                        const uint32_t a0[4] = {nibbles_low(x), nibbles_high(x), nibbles_low(y), nibbles_high(y)};
+                        const uint32_t a1[4] = {nibbles_low(x >> 8), nibbles_high(x >> 8), nibbles_low(y >> 8), nibbles_high(y >> 8)};
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) {
+                            mma_16816(o[2 * w][nb], a0, pf[nb][0], pf[nb][1], false);
+                            mma_16816(o[2 * w + 1][nb], a1, pf[nb][0], pf[nb][1], false);
+                        }
+                    }
+                } else if constexpr (INT8) {
 #pragma unroll
                     for (int w = 0; w < VW; ++w) {
                         const uint32_t x0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), x1 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
@@ -431,8 +543,14 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) {
                     // block k holds, of lane group g, the dimensions at and at + 1
-                    const int at = INT8 ? (D / 8) * g + 2 * k : 8 * (g + 8 * (k >> 2)) + 2 * (k & 3);
-                    *reinterpret_cast<float2*>(&sm_o[warp][r][at]) = make_float2(o[k][nb][e], o[k][nb][e + 2]);
+                    const int at = INT8 || INT4 ? (D / 8) * g + 2 * k : 8 * (g + 8 * (k >> 2)) + 2 * (k & 3);
+                    float2 v = make_float2(o[k][nb][e], o[k][nb][e + 2]);
+                    if constexpr (INT4) {
+                        const float2 f = __ldg(reinterpret_cast<const float2*>(p.c.v_scale + it.h * D + at));
+                        v.x = (v.x - lift[nb][e]) * (16777216.0f * factor4(f.x));
+                        v.y = fmaf(v.y, 0.0625f, -lift[nb][e]) * (16777216.0f * factor4(f.y));
+                    }
+                    *reinterpret_cast<float2*>(&sm_o[warp][r][at]) = v;
                 }
             }
         __syncthreads();
@@ -541,7 +659,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
     const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const PartItem pi = p.part_items[c];
     if (pi.last < 0) return;
-    const float vs = p.c.v_scale != nullptr ? __ldg(p.c.v_scale + pi.h) : 1.0f;
+    const float vs = p.c.kind == SASQ_KV_INT8 ? __ldg(p.c.v_scale + pi.h) : 1.0f;      // (4-bit: already in the parts)
     constexpr int kStep = WIDE ? 8 : 1;                        // parts from one of a warp to its next
     for (int r = WIDE ? blockIdx.y : blockIdx.y * 8 + warp; r < R; r += WIDE ? gridDim.y : gridDim.y * 8) {
         const int item_row = r / TILE * pi.tile_rows + r % TILE;
