@@ -345,6 +345,28 @@ SASQ_API int sasq_static_w8a8_linear_multi_launches(int count, const sasq_linear
 SASQ_API int sasq_static_w8a8_linear_tiles(int64_t T, int64_t N, int num_pairs, int pair_id, int32_t* tiles_host,
                                            int cap);
 
+/* Linear layer with 4-bit weights and group factors, for the few tokens of a decode step: bound by the weights, half a byte
+ * each.  Groups are `group` consecutive columns; c[n,k] in [-8, 7] are codes of Eq. 1 with b = 4:
+ *   y[t,n] = narrow( sum_g s[n,g] * sum_{k in group g} x[t,k] c[n,k] (+ bias[n]) )      products exact, sums in fp32
+ *                                                                                     (order unspecified, but fixed)
+ * x: [T, K] of `dt`, as it is.  w: [N, K / 2] bytes, column 2i in the low half of byte i, two's complement.  w_scale:
+ * [N, K / group] of `dt`.  bias: [N] of `dt` or NULL, added in fp32.  y: [T, N] of `dt`, must not overlap x.
+ * group: 32, 64 or 128, a divisor of K; any N; otherwise SASQ_ERR_UNSUPPORTED (also T > 2^20, N > 2^30, K > 2^24).  Any T
+ * is served, 32 tokens at a time: for many tokens the W8A8 linears are the faster ones.  The weights are frozen: w and
+ * w_scale are read as soon as the kernel is resident, which can be before an earlier call of this library on the same stream
+ * has finished; do not hand over a buffer that such a call is still writing (sasq_quantize_weight_w4 does not let its successor
+ * start early).  A non-finite x reaches only its own token's row of y.  No workspace. */
+SASQ_API int sasq_w4_linear(const void* x, const uint8_t* w, const void* w_scale, const void* bias, void* y, int64_t T,
+                            int64_t N, int64_t K, int64_t group, int dt, void* stream);
+
+/* Weights for sasq_w4_linear from w: [N, K] fp32 (set-up, not on the hot path):
+ *   w_scale[n,g] = narrow( max_{k in group g} |w[n,k]| / 7 )      of `dt`; 1 where that is 0, not finite (bfloat16) or has no
+ *                                                                 finite reciprocal; at most float16's largest number
+ *   c[n,k]       = clamp( rint( w[n,k] * fl32(1 / w_scale[n,g]) ), -8, 7 )
+ * w_int: [N, K / 2] bytes, w_scale: [N, K / group].  group as above. */
+SASQ_API int sasq_quantize_weight_w4(const float* w, uint8_t* w_int, void* w_scale, int64_t N, int64_t K, int64_t group,
+                                     int dt, void* stream);
+
 /* ---- Paged key/value cache: what lies between the q/k/v and the o linears of a decoder layer when serving ----
  *
  * A cache is a pool of pages; a page holds `page_size` consecutive positions of ONE sequence, for every KV head.

@@ -29,7 +29,7 @@ __all__ = [
     "sasq_static_w8a8_linear_multi", "sasq_static_w8a8_linear_multi_launches", "sasq_set_gang_launch",
     "sasq_debug_int8_issue_rate", "LinearProblems", "QuantTensors",
     "SASQ_KV_16BIT", "SASQ_KV_INT8", "SASQ_KV_INT4", "KVCacheStruct", "KVBatchStruct", "KVCache", "PagedBatch", "sasq_rope_kv_append",
-    "sasq_paged_attention_workspace", "sasq_paged_attention",
+    "sasq_paged_attention_workspace", "sasq_paged_attention", "sasq_w4_linear", "sasq_quantize_weight_w4",
 ]
 
 SASQ_F16 = 0
@@ -137,6 +137,10 @@ def load_library() -> ctypes.CDLL:
     L.sasq_static_w8a8_linear_per_channel_workspace.argtypes = [i64, i64, i64]
     L.sasq_static_w8a8_linear_per_channel.restype = i32
     L.sasq_static_w8a8_linear_per_channel.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, i32, vp, sz, vp]
+    L.sasq_w4_linear.restype = i32
+    L.sasq_w4_linear.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp]
+    L.sasq_quantize_weight_w4.restype = i32
+    L.sasq_quantize_weight_w4.argtypes = [vp, vp, vp, i64, i64, i64, i32, vp]
     L.sasq_dynamic_w8a8_linear_workspace.restype = sz
     L.sasq_dynamic_w8a8_linear_workspace.argtypes = [i64, i64, i64]
     L.sasq_dynamic_w8a8_linear.restype = i32
@@ -715,6 +719,49 @@ def sasq_fakequant_fwd_bwd_static(x, grad_y, y, grad_x, grad_scale, scale, bits:
                                                         _ptr(grad_scale), int(bool(accumulate)), x.numel(), _dt(x),
                                                         _ptr(scale), int(bits), _stream(stream)),
            "sasq_fakequant_fwd_bwd_static")
+
+
+def _on(device: int, *pairs) -> None:
+    """Tensors of a call that launches on the current device: contiguous, on that device, of the given dtypes."""
+    if _current_device() != device:
+        raise ValueError(f"the tensors lie on cuda:{device}, the current device is cuda:{_current_device()} (enter "
+                         f"torch.cuda.device({device}))")
+    for t, name, dtype in pairs:
+        if t is not None:
+            _flat(t, name, device, dtype)
+
+
+def sasq_w4_linear(x, w, w_scale, y, bias=None, stream=None) -> None:
+    """y [T, N] = x [T, K] times 4-bit weights: w [N, K / 2] uint8 (column 2i in the low half of byte i), w_scale
+    [N, K / group] of x's dtype with group 32, 64 or 128; bias [N] or None."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("x must be a CUDA tensor")
+    device, dt = x.get_device(), x.dtype
+    _on(device, (x, "x", None), (w, "w", torch.uint8), (w_scale, "w_scale", dt), (y, "y", dt), (bias, "bias", dt))
+    if x.dim() != 2 or w.dim() != 2 or w_scale.dim() != 2 or y.dim() != 2:
+        raise ValueError("x, w, w_scale and y must be matrices")
+    (T, K), (N, half), (rows, groups) = x.shape, w.shape, w_scale.shape
+    if K != 2 * half or rows != N or groups <= 0 or K % groups != 0 or y.shape != (T, N) or (bias is not None and bias.shape != (N,)):
+        raise ValueError(f"x [{T}, K], w [N, K / 2], w_scale [N, K / group], y [{T}, N] and bias [N] do not fit together: "
+                         f"{tuple(x.shape)}, {tuple(w.shape)}, {tuple(w_scale.shape)}, {tuple(y.shape)}")
+    status = (_lib or load_library()).sasq_w4_linear(x.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _ptr(bias), y.data_ptr(), T, N, K,
+                                                     K // groups, _dt(x), _stream_of(device, stream))
+    if status != 0 or _DEBUG_STATUS:
+        _check(status, "sasq_w4_linear")
+
+
+def sasq_quantize_weight_w4(w, w_int, w_scale, stream=None) -> None:
+    """w [N, K] fp32 -> w_int [N, K / 2] uint8 and w_scale [N, K / group] fp16 or bf16, for sasq_w4_linear."""
+    if not isinstance(w, torch.Tensor) or not w.is_cuda:
+        raise TypeError("w must be a CUDA tensor")
+    device = w.get_device()
+    _on(device, (w, "w", torch.float32), (w_int, "w_int", torch.uint8), (w_scale, "w_scale", None))
+    if w.dim() != 2 or w_scale.dim() != 2 or w_int.shape != (w.shape[0], w.shape[1] // 2) or w.shape[1] % 2 or \
+            w_scale.shape[0] != w.shape[0] or w_scale.shape[1] <= 0 or w.shape[1] % w_scale.shape[1] != 0:
+        raise ValueError("w must be [N, K], w_int [N, K / 2] and w_scale [N, K / group]")
+    N, K = w.shape
+    _check(load_library().sasq_quantize_weight_w4(w.data_ptr(), w_int.data_ptr(), w_scale.data_ptr(), N, K, K // w_scale.shape[1],
+                                                  _dt(w_scale), _stream_of(device, stream)), "sasq_quantize_weight_w4")
 
 
 # ---------------------------------------------------------------------------
