@@ -21,9 +21,9 @@ def problem(T, N, K, group, dtype, bias=False, seed=0):
 
 
 def exact(x, codes, scale, bias):
-    """y in 64 bits and how far off the kernel may be.  More than 8 tokens: products are exact, and a sum of K of them, taken by
+    """y in 64 bits and how far off the kernel may be.  More than 2 tokens: products are exact, and a sum of K of them, taken by
     groups and then over the groups, with K + K / group + 32 additions at most, is off by 2^-23 (the tensor cores may truncate) of
-    the sum of the magnitudes each.  Up to 8 tokens: an x is off by at most 2^-22 of the largest of its 256 columns, a group's
+    the sum of the magnitudes each.  Up to 2 tokens: an x is off by at most 2^-22 of the largest of its 256 columns, a group's
     sum is exact, and over the groups there are at most K / group + 40 roundings of 2^-24; the three digits' magnitudes add up to
     at most twice the value's (and 2^-13 of the largest for a value that has fewer).  One narrowing, which may also underflow."""
     N, K = codes.shape
@@ -32,7 +32,7 @@ def exact(x, codes, scale, bias):
     y, size = x.double() @ w.T, x.double().abs() @ w.abs().T
     if bias is not None:
         y, size = y + bias.double(), size + bias.double().abs()
-    if x.shape[0] > 8:
+    if x.shape[0] > 2:
         inner = (K + K // group + 32) * 2.0 ** -23 * size
     else:
         most = torch.nn.functional.pad(x.double().abs(), (0, -K % 256)).view(x.shape[0], -1, 256).amax(dim=2)
