@@ -14,6 +14,16 @@
 namespace sasq {
 namespace {
 
+#ifndef S2
+#define S2 4
+#define S8 3
+#define S16 3
+#endif
+#ifndef WARPS2
+#define WARPS2 8
+#define WARPS8 16
+#define WARPS16 8
+#endif
 struct W4Params {
     const uint16_t* x;          // [T, K]
     const uint8_t* w;           // [N, K / 2]
@@ -168,7 +178,8 @@ __device__ __forceinline__ void window_words(uint32_t row_base, int turn, int j,
 template <int TOKENS, int STAGES, int G>
 struct W4Shape {
     static constexpr bool kDigits = TOKENS == 2;
-    static constexpr int kWarps = 8;
+    static constexpr int kWarps = TOKENS == 2 ? WARPS2 : TOKENS == 8 ? WARPS8 : WARPS16, kThreads = 32 * kWarps;
+    static constexpr int kPerSm = 16 / kWarps;             // blocks of an SM by their registers
     static constexpr int kRows = kDigits ? 16 : 32;        // of a tile
     static constexpr int kWindow = kDigits ? 256 : 128;    // columns of a step
     static constexpr int kRowBytes = kWindow / 2;
@@ -188,7 +199,7 @@ struct W4Shape {
 // tile or its run ends.  The tokens lie in shared memory, and each warp streams its weights through a ring of its own
 // (STAGES - 1 windows under way): no barrier until the sums of all the block's rows meet.
 template <int TOKENS, int STAGES, bool BF, int G>
-__global__ void __launch_bounds__(256, 2) w4_linear_kernel(const __grid_constant__ W4Params p, const __grid_constant__ Bits bits_) {
+__global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<TOKENS, STAGES, G>::kPerSm) w4_linear_kernel(const __grid_constant__ W4Params p, const __grid_constant__ Bits bits_) {
     using Shape = W4Shape<TOKENS, STAGES, G>;
     constexpr bool kDigits = Shape::kDigits;
     constexpr int kWindow = Shape::kWindow, kRows = Shape::kRows, kRowBytes = Shape::kRowBytes;
@@ -396,6 +407,19 @@ __global__ void __launch_bounds__(256, 2) w4_linear_kernel(const __grid_constant
     uint32_t at = ring;                                    // the slot that is read next
     for (int pass = tile_begin; pass < tile_end; pass += p.pass_tiles) {
         const int rows = kRows * min(p.pass_tiles, tile_end - pass);
+        // every token and row once among the threads of `of` blocks; with many tokens a warp takes 32 rows of one at a time
+        auto each_row = [&](int block, int of, auto&& f) {
+            if constexpr (kDigits) {
+                for (int t = 0; t < tokens; ++t)
+                    for (int row = block * Shape::kThreads + tid; row < rows; row += of * Shape::kThreads) f(t, row);
+            } else {
+                for (int t = 0, row = 32 * (block * WK + warp) + lane;; row += 32 * WK * of) {
+                    for (; row - lane >= rows && t < tokens; ++t) row -= rows;
+                    if (t >= tokens) break;
+                    f(t, row);
+                }
+            }
+        };
         for (int part = 0; part < p.parts; ++part) {
             Run r = run_of(pass, part);
             const int windows = r.windows;
@@ -571,38 +595,38 @@ __global__ void __launch_bounds__(256, 2) w4_linear_kernel(const __grid_constant
             int tile_of[2 * WK];
 #pragma unroll
             for (int k = 0; k < 2 * WK; ++k) tile_of[k] = piece_tile[k];
-            for (int t = 0; t < tokens; ++t)
-                for (int row = tid; row < rows; row += 256) {
-                    float* const cell = sums + t * sum_pitch + row;
-                    float v = 0.0f;
-                    bool cut = windows == 0;
+            const bool out = p.split == 1 && part + 1 == p.parts;
+            each_row(0, 1, [&](int t, int row) {
+                float* const cell = sums + t * sum_pitch + row;
+                const float* const mine = pieces + t * Shape::kPiece + row % kRows;
+                float v = 0.0f;
+                bool cut = windows == 0;
 #pragma unroll
-                    for (int k = 0; k < 2 * WK; ++k)
-                        if (tile_of[k] == row / kRows) {
-                            v += pieces[(k * p.x_rows + t) * Shape::kPiece + row % kRows];
-                            cut = true;
-                        }
-                    if (!cut) v = *cell;
-                    else if (part > 0) v += *cell;
-                    if (p.split == 1 && part + 1 == p.parts) store(pass, t, row, v);
-                    else if (cut) *cell = v;
-                }
+                for (int k = 0; k < 2 * WK; ++k)
+                    if (tile_of[k] == row / kRows) {
+                        v += mine[k * p.x_rows * Shape::kPiece];
+                        cut = true;
+                    }
+                if (!cut) v = *cell;
+                else if (part > 0) v += *cell;
+                if (out) store(pass, t, row, v);
+                else if (cut) *cell = v;
+            });
         }
         if (p.split > 1) {
             ptx::cluster_sync_all();
-            for (int t = 0; t < tokens; ++t)
-                for (int row = rank * 256 + tid; row < rows; row += p.split * 256) {
-                    const uint32_t here = ptx::smem_u32(&sums[t * sum_pitch + row]);
-                    float v = 0.0f;
-                    for (int k = 0; k < p.split; ++k) {
-                        uint32_t peer;
-                        float part;
-                        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(here), "r"(k));
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(peer));
-                        v += part;
-                    }
-                    store(pass, t, row, v);
+            each_row(rank, p.split, [&](int t, int row) {
+                const uint32_t here = ptx::smem_u32(&sums[t * sum_pitch + row]);
+                float v = 0.0f;
+                for (int k = 0; k < p.split; ++k) {
+                    uint32_t peer;
+                    float part;
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(here), "r"(k));
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(peer));
+                    v += part;
                 }
+                store(pass, t, row, v);
+            });
             ptx::cluster_sync_all();                       // nobody goes on, or leaves, while its sums are being read
         }
     }
@@ -649,13 +673,13 @@ __global__ void __launch_bounds__(256) quantize_w4_kernel(const float* __restric
 constexpr int kMaxSmem = 227 * 1024, kSmSmem = 228 * 1024;     // of a block, and of an SM (each block takes 1 KB more)
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-__global__ void __launch_bounds__(256, 2) cluster_room_kernel() {}
+__global__ void __launch_bounds__(512, 1) cluster_room_kernel() {}
 
 // Clusters of `split` blocks, `per_sm` of them on an SM by their shared memory, that the device holds at once: fewer than the
 // blocks alone would allow, for a cluster stays within a part of the chip (B200: 33 clusters of 8 at two an SM, not 37).
-int cluster_slots(int split, int per_sm, int sms) {
+int cluster_slots(int split, int per_sm, int threads, int sms) {
     if (split == 1) return sms * per_sm;
-    static std::atomic<int> known[64][4][4];
+    static std::atomic<int> known[64][4][4];               // (threads do not matter: shared memory decides)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 1;
     const int log = split == 2 ? 1 : split == 4 ? 2 : 3;
@@ -664,7 +688,7 @@ int cluster_slots(int split, int per_sm, int sms) {
         int n = 0;
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3((unsigned)(split * sms));
-        cfg.blockDim = dim3(256);
+        cfg.blockDim = dim3((unsigned)threads);
         cfg.dynamicSmemBytes = kSmSmem / per_sm - 1024;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -693,9 +717,9 @@ W4Plan plan_w4(int tiles_all, int windows_all, int x_rows, int chunks, int sms) 
     long long least = -1;
     for (int split = 1; split <= 8 && split <= windows_all; split *= 2) {
         const int windows = ceil_div(windows_all, split);
-        for (int per_sm = 2; per_sm >= 1; --per_sm) {
+        for (int per_sm = Shape::kPerSm; per_sm >= 1; --per_sm) {
             const long long room = kSmSmem / per_sm - 1024 - Shape::kRing;
-            const int slots = cluster_slots(split, per_sm, sms) / chunks;
+            const int slots = cluster_slots(split, per_sm, Shape::kThreads, sms) / chunks;
             const int clusters = tiles_all < slots ? tiles_all : slots < 1 ? 1 : slots;
             const int tiles = ceil_div(tiles_all, clusters);
             // sums of the block's rows get up to half of the room, tokens the rest
@@ -707,10 +731,10 @@ W4Plan plan_w4(int tiles_all, int windows_all, int x_rows, int chunks, int sms) 
             const int fit = (int)(x_room / (long long)Shape::x_bytes(x_rows, 1)), part = fit < windows ? fit : windows;
             const int parts = ceil_div(windows, part);
             const long long run = (long long)passes * parts * (ceil_div((long long)pass * part, Shape::kWarps) + 1);
-            const long long busy = per_sm * (Shape::kDigits ? 400 : TOKENS == 8 ? 700 : 800);
+            const long long busy = per_sm * Shape::kWarps / 8 * (Shape::kDigits ? 400 : TOKENS == 8 ? 700 : 800);
             const long long step = busy > 900 ? busy : 900;
             const long long staged = (long long)ceil_div((long long)windows * x_rows, Shape::kWarps) * (parts > 1 ? passes : 1);
-            const long long cost = run * step + staged * per_sm * (Shape::kDigits ? 400 : 60) + passes * (split > 1 ? 3000 : 500) +
+            const long long cost = run * step + staged * per_sm * Shape::kWarps / 8 * (Shape::kDigits ? 400 : 60) + passes * (split > 1 ? 3000 : 500) +
                                    (parts > 1 ? (long long)passes * parts * 1500 : 0);
             if (least >= 0 && cost >= least) continue;
             least = cost;
@@ -756,7 +780,7 @@ cudaError_t launch_w4(W4Params p, int sms, cudaStream_t st) {
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(k.plan.clusters * p.split), (unsigned)chunks);
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(Shape::kThreads);
     cfg.dynamicSmemBytes = k.plan.smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -769,15 +793,11 @@ cudaError_t launch_w4(W4Params p, int sms, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, w4_linear_kernel<TOKENS, STAGES, BF, G>, p, kBits<BF>);
 }
 
-#ifndef W4_STAGES
-#define W4_STAGES 4, 3, 3
-#endif
 template <bool BF, int G>
 cudaError_t launch_tokens(const W4Params& p, int sms, cudaStream_t st) {
-    constexpr int kStages[3] = {W4_STAGES};
-    if (p.T <= 2) return launch_w4<2, kStages[0], BF, G>(p, sms, st);
-    if (p.T <= 8) return launch_w4<8, kStages[1], BF, G>(p, sms, st);
-    return launch_w4<16, kStages[2], BF, G>(p, sms, st);
+    if (p.T <= 2) return launch_w4<2, S2, BF, G>(p, sms, st);
+    if (p.T <= 8) return launch_w4<8, S8, BF, G>(p, sms, st);
+    return launch_w4<16, S16, BF, G>(p, sms, st);
 }
 template <bool BF>
 cudaError_t launch_group(const W4Params& p, int group, int sms, cudaStream_t st) {
