@@ -318,6 +318,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.item_rows = pl.rows;
     p.tile_bound = pl.tile_bound;
     p.wait_limit = debug_wait_limit();
+    p.flips = kFlips;
     p.part_items = static_cast<PartItem*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + l.ml);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.o);

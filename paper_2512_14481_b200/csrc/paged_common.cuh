@@ -266,10 +266,23 @@ __device__ __forceinline__ uint32_t codes_to_pair(uint32_t w) {
 __device__ __forceinline__ float factor4(float s) { return __bfloat162float(__float2bfloat16_rn(s)); }
 
 // 4-bit codes as f16, without arithmetic: a nibble that is alone in the low byte of a 16-bit half is a subnormal number, 2^-24
-// times the nibble (low nibble of the byte) or 2^-20 times (high nibble).  The code's sign bit is flipped on the way, so the
-// nibble stands for u = code + 8.
-__device__ __forceinline__ uint32_t nibbles_low(uint32_t w) { return (w & 0x000F000Fu) ^ 0x00080008u; }
-__device__ __forceinline__ uint32_t nibbles_high(uint32_t w) { return (w & 0x00F000F0u) ^ 0x00800080u; }
+// times the nibble (low nibble of the byte) or 2^-20 times (high nibble).  The code's sign bit is flipped on the way (`flip`), so
+// the nibble stands for u = code + 8.  The bits to flip come as kernel parameters: a logic instruction takes one immediate, and
+// of a mask and another constant the compiler makes two instructions (measured).
+struct Flips {
+    uint32_t low, high;
+};
+constexpr Flips kFlips{0x00080008u, 0x00800080u};
+__device__ __forceinline__ uint32_t nibbles_low(uint32_t w, const Flips& f) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6A;" : "=r"(d) : "r"(w), "r"(f.low));      // (w & mask) ^ flip
+    return d;
+}
+__device__ __forceinline__ uint32_t nibbles_high(uint32_t w, const Flips& f) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0x6A;" : "=r"(d) : "r"(w), "r"(f.high));
+    return d;
+}
 
 // 2^x by the hardware's approximation (2^-inf = 0)
 __device__ __forceinline__ float exp2_approx(float x) {

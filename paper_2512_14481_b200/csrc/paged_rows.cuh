@@ -22,14 +22,19 @@ struct AttendParams {
     float2* part_ml;            // [2 * max_blocks][R]: maximum (log2 units) and sum
     float* part_o;              // [2 * max_blocks][R][D]
     long long wait_limit;
+    Flips flips;                // 4-bit codes
 };
 
 namespace {
 
 // Blocks of 16 keys of a warp's step: with 8 rows as many bytes are under way whatever the cache holds (16 rows' sums leave
 // no registers for that), and keys of a unit: a step of four warps.
+#ifndef SUB4
+#define SUB4 2
+#define BLK4 3
+#endif
 template <int NB, int KIND>
-constexpr int kRowsSub = NB != 1 || KIND == SASQ_KV_16BIT ? 1 : 2;
+constexpr int kRowsSub = NB != 1 || KIND == SASQ_KV_16BIT ? 1 : KIND == SASQ_KV_INT4 ? SUB4 : 2;
 template <int NB, int KIND>
 constexpr int kRowsUnit = 64 * kRowsSub<NB, KIND>;
 constexpr int kClusterBlocks = 8;
@@ -95,11 +100,27 @@ __device__ __forceinline__ uint32_t ldg_stream4(const void* p) {
     asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
 }
+// the first 1, 2 or 4 words
+template <int WORDS>
+__device__ __forceinline__ uint4 load_codes(const void* p) {
+    if constexpr (WORDS == 4) return ldg_stream16(p);
+    if constexpr (WORDS == 2) {
+        const uint2 v = ldg_stream8(p);
+        return make_uint4(v.x, v.y, 0, 0);
+    }
+    return make_uint4(ldg_stream4(p), 0, 0, 0);
+}
+__device__ __forceinline__ void mma_16832(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+constexpr uint32_t kMagic = 0x4B400000u;                     // 1.5 * 2^23
 
 // Blocks that an SM holds: as many as the registers of the fragments leave room for.  At this bound the variants for 8 rows
 // over int8 codes spill 4 to 20 bytes a thread, outside the loop over the keys (2072 local loads in a launch of 1776 warps).
 template <int D, int NB, int KIND>
-constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
+constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : KIND == SASQ_KV_INT4 ? (D == 128 ? BLK4 : BLK4 + 1) : D == 128 ? 3 : 4;
 
 // Both products are taken transposed, keys (then dimensions) on the 16-row side of m16n8k16 and query rows on its
 // 8-column side, so that one query row wastes 7/8 of the instruction and not 15/16, and neither K nor V passes through
@@ -113,12 +134,15 @@ constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
 // CLUSTER: a cluster of eight blocks has an item to itself, each block an eighth of its units, and the blocks' sums meet
 // through distributed shared memory: no scan of the batch, no second launch.
 //
-// 4-bit codes: a lane takes D / 4 neighbouring channels of a key and D / 8 of a value.  Masked in place, two of them are the
-// two halves of an f16 operand (nibbles_low, nibbles_high): five instructions for eight codes, where adding a bias and taking
-// it off again in f16 would need nine.  The nibble stands for code + 8; that product is a constant of the query row for S,
-// and for O eight times the sum of the rounded probabilities, which a product with a constant operand adds up.  A channel's
-// factor goes into the query for K and into the result for V.  Query times factor has up to 19 bits: it is taken as the sum of
-// two f16, each with its own product (exact; the tensor cores have the room).
+// 4-bit codes: a lane takes D / 4 neighbouring channels of a key and D / 8 of a value; a channel's factor goes into the query for K
+// and into the result for V.  What bounds these kernels is the logic pipe, which runs at half the others' rate.
+//   S: as signed bytes, 16 times the code, eight codes are a shift and two masks, and one s8 product of m16n8k32 takes all of them.
+//      Query times factor becomes an integer, a multiple of 2^-22 of the row's largest (a bf16 or f16 query times a bf16 factor has 16
+//      or 19 bits), whose three digits to the base 256, from -128 to 127, each have their product.  The sums are exact integers of at
+//      most 2^21; they start at the bits of the float 1.5 * 2^23, so that the float they end as is that plus the sum.
+//   O: masked in place, two nibbles are the two halves of an f16 operand (nibbles_low, nibbles_high): six instructions for eight codes
+//      of two keys each.  The nibble stands for code + 8: eight times the sum of the rounded probabilities is taken off again,
+//      which a product with a constant operand adds up.
 template <int D, int NB, bool BF, int KIND, bool CLUSTER, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, NB, KIND> : 1) paged_rows_kernel(const __grid_constant__ AttendParams p) {
     constexpr int R = 8 * NB, kThreads = 32 * WARPS;
@@ -132,7 +156,6 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
     constexpr int kWords = INT4 ? 1 : INT8 ? D / 64 : D / 32;   // 16-byte words of a key that a lane takes (INT4, D = 64: half of one)
     constexpr int kSteps = D / 16;                          // k16 steps of S, and 16-row blocks of O
     constexpr int VW = INT4 ? D / 64 : D / 8 * (INT8 ? 1 : 2) / 4;   // 32-bit words of a V row that a lane takes: D / 8 elements
-    constexpr int QL = INT4 ? 2 * kSteps : 1;                // registers of the queries' second parts
 
     __shared__ float sm_m[WARPS][R], sm_l[WARPS][R];
     __shared__ float2 block_ml[R];                            // CLUSTER: the block's references and sums
@@ -140,6 +163,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
     pdl_launch_dependents();
+    const Flips flips = p.flips;
     pdl_wait();
     const Schedule<kUnit, kRowsItemCost> sch{R, p.group, p.causal, p.c.kv_heads};
     const int rank = blockIdx.x % kClusterBlocks;             // CLUSTER: of the block in its cluster
@@ -171,8 +195,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         const int first_row = it.i * R;
         const int rows = min(R, rows_all - first_row);
         const int limit = sch.key_limit(it.s, it.i);
-        // (4-bit: the operands' 2^24 less the queries' 2^12)
-        const float scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : INT4 ? p.scale * 4096.0f : p.scale;
+        const float scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
         if (INT8 && tid == 0 && (scale_is_bad(__ldg(p.c.k_scale + it.h)) || scale_is_bad(__ldg(p.c.v_scale + it.h))))
             atomicMax(p.c.status, (int)SASQ_ERR_BAD_SCALE);
         if (INT4)
@@ -181,8 +204,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     atomicMax(p.c.status, (int)SASQ_ERR_BAD_SCALE);
 
         // queries: the fragment of row g of each block of 8 rows, in the order of the keys' words
-        uint32_t qf[NB][2 * kSteps], ql[NB][QL];
-        float row_off[NB][2];                                // INT4: what the nibbles' bias of 8 adds to their logits
+        uint32_t qf[NB][2 * kSteps];
+        uint32_t qd[NB][3][INT4 ? kSteps : 1];               // INT4: the queries' digits, in their place
         int row_limit[NB][2];                                // keys that rows 2j, 2j + 1 see
         float row_scale[NB][2];                              // and what turns their products into powers of two
 #pragma unroll
@@ -227,7 +250,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
             if constexpr (INT4) {
                 float f[4 * kSteps];                         // D / 4 channels, times their factors
-                float big = 0.0f, sum = 0.0f;
+                uint32_t seen = 0;                           // NaN compares as the largest
                 const float4* fk = reinterpret_cast<const float4*>(p.c.k_scale + it.h * D + D / 4 * j);
 #pragma unroll
                 for (int w = 0; w < kSteps; ++w) {
@@ -239,39 +262,32 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     f[4 * w + 3] = b.y * factor4(s4.w);
                 }
 #pragma unroll
-                for (int w = 0; w < 4 * kSteps; ++w) big = fmaxf(big, fabsf(f[w]));
-                big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
-                big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
-                // A power of two brings the row's largest to 2^12 ... 2^13: then the parts, a sixteenth of them included, keep
-                // 2^-33 of it, and what remains of 2^24 for the subnormal operands leaves fp32 its range.
-                const uint32_t top = min(max(__float_as_uint(big) & 0x7F800000u, 0x06800000u), 0x7E800000u);
-                const float inv = __uint_as_float(0x7F000000u + (12u << 23) - top);
-                unit = __uint_as_float(top);
+                for (int w = 0; w < 4 * kSteps; ++w) seen = max(seen, __float_as_uint(f[w]) & 0x7FFFFFFFu);
+                seen = max(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, 1));
+                seen = max(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, 2));
+                // the row's largest becomes 2^21 ... 2^22
+                const uint32_t top = max(seen & 0x7F800000u, 26u << 23);
+                const float up = __uint_as_float((275u << 23) - top);
+                unit = seen >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top - (25u << 23));    // less 16 times the code
 #pragma unroll
-                for (int w = 0; w < 4 * kSteps; ++w) {
-                    f[w] *= inv;
-                    sum += f[w];
-                    if (w & 1) f[w] *= 0.0625f;              // meets the high nibble
+                for (int w = 0; w < kSteps / 2; ++w) {       // a word's eight channels
+                    uint32_t d[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        d[i] = __float_as_uint(fmaf(f[8 * w + i], up, __uint_as_float(kMagic))) - kMagic + 0x00808080u;
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {            // the even, then the odd ones
+                        const uint32_t ab = __byte_perm(d[o], d[2 + o], 0x5140), cd = __byte_perm(d[4 + o], d[6 + o], 0x5140);
+                        qd[nb][0][2 * w + o] = __byte_perm(ab, cd, 0x5410) ^ 0x80808080u;
+                        qd[nb][1][2 * w + o] = __byte_perm(ab, cd, 0x7632) ^ 0x80808080u;
+                        qd[nb][2][2 * w + o] =
+                            __byte_perm(__byte_perm(d[o], d[2 + o], 0x0062), __byte_perm(d[4 + o], d[6 + o], 0x0062), 0x5410) ^ 0x80808080u;
+                    }
                 }
-                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-                // of eight channels, the pairs that their nibbles stand in: (0, 4), (2, 6) and (1, 5), (3, 7)
-#pragma unroll
-                for (int w = 0; w < 2 * kSteps; ++w) {
-                    const int a = 8 * (w >> 2) + (w & 1) * 2 + (w >> 1 & 1);
-                    const uint32_t hi = narrow2<false>(f[a], f[a + 4]);
-                    const float2 h = widen2<false>(hi);
-                    qf[nb][w] = hi;
-                    ql[nb][w] = narrow2<false>(f[a] - h.x, f[a + 4] - h.y);
-                }
-                sum *= 8.0f * 5.9604644775390625e-8f;        // in the products' units
-#pragma unroll
-                for (int e = 0; e < 2; ++e) row_off[nb][e] = __shfl_sync(0xFFFFFFFFu, sum, 4 * (2 * j + e));
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 row_scale[nb][e] = scale * __shfl_sync(0xFFFFFFFFu, unit, 4 * (2 * j + e));
-                if (INT4) row_off[nb][e] *= row_scale[nb][e];
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -281,6 +297,13 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
         }
 
+        // keys that every row sees (rows behind the last ones see no fewer)
+        int seen_by_all = limit;
+        if (INT4) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) seen_by_all = min(seen_by_all, min(row_limit[nb][0], row_limit[nb][1]));
+            seen_by_all = __reduce_min_sync(0xFFFFFFFFu, seen_by_all);
+        }
         float o[kSteps][NB][4];
         float m[NB][2], l[NB][2];
         float lift[NB][4];                                   // INT4: the nibbles' bias in O
@@ -313,16 +336,27 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
             return bytes(page * p.c.page_stride + (at & page_mask) * p.c.token_stride);
         };
+        // INT4: where this lane's words lie behind a step's first row
+        const long long one_row = bytes(p.c.token_stride), eight_rows = 8 * one_row;
+        const char* const klane = kbase + g * one_row + D / 8 * j;
+        const char* const vlane = vbase + 2 * j * one_row + D / 16 * g;
         uint4 kws[SUB][2][kWords];                            // keys g and g + 8
         auto load_k = [&](int at, long long off, uint4 (&kw)[2][kWords]) {
+            if constexpr (INT4) {
+                const char* row = klane + off;
+                if (off >= 0 && at + 16 <= last_key) {         // all there, which a test of each costs much of a step
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const bool in = off >= 0 && at + g + 8 * r < last_key;
-                const char* row = kbase + off + bytes((g + 8 * r) * p.c.token_stride);
-                if constexpr (INT4 && D == 64) {
-                    const uint2 v = in ? ldg_stream8(row + 8 * j) : make_uint2(0, 0);
-                    kw[r][0] = make_uint4(v.x, v.y, 0, 0);
+                    for (int r = 0; r < 2; ++r) kw[r][0] = load_codes<D / 32>(row + r * eight_rows);
                 } else {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        kw[r][0] = off >= 0 && at + g + 8 * r < last_key ? load_codes<D / 32>(row + r * eight_rows) : make_uint4(0, 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const bool in = off >= 0 && at + g + 8 * r < last_key;
+                    const char* row = kbase + off + bytes((g + 8 * r) * p.c.token_stride);
 #pragma unroll
                     for (int w = 0; w < kWords; ++w)
                         kw[r][w] = in ? ldg_stream16(row + 16 * (j + 4 * w)) : make_uint4(0, 0, 0, 0);
@@ -331,25 +365,36 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         };
         uint32_t vws[SUB][4][VW];                             // keys 2j, 2j + 1, 2j + 8, 2j + 9
         auto load_v = [&](int at, long long off, uint32_t (&vw)[4][VW]) {
+            if constexpr (INT4) {
+                const char* row = vlane + off;
+                const bool all = off >= 0 && at + 16 <= last_key;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int kk = 2 * j + (r & 1) + 8 * (r >> 1);
-                const bool in = off >= 0 && at + kk < last_key;
-                const char* row = vbase + off + bytes(kk * p.c.token_stride);
-                if constexpr (VW == 1) {
-                    vw[r][0] = in ? ldg_stream4(row + 4 * g) : 0u;
-                } else if constexpr (VW == 2) {
-                    const uint2 v = in ? ldg_stream8(row + 8 * g) : make_uint2(0, 0);
+                for (int r = 0; r < 4; ++r) {
+                    const int kk = 2 * j + (r & 1) + 8 * (r >> 1);
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (all || (off >= 0 && at + kk < last_key)) v = load_codes<VW>(row + (r & 1) * one_row + (r >> 1) * eight_rows);
                     vw[r][0] = v.x;
-                    vw[r][1] = v.y;
-                } else {
+                    if constexpr (VW == 2) vw[r][1] = v.y;
+                }
+            } else {
 #pragma unroll
-                    for (int w = 0; w < VW / 4; ++w) {
-                        const uint4 v = in ? ldg_stream16(row + 16 * (g + 8 * w)) : make_uint4(0, 0, 0, 0);
-                        vw[r][4 * w] = v.x;
-                        vw[r][4 * w + 1] = v.y;
-                        vw[r][4 * w + 2] = v.z;
-                        vw[r][4 * w + 3] = v.w;
+                for (int r = 0; r < 4; ++r) {
+                    const int kk = 2 * j + (r & 1) + 8 * (r >> 1);
+                    const bool in = off >= 0 && at + kk < last_key;
+                    const char* row = vbase + off + bytes(kk * p.c.token_stride);
+                    if constexpr (VW == 2) {
+                        const uint2 v = in ? ldg_stream8(row + 8 * g) : make_uint2(0, 0);
+                        vw[r][0] = v.x;
+                        vw[r][1] = v.y;
+                    } else {
+#pragma unroll
+                        for (int w = 0; w < VW / 4; ++w) {
+                            const uint4 v = in ? ldg_stream16(row + 16 * (g + 8 * w)) : make_uint4(0, 0, 0, 0);
+                            vw[r][4 * w] = v.x;
+                            vw[r][4 * w + 1] = v.y;
+                            vw[r][4 * w + 2] = v.z;
+                            vw[r][4 * w + 3] = v.w;
+                        }
                     }
                 }
             }
@@ -381,19 +426,28 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     const uint32_t k0[4] = {kws[u][0][w].x, kws[u][0][w].y, kws[u][0][w].z, kws[u][0][w].w};
                     const uint32_t k1[4] = {kws[u][1][w].x, kws[u][1][w].y, kws[u][1][w].z, kws[u][1][w].w};
                     if constexpr (INT4) {
+                        // 16 times the codes, as signed bytes: a word's even ones, and its odd ones
+                        int digit[NB][3][4];
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                            for (int l = 0; l < 3; ++l) digit[nb][l][0] = digit[nb][l][1] = digit[nb][l][2] = digit[nb][l][3] = (int)kMagic;
 #pragma unroll
                         for (int e = 0; e < D / 32; ++e) {
-                            const uint32_t x0 = k0[e], x1 = k1[e], y0 = x0 >> 8, y1 = x1 >> 8;
-                            const uint32_t low[4] = {nibbles_low(x0), nibbles_low(x1), nibbles_low(y0), nibbles_low(y1)};
-                            const uint32_t high[4] = {nibbles_high(x0), nibbles_high(x1), nibbles_high(y0), nibbles_high(y1)};
+                            const uint32_t a[4] = {k0[e] << 4 & 0xF0F0F0F0u, k1[e] << 4 & 0xF0F0F0F0u, k0[e] & 0xF0F0F0F0u, k1[e] & 0xF0F0F0F0u};
 #pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) {
-                                mma_16816(s[u][nb], low, qf[nb][4 * e], qf[nb][4 * e + 1], false);
-                                mma_16816(s[u][nb], high, qf[nb][4 * e + 2], qf[nb][4 * e + 3], false);
-                                mma_16816(s[u][nb], low, ql[nb][4 * e], ql[nb][4 * e + 1], false);
-                                mma_16816(s[u][nb], high, ql[nb][4 * e + 2], ql[nb][4 * e + 3], false);
-                            }
+                            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                                for (int l = 0; l < 3; ++l) mma_16832(digit[nb][l], a, qd[nb][l][2 * e], qd[nb][l][2 * e + 1]);
                         }
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float magic = __uint_as_float(kMagic);
+                                const float high = fmaf(__int_as_float(digit[nb][2][e]) - magic, 256.0f, __int_as_float(digit[nb][1][e]) - magic);
+                                s[u][nb][e] = fmaf(high, 256.0f, __int_as_float(digit[nb][0][e]) - magic);
+                            }
                     } else if constexpr (INT8) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -423,6 +477,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             // enough, so that most steps need neither the shuffles nor the rescaling (P stays below
             // 2^(kRescaleAt + kHeadroom))
             bool moves = false;
+            const bool all_seen = INT4 && key_now + 16 * SUB <= seen_by_all;
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -430,8 +485,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int at = key_now + 16 * u + g + 8 * (e >> 1);
-                        const float logit = INT4 ? fmaf(s[u][nb][e], row_scale[nb][e & 1], -row_off[nb][e & 1]) : s[u][nb][e] * row_scale[nb][e & 1];
-                        s[u][nb][e] = at < row_limit[nb][e & 1] ? logit : -INFINITY;
+                        const float logit = s[u][nb][e] * row_scale[nb][e & 1];
+                        s[u][nb][e] = (INT4 && all_seen) || at < row_limit[nb][e & 1] ? logit : -INFINITY;
                     }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) moves |= fmaxf(s[u][nb][e], s[u][nb][e + 2]) > m[nb][e] + (kRescaleAt + kHeadroom<!PBF>);
@@ -489,8 +544,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     for (int w = 0; w < 2 * VW; ++w) {       // four channels: a half of a word
                         const uint32_t pick = w & 1 ? 0x7632 : 0x5410;
                         const uint32_t x = __byte_perm(vw[0][w >> 1], vw[1][w >> 1], pick), y = __byte_perm(vw[2][w >> 1], vw[3][w >> 1], pick);
-                        const uint32_t a0[4] = {nibbles_low(x), nibbles_high(x), nibbles_low(y), nibbles_high(y)};
-                        const uint32_t a1[4] = {nibbles_low(x >> 8), nibbles_high(x >> 8), nibbles_low(y >> 8), nibbles_high(y >> 8)};
+                        const uint32_t a0[4] = {nibbles_low(x, flips), nibbles_high(x, flips), nibbles_low(y, flips), nibbles_high(y, flips)};
+                        const uint32_t a1[4] = {nibbles_low(x >> 8, flips), nibbles_high(x >> 8, flips), nibbles_low(y >> 8, flips), nibbles_high(y >> 8, flips)};
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) {
                             mma_16816(o[2 * w][nb], a0, pf[nb][0], pf[nb][1], false);

@@ -47,12 +47,12 @@ class Batch(R.Batch):
 def attention(batch, scale, causal):
     """As paged_reference.attention, with the 4-bit cache's bounds.
 
-    A logit is the sum of q s (c + 8) over the channels, each in two parts that are exact, less 8 sum q s.  With n non-zero
-    elements of q that is at most 2 n additions, each off by at most 2^-23 (the tensor cores may truncate) of partial sums
-    of at most 15 A, A = sum |q s| scale; the second sum and the difference add 2^-23 (n + 3) 8 A:
-    e = (2 n 15 + 8 n + 64) 2^-23 A.  A product's own f16 parts are exact while the row's elements lie within 2^16 of its
-    largest, which these inputs do.  The second product is taken with c + 8 too: its fp32 sums add keys 2^-23 15 max(s) to
-    what the other caches' bound allows."""
+    A logit is the sum of q s c over the channels.  Either q s is taken as a multiple of 2^-22 of the row's largest, M, half a
+    step off at most for each of n non-zero elements, and the sums are exact but for 8 roundings of 2^-24 of at most 16 A,
+    A = sum |q s|; or q and s c are taken as 16-bit floats (exact while a row's elements lie within 2^16 of its largest, which
+    these inputs do), and n additions are off by at most 2^-23 (the tensor cores may truncate) of 8 A each:
+    e = max(8 n 2^-22 M + 2^-17 A, (n + 8) 2^-20 A) scale.  The second product is taken with c + 8: its fp32 sums add
+    keys 2^-23 15 max(s) to what the other caches' bound allows."""
     out, lse, out_tol, lse_tol = R.attention(batch, scale, causal)
     q_all = batch.q_wide[:, :batch.heads].double().numpy()
     G = batch.heads // batch.kv_heads
@@ -62,7 +62,9 @@ def attention(batch, scale, causal):
         for c in range(batch.heads):
             s = used(batch.k_scale[c // G]).double().abs().numpy()
             nz = (q_all[rows, c] != 0).sum(axis=1)
-            e = (38 * nz + 64) * 2.0 ** -23 * (np.abs(q_all[rows, c]) @ s) * abs(scale)
+            qs = np.abs(q_all[rows, c]) * s
+            A = qs.sum(axis=1)
+            e = np.maximum(8 * nz * 2.0 ** -22 * qs.max(axis=1, initial=0.0) + 2.0 ** -17 * A, (nz + 8) * 2.0 ** -20 * A) * abs(scale)
             big = np.abs(v[:, c // G]).max(initial=0.0)
             sv = used(batch.v_scale[c // G]).double().abs().numpy().max()
             lse_tol[rows, c] += e
