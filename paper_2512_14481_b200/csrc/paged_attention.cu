@@ -90,7 +90,7 @@ void set_blocks(Plan* pl, const sasq_kv_batch_t* b) {
 }
 bool tiles_possible(const sasq_kv_cache_t* c, const sasq_kv_batch_t* b, int heads) {
     const int group = heads / c->num_kv_heads;
-    return (long long)b->max_q_len * group > 16 && group <= 128 && c->num_pages > 0 && c->kind != SASQ_KV_INT4;
+    return (long long)b->max_q_len * group > 16 && group <= 128 && c->num_pages > 0;
 }
 
 // The batch with its bounds cut to what q and the page table can hold (the device cuts lengths to the same), so that a
@@ -229,29 +229,29 @@ unsigned join_rows(const AttendParams& p, int max_rows) {
     return max_rows > p.item_rows / 2 ? 256 / 8 : (unsigned)ceil_div(max_rows < 1 ? 1 : max_rows, 8);
 }
 
-template <int D, bool BF, bool INT8>
+template <int D, bool BF, int KIND>
 cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, int max_rows, cudaStream_t st) {
     static std::atomic<unsigned long long> ready{0};          // devices whose shared-memory limit has been raised
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (!(ready.load() >> (dev & 63) & 1)) {
-        e = cudaFuncSetAttribute(paged_tiles_kernel<D, BF, INT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTileSmem<D>);
+        e = cudaFuncSetAttribute(paged_tiles_kernel<D, BF, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTileSmem<D>);
         if (e != cudaSuccess) return e;
         ready.fetch_or(1ull << (dev & 63));
     }
     CUtensorMap map_q{}, map_k{}, map_v{};
     if (!encode_queries<D, BF>(&map_q, p)) return cudaErrorInvalidValue;
-    if (!INT8 && (!encode_pages<D, BF>(&map_k, c, c->k) || !encode_pages<D, BF>(&map_v, c, c->v))) return cudaErrorInvalidValue;
+    if (KIND == SASQ_KV_16BIT && (!encode_pages<D, BF>(&map_k, c, c->k) || !encode_pages<D, BF>(&map_v, c, c->v))) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)p.max_blocks);
-    cfg.blockDim = dim3(kTileThreads<INT8>);
+    cfg.blockDim = dim3(kTileThreads<KIND>);
     cfg.dynamicSmemBytes = kTileSmem<D>;
     cfg.stream = st;
     cudaLaunchAttribute attr = pdl_attribute();
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF, INT8>, map_q, map_k, map_v, p);
+    e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF, KIND>, map_q, map_k, map_v, p);
     if (e != cudaSuccess || !p.split) return e;
     return launch(paged_join_kernel<256, 128, D, BF, false>, dim3(p.max_blocks, join_rows(p, max_rows)), 256, 0, st, p);
 }
@@ -259,7 +259,9 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, int ma
 template <int D, bool BF>
 cudaError_t launch_all(const Plan& pl, const AttendParams& p, const sasq_kv_cache_t* c, cudaStream_t st) {
     if (pl.tiles)
-        return c->kind == SASQ_KV_INT8 ? launch_tiles<D, BF, true>(p, c, pl.max_rows, st) : launch_tiles<D, BF, false>(p, c, pl.max_rows, st);
+        return c->kind == SASQ_KV_INT4   ? launch_tiles<D, BF, SASQ_KV_INT4>(p, c, pl.max_rows, st)
+               : c->kind == SASQ_KV_INT8 ? launch_tiles<D, BF, SASQ_KV_INT8>(p, c, pl.max_rows, st)
+                                         : launch_tiles<D, BF, SASQ_KV_16BIT>(p, c, pl.max_rows, st);
     return c->kind == SASQ_KV_INT4   ? launch_few<D, BF, SASQ_KV_INT4>(pl, p, st)
            : c->kind == SASQ_KV_INT8 ? launch_few<D, BF, SASQ_KV_INT8>(pl, p, st)
                                      : launch_few<D, BF, SASQ_KV_16BIT>(pl, p, st);
@@ -319,6 +321,7 @@ int sasq_paged_attention(const sasq_kv_cache_t* cache, const sasq_kv_batch_t* ba
     p.tile_bound = pl.tile_bound;
     p.wait_limit = debug_wait_limit();
     p.flips = kFlips;
+    p.half_flips = kHalfFlips;
     p.part_items = static_cast<PartItem*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + l.ml);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.o);

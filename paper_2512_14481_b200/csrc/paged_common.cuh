@@ -272,7 +272,7 @@ __device__ __forceinline__ float factor4(float s) { return __bfloat162float(__fl
 struct Flips {
     uint32_t low, high;
 };
-constexpr Flips kFlips{0x00080008u, 0x00800080u};
+constexpr Flips kFlips{0x00080008u, 0x00800080u}, kHalfFlips{0x64086408u, 0x64806480u};    // the latter with the exponent of 1024
 __device__ __forceinline__ uint32_t nibbles_low(uint32_t w, const Flips& f) {
     uint32_t d;
     asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6A;" : "=r"(d) : "r"(w), "r"(f.low));      // (w & mask) ^ flip

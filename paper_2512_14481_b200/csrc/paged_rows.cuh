@@ -22,7 +22,7 @@ struct AttendParams {
     float2* part_ml;            // [2 * max_blocks][R]: maximum (log2 units) and sum
     float* part_o;              // [2 * max_blocks][R][D]
     long long wait_limit;
-    Flips flips;                // 4-bit codes
+    Flips flips, half_flips;    // 4-bit codes
 };
 
 namespace {

@@ -71,13 +71,16 @@ namespace {
 // An item is two row tiles, each the tokens whose heads fit 128 MMA rows: 128 / group tokens, so that a row tile is one
 // box of q (of a group of five heads 125 rows are used).
 constexpr int kTileKeys = 128;            // keys of a unit
-// Readers of the item queue: the softmax warps, the MMA lane, and whoever fetches K and V
-template <bool INT8>
-constexpr int kReaders = 8 + 1 + (INT8 ? 8 : 2);
-// Warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q and the items; 11: V's tails.  With an int8 cache warps
-// 12-19 fetch and convert K and V, and 9 and 11 are idle.
-template <bool INT8>
-constexpr int kTileThreads = INT8 ? 640 : 384;
+// With a 4-bit cache bf16 queries meet K as f16: a warp for each row tile brings them there.
+template <bool BF, int KIND>
+constexpr bool kQueriesConverted = BF && KIND == SASQ_KV_INT4;
+// Readers of the item queue: the softmax warps, the MMA lane, and whoever fetches K and V, and converts queries
+template <bool BF, int KIND>
+constexpr int kReaders = 8 + 1 + (KIND != SASQ_KV_16BIT ? 8 : 2) + (kQueriesConverted<BF, KIND> ? 2 : 0);
+// Warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q and the items; 11: V's tails.  With an int8 or 4-bit cache
+// warps 12-19 fetch and convert K and V, and 9 and 11 are idle, or convert the queries.
+template <int KIND>
+constexpr int kTileThreads = KIND != SASQ_KV_16BIT ? 640 : 384;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11, kConvertWarp = 12;
 constexpr int kConvertThreads = 256;
 // Registers of a thread.  384 threads get 168 each, enough for every role.  640 get 96 at launch, of which the four-warp
@@ -122,6 +125,8 @@ struct TileTail {
     uint64_t s_full[2], p_full[2][2], o_full[2];            // p_full: either half of the unit's keys
     uint64_t drain, meet[4];
     float2 other[128];        // reference and sum of the second row tile's rows, for the first
+    uint64_t unit_empty[2];      // converted queries: the softmax warps have read row_exponent
+    uint8_t row_exponent[2][128];    // of the power of two that a row was divided by, biased as a float's, of either row tile
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -226,19 +231,81 @@ __device__ __forceinline__ void store_codes(uint8_t* tile, int r, int chunk, int
         make_uint4(codes_to_pair<BF, 0>(hi.x), codes_to_pair<BF, 1>(hi.x), codes_to_pair<BF, 0>(hi.y), codes_to_pair<BF, 1>(hi.y));
 }
 
-// The warps that fill the ring from an int8 cache (`me` of kConvertThreads): K and V of each unit in turn, in the layout
+// A head's 4-bit key factors are divided by this power of two on their way to f16 (the largest becomes 2^11 ... 2^12, so that
+// codes times factors fit, and are exact as long as a factor is no smaller than 2^-28 of it); from the bits of the largest.
+__device__ __forceinline__ uint32_t head_unit(uint32_t largest) {
+    return min(max(largest & 0x7F800000u, 13u << 23), 253u << 23) - (11u << 23);
+}
+
+// 32 4-bit codes of a key, in natural order, as f16 into row r of a swizzled tile: four chunks of 8, of which lanes with `turn` store
+// the second two first.  K is multiplied by its factors (exact: 11 bits).
+template <bool KEYS>
+__device__ __forceinline__ void store_codes4(uint8_t* tile, int r, int chunk, int turn, const uint4& v, const Flips& flips,
+                                             const __half2* factor) {
+    uint8_t* const row = tile + r * 128;
+    const uint32_t words[4] = {turn ? v.z : v.x, turn ? v.w : v.y, turn ? v.x : v.z, turn ? v.y : v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = words[i], y = w >> 8;
+        // 1024 + u and 1024 + 16 u, u = code + 8: of channels (0, 4), (1, 5), (2, 6), (3, 7)
+        uint32_t u[4];
+        asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6A;" : "=r"(u[0]) : "r"(w), "r"(flips.low));
+        asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0x6A;" : "=r"(u[1]) : "r"(w), "r"(flips.high));
+        asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6A;" : "=r"(u[2]) : "r"(y), "r"(flips.low));
+        asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0x6A;" : "=r"(u[3]) : "r"(y), "r"(flips.high));
+        uint32_t c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t off = 0x64086408u, sixteenth = 0x2C002C00u, minus72 = 0xD480D480u;      // 1032, 1/16, -72
+            __half2 x = *reinterpret_cast<const __half2*>(&u[e]);
+            x = e & 1 ? __hfma2(x, *reinterpret_cast<const __half2*>(&sixteenth), *reinterpret_cast<const __half2*>(&minus72))
+                      : __hsub2(x, *reinterpret_cast<const __half2*>(&off));
+            if (KEYS) x = __hmul2(x, factor[4 * i + e]);
+            c[e] = *reinterpret_cast<const uint32_t*>(&x);
+        }
+        const uint4 out = make_uint4(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410), __byte_perm(c[0], c[1], 0x7632),
+                                     __byte_perm(c[2], c[3], 0x7632));
+        *reinterpret_cast<uint4*>(row + (((chunk + (i ^ (turn << 1))) ^ (r & 7)) << 4)) = out;
+    }
+}
+
+// The warps that fill the ring from an int8 or 4-bit cache (`me` of kConvertThreads): K and V of each unit in turn, in the layout
 // that the 16-bit copies leave: keys along the rows, 128-byte swizzle.  Keys behind the sequence's last are zeros.
-template <int D, bool BF>
+template <int D, bool BF, int KIND>
 __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uint8_t* ring, TileTail* tail) {
     using Shape = TileShape<D>;
-    constexpr int kWords = D / 16;                 // 16-byte words of a key's codes
+    constexpr bool INT4 = KIND == SASQ_KV_INT4;
+    constexpr int kWords = INT4 ? D / 32 : D / 16; // 16-byte words of a key's codes
     constexpr int kKeys = kConvertThreads / kWords;        // keys of a step
     constexpr int kSteps = kTileKeys / kKeys;
     const int word = me % kWords, first = me / kWords, lane = me & 31;
     const int page_mask = (1 << p.c.page_shift) - 1;
-    // the word's two chunks of 8 elements; half a row's lanes store the second first, which spreads them over the banks
-    uint8_t* const column = ring + (word >> 2) * kTileKeys * 128;
-    const int chunk = 2 * (word & 3), turn = word >> 2 & 1;
+    // the word's two (4-bit: four) chunks of 8 elements; half a row's lanes store the second half first, which spreads them over
+    // the banks
+    uint8_t* const column = ring + (INT4 ? word >> 1 : word >> 2) * kTileKeys * 128;
+    const int chunk = INT4 ? 4 * (word & 1) : 2 * (word & 3), turn = INT4 ? word >> 1 & 1 : word >> 2 & 1;
+    // 4-bit: K's factors of the word's channels, (0, 4), (1, 5), (2, 6), (3, 7) of each eight, as store_codes4 wants them
+    __half2 factor[INT4 ? 16 : 1];
+    auto load_factors = [&](int h) {
+        const float4* f4 = reinterpret_cast<const float4*>(p.c.k_scale + h * D + 32 * word);
+        float f[32];
+        uint32_t seen = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 v = __ldg(f4 + (i ^ turn << 2));          // in the order of the stores
+            f[4 * i] = factor4(v.x), f[4 * i + 1] = factor4(v.y), f[4 * i + 2] = factor4(v.z), f[4 * i + 3] = factor4(v.w);
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) seen = max(seen, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+#pragma unroll
+        for (int o = 1; o < kWords; o <<= 1) seen = max(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, o));
+        const float down = 1.0f / __uint_as_float(head_unit(seen));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = 8 * (i >> 2) + (i & 3);
+            factor[INT4 ? i : 0] = __floats2half2_rn(f[at] * down, f[at + 4] * down);
+        }
+    };
     ItemReader items{tail, p, 0, true, false};
     bool ok = true, more;
     TileItem it{};
@@ -266,13 +333,14 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
         return more && key < it.len ? __ldg(table + (key >> p.c.page_shift)) : -1;
     };
     auto load = [&](const void* base, int entry, uint4 (&v)[kSteps]) {
-        const char* head = static_cast<const char*>(base) + it.h * p.c.head_stride + word * 16;
+        auto bytes = [](long long elements) { return INT4 ? elements >> 1 : elements; };
+        const char* head = static_cast<const char*>(base) + bytes(it.h * p.c.head_stride) + word * 16;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int key = t * kTileKeys + i * kKeys + first;
             const int page = __shfl_sync(0xFFFFFFFFu, entry, (i * kKeys + first) >> 4);
             const bool in = key < it.len && page >= 0 && page < p.c.num_pages;
-            v[i] = in ? ldg_stream16(head + page * p.c.page_stride + (key & page_mask) * p.c.token_stride) : make_uint4(0, 0, 0, 0);
+            v[i] = in ? ldg_stream16(head + bytes(page * p.c.page_stride + (key & page_mask) * p.c.token_stride)) : make_uint4(0, 0, 0, 0);
         }
     };
     int slot = 0;
@@ -284,7 +352,10 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
         uint8_t* const tile = column + (size_t)slot * Shape::kSlotBytes;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            if (values) store_codes<false>(tile, i * kKeys + first, chunk, turn, v[i]);
+            if constexpr (INT4) {
+                if (values) store_codes4<false>(tile, i * kKeys + first, chunk, turn, v[i], p.half_flips, factor);
+                else store_codes4<true>(tile, i * kKeys + first, chunk, turn, v[i], p.half_flips, factor);
+            } else if (values) store_codes<false>(tile, i * kKeys + first, chunk, turn, v[i]);
             else store_codes<BF>(tile, i * kKeys + first, chunk, turn, v[i]);
         }
         ptx::fence_proxy_async_smem();
@@ -297,6 +368,8 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
     next();
     int entry = look_up();
     if (more) load(p.c.k, entry, k);
+    int head = more ? it.h : 0;                    // whose factors are in place
+    if (INT4 && more) load_factors(head);
     while (more && ok) {
         if (t * kTileKeys + 16 * (lane & 7) < it.len && (entry < 0 || entry >= p.c.num_pages))
             atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
@@ -305,13 +378,74 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
         entry = look_up();
         store(k, false);
         if (more) load(p.c.k, entry, k);
+        if (INT4 && more && it.h != head) load_factors(head = it.h);
         if (ok) store(v, true);
     }
 }
 
-template <bool INT8, bool MORE, int N>
+// The warp that brings the bf16 queries of row tile x to shared memory as f16, each row divided by a power of two (its largest
+// becomes 2^14 ... 2^15: exact as long as an element is no smaller than 2^-31 of it), in the layout that the copies leave.
+template <int D>
+__device__ __forceinline__ void convert_queries(const AttendParams& p, int x, uint8_t* q_tile, TileTail* tail) {
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes, kAhead = 4;           // lanes of a row, rows of a step, steps under way
+    const int lane = threadIdx.x & 31, word = lane % kLanes, sub = lane / kLanes;
+    const int tokens = 128 / p.group, rows = tokens * p.group;
+    uint8_t* const column = q_tile + (word >> 3) * 128 * 128;
+    ItemReader items{tail, p, 0, true, false};
+    bool ok = true;
+    for (uint32_t filled = 0; ok; items.template leave<true>(lane == 0)) {
+        items.template fetch<true>();
+        ok = items.ok;
+        if (!items.more) break;
+        const TileItem& it = items.item();
+        if (it.end[x] == it.begin[x]) continue;
+        ok = tile_wait(&tail->q_empty[x], (filled & 1u) ^ 1u, tail, p) && tile_wait(&tail->unit_empty[x], (filled & 1u) ^ 1u, tail, p);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) continue;
+        const int token0 = it.first_token + it.first_row / p.group + (it.fold != 0 ? 0 : x * tokens);
+        auto fetch = [&](int r) {
+            const int t = r / p.group;
+            return r < rows && token0 + t < p.c.total_q
+                       ? *reinterpret_cast<const uint4*>(p.q + (long long)(token0 + t) * p.q_stride + (long long)(it.h * p.group + r - t * p.group) * D + 8 * word)
+                       : make_uint4(0, 0, 0, 0);
+        };
+        for (int first = sub; first - sub < rows; first += kRows * kAhead) {
+            uint4 v[kAhead];
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) v[e] = fetch(first + kRows * e);
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                const uint32_t w[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
+                uint32_t seen = 0;                                            // NaN compares as the largest
+#pragma unroll
+                for (int i = 0; i < 4; ++i) seen = max(seen, max((w[i] << 16) & 0x7FFF0000u, w[i] & 0x7FFF0000u));
+#pragma unroll
+                for (int o = 1; o < kLanes; o <<= 1) seen = max(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, o));
+                const uint32_t top = min(max(seen & 0x7F800000u, 15u << 23), 253u << 23);
+                const float up = __uint_as_float((268u << 23) - top);         // 2^14 over the power of two at or below the largest
+                uint32_t h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = widen2<true>(w[i]);
+                    h[i] = narrow2<false>(f.x * up, f.y * up);
+                }
+                const int r = first + kRows * e;
+                if (r < rows) {
+                    *reinterpret_cast<uint4*>(column + r * 128 + (((word & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                    if (word == 0) tail->row_exponent[x][r] = (uint8_t)((top >> 23) - 14u);
+                }
+            }
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&tail->q_full[x]);
+        ++filled;
+    }
+}
+
+template <int KIND, bool MORE, int N>
 __device__ __forceinline__ void registers_to() {
-    if constexpr (INT8) {
+    if constexpr (KIND != SASQ_KV_16BIT) {
         if constexpr (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
     }
@@ -327,12 +461,14 @@ __device__ __forceinline__ void registers_to() {
 // Bound by that alternation: 256 rows x 128 keys take 2050 clocks of MMAs and 2048 of exponentials, and a step takes about
 // 3500 (8192 causal tokens, 32 heads of 128, bf16: 511 us, 1076 TFLOP/s in short bursts; 619 us, 888 TFLOP/s, one call after
 // another under the power cap, at 1.4 to 1.65 GHz).
-template <int D, bool BF, bool INT8>
-__global__ void __launch_bounds__(kTileThreads<INT8>, 1)
+template <int D, bool BF, int KIND>
+__global__ void __launch_bounds__(kTileThreads<KIND>, 1)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendParams p) {
     using Shape = TileShape<D>;
-    constexpr bool PBF = BF && !INT8;                          // the second product's type; else f16
+    constexpr bool INT8 = KIND == SASQ_KV_INT8, INT4 = KIND == SASQ_KV_INT4, kCodes = KIND != SASQ_KV_16BIT;
+    constexpr bool PBF = BF && !kCodes, SBF = BF && !INT4;     // the second and the first product's type; else f16
+    constexpr bool kConvertsQ = kQueriesConverted<BF, KIND>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* q_smem = smem;
@@ -342,13 +478,14 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
     if (tid == 0) {
         for (int s = 0; s < Shape::kSlots; ++s) {
-            ptx::mbar_init(&tail->kv_full[s], INT8 ? kConvertThreads : 1);
+            ptx::mbar_init(&tail->kv_full[s], kCodes ? kConvertThreads : 1);
             ptx::mbar_init(&tail->kv_empty[s], 1);
             ptx::mbar_init(&tail->raw_full[s], 1);
         }
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&tail->q_full[x], 1);
             ptx::mbar_init(&tail->q_empty[x], 1);
+            ptx::mbar_init(&tail->unit_empty[x], 4);
             ptx::mbar_init(&tail->s_full[x], 1);
             ptx::mbar_init(&tail->p_full[x][0], 128);
             ptx::mbar_init(&tail->p_full[x][1], 128);
@@ -358,12 +495,12 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&tail->meet[i], 64);
         for (int i = 0; i < kItems; ++i) {
             ptx::mbar_init(&tail->item_full[i], 1);
-            ptx::mbar_init(&tail->item_empty[i], kReaders<INT8>);
+            ptx::mbar_init(&tail->item_empty[i], kReaders<BF, KIND>);
         }
         tail->abort_flag = 0;
         ptx::mbar_init_fence();
         ptx::prefetch_tensormap(&map_q);
-        if constexpr (!INT8) {
+        if constexpr (!kCodes) {
             ptx::prefetch_tensormap(&map_k);
             ptx::prefetch_tensormap(&map_v);
         }
@@ -390,7 +527,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     };
 
     if (warp == kLoadWarp) {
-        registers_to<INT8, false, kOtherRegs>();
+        registers_to<KIND, false, kOtherRegs>();
+        if constexpr (kConvertsQ) convert_queries<D>(p, 0, q_smem, tail);
         // ---------------- K and V of each unit, in turn, a lane per page ----------------
         int slot = 0;
         uint32_t phase = 0;
@@ -398,7 +536,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int boxes = kTileKeys / box;
         const int page_mask = (1 << p.c.page_shift) - 1;
         ItemReader items{tail, p, 0, true, false};
-        for (; !INT8 && ok; items.template leave<true>(lane == 0)) {
+        for (; !kCodes && ok; items.template leave<true>(lane == 0)) {
             items.template fetch<true>();
             ok = items.ok;
             if (!items.more) break;
@@ -441,7 +579,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         // Copies still in flight must land before the block's shared memory goes away: at once, unless a role gave up.
         // (A tile with a tail to clear may then never be announced; the limit is far above a copy's flight.)
-        if (lane == 0) {
+        if (lane == 0 && !kCodes) {
             for (int s = 0; s < Shape::kSlots; ++s) {
                 const long long t0 = clock64();
                 const uint32_t par = s < slot ? phase : (phase ^ 1u);
@@ -451,7 +589,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
     } else if (warp == kQueryWarp) {
-        registers_to<INT8, false, kOtherRegs>();
+        registers_to<KIND, false, kOtherRegs>();
         // ---------------- the block's items, for everyone, and their Q ----------------
         uint32_t filled[2] = {0, 0};                            // times that each row tile's queries were asked for
         const int tokens = 128 / p.group;
@@ -467,6 +605,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (more) {
                 if (INT8 && lane == 0 && (scale_is_bad(__ldg(p.c.k_scale + w.h)) || scale_is_bad(__ldg(p.c.v_scale + w.h))))
                     atomicMax(p.c.status, (int)SASQ_ERR_BAD_SCALE);
+                if (INT4)
+                    for (int d = lane; d < D; d += 32)
+                        if (scale_is_bad(factor4(__ldg(p.c.k_scale + w.h * D + d))) || scale_is_bad(factor4(__ldg(p.c.v_scale + w.h * D + d))))
+                            atomicMax(p.c.status, (int)SASQ_ERR_BAD_SCALE);
                 it.b = w.b;
                 it.h = w.h;
                 it.len = w.s.len;
@@ -497,7 +639,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (!more) break;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (!ok || it.end[x] == it.begin[x]) continue;
+                if (kConvertsQ || !ok || it.end[x] == it.begin[x]) continue;
                 if (!wait(&tail->q_empty[x], (filled[x] & 1u) ^ 1u)) continue;
                 ++filled[x];
                 if (lane == 0) {
@@ -520,10 +662,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        registers_to<INT8, false, kOtherRegs>();
+        registers_to<KIND, false, kOtherRegs>();
         // ---------------- MMAs, all by one lane (which lets the descriptors live in uniform registers) ----------------
         if (ptx::elect_one()) {
-            constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, BF);
+            constexpr uint32_t idesc_s = ptx::idesc_f16(128, kTileKeys, SBF);
             constexpr uint32_t idesc_o = ptx::idesc_f16(128, D, PBF) | ptx::kIdescBTransposed;
             uint32_t q_phase = 0, p_phase = 0;                        // a bit per row tile
             const uint64_t q_desc = ptx::smem_desc_k_major_sw128(ptx::smem_u32(q_smem));
@@ -634,14 +776,15 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
     } else if (warp == kTailWarp) {
-        registers_to<INT8, false, kOtherRegs>();
+        registers_to<KIND, false, kOtherRegs>();
+        if constexpr (kConvertsQ) convert_queries<D>(p, 1, q_smem + Shape::kQBytes, tail);
         // ---------------- rows of V behind a sequence's last key ----------------
         // Whatever they hold is multiplied by P = 0, and must be finite.  The copy of such a tile is announced here, and
         // the MMAs learn of it when the rows are zero.
         int slot = 1;                                               // of the unit's V: slots go K, V, K, V, ...
         uint32_t phases = 0;                                        // a bit per slot
         ItemReader items{tail, p, 0, true, false};
-        for (; !INT8 && ok; items.template leave<true>(lane == 0)) {
+        for (; !kCodes && ok; items.template leave<true>(lane == 0)) {
             items.template fetch<true>();
             ok = items.ok;
             if (!items.more) break;
@@ -664,13 +807,13 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 slot = (slot + 2) % Shape::kSlots;
             }
         }
-    } else if (INT8 && warp >= kConvertWarp) {
-        // ---------------- int8 cache: K and V of each unit, converted on the way to shared memory ----------------
+    } else if (kCodes && warp >= kConvertWarp) {
+        // ---------------- int8 or 4-bit cache: K and V of each unit, converted on the way to shared memory ----------------
         // 16 codes a thread and step; the next tile's codes travel while this one's are converted.
-        registers_to<INT8, false, kConvertRegs>();
-        if constexpr (INT8) convert_tiles<D, BF>(p, tid - 32 * kConvertWarp, ring, tail);
+        registers_to<KIND, false, kConvertRegs>();
+        if constexpr (kCodes) convert_tiles<D, BF, KIND>(p, tid - 32 * kConvertWarp, ring, tail);
     } else {
-        registers_to<INT8, true, kSoftmaxRegs>();
+        registers_to<KIND, true, kSoftmaxRegs>();
         // ---------------- softmax: row tile x, one row per thread ----------------
         const int x = warp >> 2, quad = warp & 3;
         const int half = sch.rows >> 1;
@@ -688,6 +831,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             ptx::tc_fence_after_sync();
             return true;
         };
+        uint32_t q_fills = 0;                                      // converted queries: times that this row tile's came
         ItemReader items{tail, p, 0, true, false};
         for (; ok; items.template leave<true>(lane == 0)) {
             items.template fetch<true>();
@@ -701,7 +845,20 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const bool valid = row < half && item_row < it.rows;
             int row_limit = it.limit;
             if (p.causal && valid) row_limit = it.before + item_row / p.group + 1;
-            const float signed_scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
+            float signed_scale = INT8 ? p.scale * __ldg(p.c.k_scale + it.h) : p.scale;
+            if constexpr (INT4) {                                  // what K's factors, and the row's queries, were divided by
+                uint32_t largest = 0;
+#pragma unroll
+                for (int d = lane; d < D; d += 32) largest = max(largest, __float_as_uint(factor4(__ldg(p.c.k_scale + it.h * D + d))) & 0x7FFFFFFFu);
+                signed_scale *= __uint_as_float(head_unit(__reduce_max_sync(0xFFFFFFFFu, largest)));
+                if (kConvertsQ && any) {
+                    if (!wait(&tail->q_full[x], q_fills & 1u)) break;
+                    signed_scale *= __uint_as_float((uint32_t)tail->row_exponent[x][row] << 23);
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&tail->unit_empty[x]);
+                    ++q_fills;
+                }
+            }
             // A scale of zero, or one that vanished in the product with the factor, would turn masked logits, -inf, into NaN; the
             // smallest number there is gives the same equal weights.
             const float scale = signed_scale == 0.0f ? __uint_as_float(1u) : fabsf(signed_scale);
@@ -716,9 +873,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const bool cut = __any_sync(0xFFFFFFFFu, seen < kTileKeys);
                 // The row is read in halves, the second one twice: for its maximum before the first half, and for its
                 // exponentials behind it.  128 logits and what is made of them do not fit a thread's registers.  With the
-                // int8 cache the three steps share their code: the converting warps need the instruction cache too
+                // int8 (and the 4-bit) cache the three steps share their code: the converting warps need the instruction cache too
                 // (measured on a 1024-token chunk over 15000 keys: int8 350 -> 323 us, 16-bit 227 -> 246 us).
-                constexpr int kSteps = INT8 ? 1 : 3;
+                constexpr int kSteps = kCodes ? 1 : 3;
                 float most = -INFINITY;
 #pragma unroll kSteps
                 for (int step = 0; step < 3; ++step) {
@@ -836,6 +993,17 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0;
+                }
+                if constexpr (INT4) {                              // V's factors, of the parts too
+                    const float4* f4 = reinterpret_cast<const float4*>(p.c.v_scale + it.h * D + c);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 f = __ldg(f4 + e);
+                        o[4 * e] = __float_as_uint(__uint_as_float(o[4 * e]) * factor4(f.x));
+                        o[4 * e + 1] = __float_as_uint(__uint_as_float(o[4 * e + 1]) * factor4(f.y));
+                        o[4 * e + 2] = __float_as_uint(__uint_as_float(o[4 * e + 2]) * factor4(f.z));
+                        o[4 * e + 3] = __float_as_uint(__uint_as_float(o[4 * e + 3]) * factor4(f.w));
+                    }
                 }
                 if (valid && whole) {
                     uint4* dst = reinterpret_cast<uint4*>(p.out + token * p.out_stride + (long long)head * D + c);
