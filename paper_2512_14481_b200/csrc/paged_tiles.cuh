@@ -76,15 +76,16 @@ template <bool BF, int KIND>
 constexpr bool kQueriesConverted = BF && KIND == SASQ_KV_INT4;
 // Readers of the item queue: the softmax warps, the MMA lane, and whoever fetches K and V, and converts queries
 template <bool BF, int KIND>
-constexpr int kReaders = 8 + 1 + (KIND != SASQ_KV_16BIT ? 8 : 2) + (kQueriesConverted<BF, KIND> ? 2 : 0);
+constexpr int kReaders = 8 + 1 + (KIND == SASQ_KV_16BIT ? 2 : 8) + (kQueriesConverted<BF, KIND> ? 2 : 0);
 // Warps 0-3 and 4-7: softmax of either row tile; 8: MMA; 9: K and V; 10: Q and the items; 11: V's tails.  With an int8 or 4-bit cache
 // warps 12-19 fetch and convert K and V, and 9 and 11 are idle, or convert the queries.
-template <int KIND>
-constexpr int kTileThreads = KIND != SASQ_KV_16BIT ? 640 : 384;
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11, kConvertWarp = 12;
 constexpr int kConvertThreads = 256;
+template <int KIND>
+constexpr int kTileThreads = KIND == SASQ_KV_16BIT ? 384 : 384 + kConvertThreads;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10, kTailWarp = 11, kConvertWarp = 12;
 // Registers of a thread.  384 threads get 168 each, enough for every role.  640 get 96 at launch, of which the four-warp
-// groups without a row of logits give some to the softmax: 2 x 128 + 64 + 2 x 80 = 5 x 96.
+// groups without a row of logits give some to the softmax: 2 x 128 + 64 + 2 x 80 = 5 x 96.  (The 4-bit cache converted by four warps, the
+// softmax at 160 registers: 372 us instead of 353 for a chunk of 1024 tokens over 15000 keys.)
 constexpr int kSoftmaxRegs = 128, kOtherRegs = 64, kConvertRegs = 80;
 
 template <int D>
@@ -237,9 +238,10 @@ __device__ __forceinline__ uint32_t head_unit(uint32_t largest) {
     return min(max(largest & 0x7F800000u, 13u << 23), 253u << 23) - (11u << 23);
 }
 
-// 32 4-bit codes of a key, in natural order, as f16 into row r of a swizzled tile: four chunks of 8, of which lanes with `turn` store
-// the second two first.  K is multiplied by its factors (exact: 11 bits).
-template <bool KEYS>
+// 32 4-bit codes of a key as f16 into row r of a swizzled tile: four chunks of 8, of which lanes with `turn` store the second two
+// first.  K is multiplied by its factors (exact: 11 bits).  A chunk's channels lie as they come out of a word, 0 4 1 5 2 6 3 7: so do
+// converted queries', and the result's until it is stored; queries that were copied meet keys in NATURAL order.
+template <bool KEYS, bool NATURAL>
 __device__ __forceinline__ void store_codes4(uint8_t* tile, int r, int chunk, int turn, const uint4& v, const Flips& flips,
                                              const __half2* factor) {
     uint8_t* const row = tile + r * 128;
@@ -263,9 +265,10 @@ __device__ __forceinline__ void store_codes4(uint8_t* tile, int r, int chunk, in
             if (KEYS) x = __hmul2(x, factor[4 * i + e]);
             c[e] = *reinterpret_cast<const uint32_t*>(&x);
         }
-        const uint4 out = make_uint4(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410), __byte_perm(c[0], c[1], 0x7632),
-                                     __byte_perm(c[2], c[3], 0x7632));
-        *reinterpret_cast<uint4*>(row + (((chunk + (i ^ (turn << 1))) ^ (r & 7)) << 4)) = out;
+        *reinterpret_cast<uint4*>(row + (((chunk + (i ^ (turn << 1))) ^ (r & 7)) << 4)) =
+            NATURAL ? make_uint4(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410), __byte_perm(c[0], c[1], 0x7632),
+                                 __byte_perm(c[2], c[3], 0x7632))
+                    : make_uint4(c[0], c[1], c[2], c[3]);
     }
 }
 
@@ -353,8 +356,8 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             if constexpr (INT4) {
-                if (values) store_codes4<false>(tile, i * kKeys + first, chunk, turn, v[i], p.half_flips, factor);
-                else store_codes4<true>(tile, i * kKeys + first, chunk, turn, v[i], p.half_flips, factor);
+                if (values) store_codes4<false, false>(tile, i * kKeys + first, chunk, turn, v[i], p.half_flips, factor);
+                else store_codes4<true, !kQueriesConverted<BF, KIND>>(tile, i * kKeys + first, chunk, turn, v[i], p.half_flips, factor);
             } else if (values) store_codes<false>(tile, i * kKeys + first, chunk, turn, v[i]);
             else store_codes<BF>(tile, i * kKeys + first, chunk, turn, v[i]);
         }
@@ -383,13 +386,13 @@ __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uin
     }
 }
 
-// The warp that brings the bf16 queries of row tile x to shared memory as f16, each row divided by a power of two (its largest
-// becomes 2^14 ... 2^15: exact as long as an element is no smaller than 2^-31 of it), in the layout that the copies leave.
+// The warp that brings the bf16 queries of row tile x to shared memory as f16, channels in the order of K's, each row divided by a
+// power of two (its largest becomes 2^14 ... 2^15: exact as long as an element is no smaller than 2^-31 of it).
 template <int D>
 __device__ __forceinline__ void convert_queries(const AttendParams& p, int x, uint8_t* q_tile, TileTail* tail) {
-    constexpr int kLanes = D / 8, kRows = 32 / kLanes, kAhead = 4;           // lanes of a row, rows of a step, steps under way
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes, kAhead = 8;           // lanes of a row, rows of a step, steps under way
     const int lane = threadIdx.x & 31, word = lane % kLanes, sub = lane / kLanes;
-    const int tokens = 128 / p.group, rows = tokens * p.group;
+    const int tokens = 128 / p.group;
     uint8_t* const column = q_tile + (word >> 3) * 128 * 128;
     ItemReader items{tail, p, 0, true, false};
     bool ok = true;
@@ -403,6 +406,8 @@ __device__ __forceinline__ void convert_queries(const AttendParams& p, int x, ui
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) continue;
         const int token0 = it.first_token + it.first_row / p.group + (it.fold != 0 ? 0 : x * tokens);
+        // the rows behind the sequence's last stay as they are: their products are not stored
+        const int rows = min(tokens * p.group, it.rows - it.first_row - (it.fold != 0 ? 0 : x * tokens * p.group));
         auto fetch = [&](int r) {
             const int t = r / p.group;
             return r < rows && token0 + t < p.c.total_q
@@ -416,14 +421,13 @@ __device__ __forceinline__ void convert_queries(const AttendParams& p, int x, ui
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) {
                 const uint32_t w[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
-                uint32_t seen = 0;                                            // NaN compares as the largest
+                uint32_t seen = 0, h[4];                                      // NaN compares as the largest
 #pragma unroll
                 for (int i = 0; i < 4; ++i) seen = max(seen, max((w[i] << 16) & 0x7FFF0000u, w[i] & 0x7FFF0000u));
 #pragma unroll
                 for (int o = 1; o < kLanes; o <<= 1) seen = max(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, o));
                 const uint32_t top = min(max(seen & 0x7F800000u, 15u << 23), 253u << 23);
                 const float up = __uint_as_float((268u << 23) - top);         // 2^14 over the power of two at or below the largest
-                uint32_t h[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 f = widen2<true>(w[i]);
@@ -431,7 +435,9 @@ __device__ __forceinline__ void convert_queries(const AttendParams& p, int x, ui
                 }
                 const int r = first + kRows * e;
                 if (r < rows) {
-                    *reinterpret_cast<uint4*>(column + r * 128 + (((word & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                    *reinterpret_cast<uint4*>(column + r * 128 + (((word & 7) ^ (r & 7)) << 4)) =
+                        make_uint4(__byte_perm(h[0], h[2], 0x5410), __byte_perm(h[0], h[2], 0x7632), __byte_perm(h[1], h[3], 0x5410),
+                                   __byte_perm(h[1], h[3], 0x7632));
                     if (word == 0) tail->row_exponent[x][r] = (uint8_t)((top >> 23) - 14u);
                 }
             }
@@ -467,8 +473,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendParams p) {
     using Shape = TileShape<D>;
     constexpr bool INT8 = KIND == SASQ_KV_INT8, INT4 = KIND == SASQ_KV_INT4, kCodes = KIND != SASQ_KV_16BIT;
-    constexpr bool PBF = BF && !kCodes, SBF = BF && !INT4;     // the second and the first product's type; else f16
     constexpr bool kConvertsQ = kQueriesConverted<BF, KIND>;
+    constexpr bool PBF = BF && !kCodes, SBF = BF && !INT4;     // the second and the first product's type; else f16
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* q_smem = smem;
@@ -994,15 +1000,17 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0;
                 }
-                if constexpr (INT4) {                              // V's factors, of the parts too
+                if constexpr (INT4) {                              // channels in their order; V's factors, of the parts too
                     const float4* f4 = reinterpret_cast<const float4*>(p.c.v_scale + it.h * D + c);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float4 f = __ldg(f4 + e);
-                        o[4 * e] = __float_as_uint(__uint_as_float(o[4 * e]) * factor4(f.x));
-                        o[4 * e + 1] = __float_as_uint(__uint_as_float(o[4 * e + 1]) * factor4(f.y));
-                        o[4 * e + 2] = __float_as_uint(__uint_as_float(o[4 * e + 2]) * factor4(f.z));
-                        o[4 * e + 3] = __float_as_uint(__uint_as_float(o[4 * e + 3]) * factor4(f.w));
+                    for (int e = 0; e < 32; e += 8) {
+                        const float4 a = __ldg(f4 + e / 4), b = __ldg(f4 + e / 4 + 1);
+                        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                        uint32_t v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(__uint_as_float(o[e + (k & 3) * 2 + (k >> 2)]) * factor4(f[k]));
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) o[e + k] = v[k];
                     }
                 }
                 if (valid && whole) {
