@@ -1,6 +1,8 @@
 // Attention for few query rows per KV head (decode steps, drafts): at most 8 * NB rows an item.
 #pragma once
 
+#include <type_traits>
+
 #include "paged_common.cuh"
 
 namespace sasq {
@@ -29,6 +31,14 @@ namespace {
 
 // Blocks of 16 keys of a warp's step: with 8 rows as many bytes are under way whatever the cache holds (16 rows' sums leave
 // no registers for that), and keys of a unit: a step of four warps.
+__device__ __forceinline__ uint4 lds_again(const uint4& x) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"((uint32_t)__cvta_generic_to_shared(&x)));
+    return v;
+}
+#ifndef QLOAD
+#define QLOAD lds_again
+#endif
 #ifndef SUB4
 #define SUB4 2
 #define BLK4 3
@@ -160,6 +170,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
     __shared__ float sm_m[WARPS][R], sm_l[WARPS][R];
     __shared__ float2 block_ml[R];                            // CLUSTER: the block's references and sums
     __shared__ alignas(16) float sm_o[WARPS][R][D];         // read back four at a time
+    // INT4: the queries' digits as the products take them, which leaves a warp's registers to its sums and loads
+    __shared__ uint4 sm_q[INT4 ? NB : 1][3][INT4 ? kSteps / 4 : 1][32];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
     pdl_launch_dependents();
@@ -205,7 +217,6 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 
         // queries: the fragment of row g of each block of 8 rows, in the order of the keys' words
         uint32_t qf[NB][2 * kSteps];
-        uint32_t qd[NB][3][INT4 ? kSteps : 1];               // INT4: the queries' digits, in their place
         int row_limit[NB][2];                                // keys that rows 2j, 2j + 1 see
         float row_scale[NB][2];                              // and what turns their products into powers of two
 #pragma unroll
@@ -269,6 +280,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                 const uint32_t top = max(seen & 0x7F800000u, 26u << 23);
                 const float up = __uint_as_float((275u << 23) - top);
                 unit = seen >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top - (25u << 23));    // less 16 times the code
+                uint32_t qd[3][kSteps];
 #pragma unroll
                 for (int w = 0; w < kSteps / 2; ++w) {       // a word's eight channels
                     uint32_t d[8];
@@ -278,11 +290,18 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {            // the even, then the odd ones
                         const uint32_t ab = __byte_perm(d[o], d[2 + o], 0x5140), cd = __byte_perm(d[4 + o], d[6 + o], 0x5140);
-                        qd[nb][0][2 * w + o] = __byte_perm(ab, cd, 0x5410) ^ 0x80808080u;
-                        qd[nb][1][2 * w + o] = __byte_perm(ab, cd, 0x7632) ^ 0x80808080u;
-                        qd[nb][2][2 * w + o] =
+                        qd[0][2 * w + o] = __byte_perm(ab, cd, 0x5410) ^ 0x80808080u;
+                        qd[1][2 * w + o] = __byte_perm(ab, cd, 0x7632) ^ 0x80808080u;
+                        qd[2][2 * w + o] =
                             __byte_perm(__byte_perm(d[o], d[2 + o], 0x0062), __byte_perm(d[4 + o], d[6 + o], 0x0062), 0x5410) ^ 0x80808080u;
                     }
+                }
+                if (warp == 0) {
+#pragma unroll
+                    for (int l = 0; l < 3; ++l)
+#pragma unroll
+                        for (int w = 0; w < kSteps / 4; ++w)
+                            sm_q[nb][l][w][lane] = make_uint4(qd[l][4 * w], qd[l][4 * w + 1], qd[l][4 * w + 2], qd[l][4 * w + 3]);
                 }
             }
 #pragma unroll
@@ -297,6 +316,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
         }
 
+        if (INT4) __syncthreads();                           // (the item before has been left by all)
         // keys that every row sees (rows behind the last ones see no fewer)
         int seen_by_all = limit;
         if (INT4) {
@@ -326,31 +346,31 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         const int last_key = min(it.t1 * kUnit, limit);
         int key = it.t0 * kUnit + warp * 16 * SUB;           // of this warp's step
 
-        // byte offset of key `at` of the sequence, or -1 when there is none or its page lies outside the cache
-        auto place = [&](int at) -> long long {
+        // byte offset of key `at` of the sequence (INT4: its page), or -1 when there is none or its page lies outside the cache
+        using Place = std::conditional_t<INT4, int, long long>;
+        auto place = [&](int at) -> Place {
             if (at >= last_key) return -1;
             const int page = __ldg(table + (at >> p.c.page_shift));
             if (page < 0 || page >= p.c.num_pages) {
                 atomicMax(p.c.status, (int)SASQ_ERR_BAD_INDEX);
                 return -1;
             }
-            return bytes(page * p.c.page_stride + (at & page_mask) * p.c.token_stride);
+            if constexpr (INT4) return page;
+            else return bytes(page * p.c.page_stride + (at & page_mask) * p.c.token_stride);
         };
         // INT4: where this lane's words lie behind a step's first row
         const long long one_row = bytes(p.c.token_stride), eight_rows = 8 * one_row;
         const char* const klane = kbase + g * one_row + D / 8 * j;
         const char* const vlane = vbase + 2 * j * one_row + D / 16 * g;
         uint4 kws[SUB][2][kWords];                            // keys g and g + 8
-        auto load_k = [&](int at, long long off, uint4 (&kw)[2][kWords]) {
+        auto load_k = [&](int at, Place off, uint4 (&kw)[2][kWords]) {
             if constexpr (INT4) {
-                const char* row = klane + off;
-                if (off >= 0 && at + 16 <= last_key) {         // all there, which a test of each costs much of a step
+                // any bits are codes: rows behind the last key, which lie in the same page, need no test (their logits are masked,
+                // their probabilities 0)
+                if (off >= 0) {
+                    const char* row = klane + bytes(off * p.c.page_stride) + (at & page_mask) * one_row;
 #pragma unroll
                     for (int r = 0; r < 2; ++r) kw[r][0] = load_codes<D / 32>(row + r * eight_rows);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        kw[r][0] = off >= 0 && at + g + 8 * r < last_key ? load_codes<D / 32>(row + r * eight_rows) : make_uint4(0, 0, 0, 0);
                 }
             } else {
 #pragma unroll
@@ -364,17 +384,16 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
         };
         uint32_t vws[SUB][4][VW];                             // keys 2j, 2j + 1, 2j + 8, 2j + 9
-        auto load_v = [&](int at, long long off, uint32_t (&vw)[4][VW]) {
+        auto load_v = [&](int at, Place off, uint32_t (&vw)[4][VW]) {
             if constexpr (INT4) {
-                const char* row = vlane + off;
-                const bool all = off >= 0 && at + 16 <= last_key;
+                if (off >= 0) {
+                    const char* row = vlane + bytes(off * p.c.page_stride) + (at & page_mask) * one_row;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int kk = 2 * j + (r & 1) + 8 * (r >> 1);
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (all || (off >= 0 && at + kk < last_key)) v = load_codes<VW>(row + (r & 1) * one_row + (r >> 1) * eight_rows);
-                    vw[r][0] = v.x;
-                    if constexpr (VW == 2) vw[r][1] = v.y;
+                    for (int r = 0; r < 4; ++r) {
+                        const uint4 v = load_codes<VW>(row + (r & 1) * one_row + (r >> 1) * eight_rows);
+                        vw[r][0] = v.x;
+                        if constexpr (VW == 2) vw[r][1] = v.y;
+                    }
                 }
             } else {
 #pragma unroll
@@ -400,7 +419,17 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             }
         };
 
-        long long off[SUB], off_next[SUB];
+        Place off[SUB], off_next[SUB];
+        if constexpr (INT4) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                kws[u][0][0] = kws[u][1][0] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) vws[u][r][w] = 0;
+            }
+        }
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             off[u] = place(key + 16 * u);
@@ -433,12 +462,22 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 #pragma unroll
                             for (int l = 0; l < 3; ++l) digit[nb][l][0] = digit[nb][l][1] = digit[nb][l][2] = digit[nb][l][3] = (int)kMagic;
 #pragma unroll
-                        for (int e = 0; e < D / 32; ++e) {
-                            const uint32_t a[4] = {k0[e] << 4 & 0xF0F0F0F0u, k1[e] << 4 & 0xF0F0F0F0u, k0[e] & 0xF0F0F0F0u, k1[e] & 0xF0F0F0F0u};
+                        for (int e = 0; e < D / 32; e += 2) {
+                            uint4 qq[NB][3];
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                                for (int l = 0; l < 3; ++l) mma_16832(digit[nb][l], a, qd[nb][l][2 * e], qd[nb][l][2 * e + 1]);
+                                for (int l = 0; l < 3; ++l) qq[nb][l] = QLOAD(sm_q[nb][l][e / 2][lane]);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const uint32_t a[4] = {k0[e + i] << 4 & 0xF0F0F0F0u, k1[e + i] << 4 & 0xF0F0F0F0u, k0[e + i] & 0xF0F0F0F0u,
+                                                       k1[e + i] & 0xF0F0F0F0u};
+#pragma unroll
+                                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                                    for (int l = 0; l < 3; ++l)
+                                        mma_16832(digit[nb][l], a, i == 0 ? qq[nb][l].x : qq[nb][l].z, i == 0 ? qq[nb][l].y : qq[nb][l].w);
+                            }
                         }
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb)
