@@ -179,7 +179,7 @@ template <int TOKENS, int STAGES, int G>
 struct W4Shape {
     static constexpr bool kDigits = TOKENS == 2;
     static constexpr int kWarps = TOKENS == 2 ? WARPS2 : TOKENS == 8 ? WARPS8 : WARPS16, kThreads = 32 * kWarps;
-    static constexpr int kPerSm = 16 / kWarps;             // blocks of an SM by their registers
+    static constexpr int kPerSm = kWarps <= 8 ? 2 : 1;     // blocks of an SM by their registers
     static constexpr int kRows = kDigits ? 16 : 32;        // of a tile
     static constexpr int kWindow = kDigits ? 256 : 128;    // columns of a step
     static constexpr int kRowBytes = kWindow / 2;
@@ -190,8 +190,10 @@ struct W4Shape {
     static constexpr int kTokenBytes = kDigits ? 3 * 256 : 256;    // of a token's window
     static constexpr int kPiece = kRows + 4;               // floats of a piece's token: neighbouring ones lie in different banks
     static size_t x_bytes(int tokens, int windows) { return (size_t)windows * (tokens * kTokenBytes + kTable); }
-    // the sums of whole tiles, two pieces of tiles for each warp, and whose they are
-    static size_t sum_bytes(int tokens, int tiles) { return ((size_t)tokens * (kRows * tiles + 4 + 2 * kWarps * kPiece) + 2 * kWarps) * sizeof(float); }
+    // The sums of whole tiles, the piece of a tile that a warp's run begins with, and whose pieces there are; the piece that a
+    // run ends with takes the place of its ring.
+    static size_t sum_bytes(int tokens, int tiles) { return ((size_t)tokens * (kRows * tiles + 4 + kWarps * kPiece) + 2 * kWarps) * sizeof(float); }
+    static_assert(TOKENS * kPiece * sizeof(float) <= (size_t)STAGES * kSlot, "a piece fits a warp's ring");
 };
 
 // A block has some row tiles and (in a cluster) a share of the columns' windows.  The windows of all its tiles, laid end to end,
@@ -219,8 +221,12 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
     const int sum_pitch = kRows * p.pass_tiles + 4;        // floats: neighbouring tokens lie in different banks
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * kSlot;
     float* const sums = reinterpret_cast<float*>(smem + Shape::kRing);
-    float* const pieces = sums + p.x_rows * sum_pitch;     // [warp][first or last][token] of Shape::kPiece
-    int* const piece_tile = reinterpret_cast<int*>(pieces + 2 * WK * p.x_rows * Shape::kPiece);
+    float* const pieces = sums + p.x_rows * sum_pitch;     // [warp][token] of Shape::kPiece: the first ones
+    int* const piece_tile = reinterpret_cast<int*>(pieces + WK * p.x_rows * Shape::kPiece);
+    // warp w's first or last piece
+    auto piece_of = [&](int w, int last) {
+        return last ? reinterpret_cast<float*>(smem + (size_t)w * STAGES * kSlot) : pieces + w * p.x_rows * Shape::kPiece;
+    };
     const uint32_t table = ptx::smem_u32(piece_tile + 2 * WK);                 // digits: a window's factors, [8]
     const uint32_t x_base = table + p.part_windows * Shape::kTable;            // [window][digit][token], or [window][token], of 256 bytes
     const uint32_t x_window = p.x_rows * Shape::kTokenBytes;
@@ -250,8 +256,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
     uint32_t w_place[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) w_place[r] = (w_row + kStep * r) * kRowBytes + ((w_chunk ^ turn(w_row + kStep * r)) << 4);
-    int load_pass = tile_begin, load_part = 0;
-    Run ld = run_of(load_pass, load_part);
+    Run ld = run_of(tile_begin, 0);
     uint32_t load_at = ring, load_row[4] = {0, 0, 0, 0};
     const uint8_t* load_w = p.w;
     auto enter_load = [&] {
@@ -261,18 +266,6 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
 #pragma unroll
         for (int r = 0; r < 4; ++r) load_row[r] = (uint32_t)min(w_row + kStep * r, p.N - 1 - first) * (uint32_t)half_k;
     };
-    auto settle = [&] {                                    // on to the next part or pass with work
-        while (ld.left == 0 && load_pass < tile_end) {
-            if (++load_part == p.parts) {
-                load_part = 0;
-                load_pass += p.pass_tiles;
-            }
-            if (load_pass < tile_end) {
-                ld = run_of(load_pass, load_part);
-                if (ld.left > 0) enter_load();
-            }
-        }
-    };
     auto load = [&] {
         if (ld.left > 0) {
             // columns behind the last are read from the last one's place, and meet zeros
@@ -280,21 +273,22 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
 #pragma unroll
             for (int r = 0; r < 4; ++r) copy16(load_at + w_place[r], src + load_row[r]);
             load_at = load_at + kSlot == ring + STAGES * kSlot ? ring : load_at + kSlot;
-            --ld.left;
             if (++ld.at == ld.windows) {
                 ld.at = 0;
                 ++ld.tile;
-                if (ld.left > 0) enter_load();
+                if (ld.left > 1) enter_load();
             }
-            settle();
+            --ld.left;
         }
         copies_end_group();
     };
-    // weights may be read at once, tokens when the kernels before this one are done
-    if (ld.left > 0) enter_load();
-    settle();
+    auto load_first = [&] {
+        if (ld.left > 0) enter_load();
 #pragma unroll 1
-    for (int s = 0; s < STAGES - 1; ++s) load();
+        for (int s = 0; s < STAGES - 1; ++s) load();
+    };
+    // weights may be read at once, tokens when the kernels before this one are done
+    load_first();
     pdl_wait();
 
     // The tokens of a part.  A lane has eight columns, chunk c of a window: group s, lane jj, word ii.
@@ -465,6 +459,10 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
             };
             if (r.left > 0) enter_sc(r.tile, r.at);
             __syncthreads();                               // the part before has been read
+            if (part > 0 || pass > tile_begin) {
+                ld = r;
+                load_first();
+            }
             if (lane < 2) piece_tile[2 * warp + lane] = -1;
             if (p.parts > 1 || pass == tile_begin) stage_x(part);
             __syncthreads();
@@ -568,15 +566,18 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
                         tot[0][0][e] += __shfl_xor_sync(0xFFFFFFFFu, tot[0][0][e], 2);
                     }
                 }
+                const bool whole = steps == windows, last = r.left == 0;           // else the end of a tile, or its beginning or middle
+                if (!whole && last) {
+                    copies_wait<0>();
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int t = 8 * nt + 2 * j + e;
                         if (t < tokens) {
-                            const bool whole = steps == windows;       // else the end of a tile, or its beginning or middle
-                            float* const to = whole ? sums + t * sum_pitch + kRows * (r.tile - pass) + g
-                                                    : pieces + ((2 * warp + (r.left == 0)) * p.x_rows + t) * Shape::kPiece + g;
+                            float* const to = whole ? sums + t * sum_pitch + kRows * (r.tile - pass) + g : piece_of(warp, last) + t * Shape::kPiece + g;
 #pragma unroll
                             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -586,7 +587,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
                                 }
                         }
                     }
-                if (steps != windows && lane == 0) piece_tile[2 * warp + (r.left == 0)] = r.tile - pass;
+                if (!whole && lane == 0) piece_tile[2 * warp + last] = r.tile - pass;
                 r.at = 0;
                 ++r.tile;
             }
@@ -598,13 +599,13 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
             const bool out = p.split == 1 && part + 1 == p.parts;
             each_row(0, 1, [&](int t, int row) {
                 float* const cell = sums + t * sum_pitch + row;
-                const float* const mine = pieces + t * Shape::kPiece + row % kRows;
+                const int mine = t * Shape::kPiece + row % kRows;
                 float v = 0.0f;
                 bool cut = windows == 0;
 #pragma unroll
                 for (int k = 0; k < 2 * WK; ++k)
                     if (tile_of[k] == row / kRows) {
-                        v += mine[k * p.x_rows * Shape::kPiece];
+                        v += piece_of(k >> 1, k & 1)[mine];
                         cut = true;
                     }
                 if (!cut) v = *cell;
@@ -630,7 +631,6 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
             ptx::cluster_sync_all();                       // nobody goes on, or leaves, while its sums are being read
         }
     }
-    copies_wait<0>();
 }
 
 // A warp per group: its largest magnitude, the factor as the linear uses it, the codes.
