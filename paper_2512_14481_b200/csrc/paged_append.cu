@@ -3,13 +3,16 @@
 // Pure movement: every element of q, k and v is read once and written once, in 16-byte words, with four multiplies per
 // rotated pair on the way.  Bound by DRAM for prompts (7815 tokens, 40 + 80 heads of 128, fp16: 80 us, 482 MB, 6.0 TB/s, 93 %
 // of a plain copy's rate) and by the launch for single tokens (2.8 us replayed from a graph).  4096 tokens into an int8 cache
-// (32 + 16 heads of 128, interleaved pairs, tokens first): 28.7 us, 94 MB, 3.3 TB/s; single tokens 3.4 us.
+// (32 + 16 heads of 128, interleaved pairs, tokens first): 28.7 us, 94 MB, 3.3 TB/s; single tokens 3.4 us.  4815 tokens into a
+// 4-bit cache (40 + 16 heads of 128, a factor for each channel): 34.5 us, 124 MB, 3.6 TB/s, bound by instructions; single
+// tokens 3.6 us.
 #include "paged_common.cuh"
 
 namespace sasq {
 namespace {
 
 constexpr int kAppendThreads = 256;
+constexpr int kAppend4Threads = 64;           // of many tokens into a 4-bit cache
 
 struct AppendParams {
     PagedParams c;
@@ -53,23 +56,23 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float inv) {
     return make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
 }
 
-// the same with b = 4, and eight of them in a word, the first in its low bits
-__device__ __forceinline__ uint32_t code4(float x, float inv) {
-    const float r = rintf(__fmul_rn(x, inv));
-    return (uint32_t)(int)fminf(fmaxf(r, -8.0f), 7.0f) & 15u;
-}
-// Codes of eight channels with a factor each; `bad` collects whether Eq. 1 can use them.
+// The same with b = 4 for eight channels with a factor each, the first in the word's low bits; `bad` collects whether Eq. 1 can
+// use the factors.  -8 and 7 are integers, so a value may be cut to them before it is rounded: adding 1.5 * 2^23 rounds it, and
+// with 8 more its low bits are the code + 8, which eight multiplications by 16 put together and one flip of their top bits turns
+// into codes.
 __device__ __forceinline__ uint32_t codes4(const float (&f)[8], const float* scale, bool* bad) {
     const float4 a = __ldg(reinterpret_cast<const float4*>(scale)), b = __ldg(reinterpret_cast<const float4*>(scale) + 1);
     const float s[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    constexpr uint32_t kRound = 0x4B400000u;                 // 1.5 * 2^23
     uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float t = factor4(s[i]);
-        *bad |= scale_is_bad(t);
-        w |= code4(f[i], __fdiv_rn(1.0f, t)) << (4 * i);
+    for (int i = 7; i >= 0; --i) {
+        const float inv = __frcp_rn(factor4(s[i]));
+        *bad |= !(fabsf(inv) > 0.0f && fabsf(inv) < __uint_as_float(0x7F800000u));      // a factor of 0, infinity or NaN, or too small
+        const float c = fminf(fmaxf(__fmul_rn(f[i], inv), -8.0f), 7.0f);
+        w = w * 16u + (__float_as_uint(__fadd_rn(c, __uint_as_float(kRound + 8u))) - kRound);
     }
-    return w;
+    return w ^ 0x88888888u;
 }
 
 // A thread owns a "unit" of a head, two 8-element words that the rotation mixes: words u and u + rot / 16 for half-split
@@ -88,6 +91,23 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
     const int h_begin = blockIdx.y * p.heads_per_block;
     const int h_end = min(h_begin + p.heads_per_block, total_heads);
     const bool idle = slot >= p.head_step;
+
+    const int pairs = p.rot >> 1;                // rotated pairs of a head
+    const bool turns = u < (p.rot >> 4);
+    const int w0 = (turns && !p.interleaved) ? u : 2 * u;
+    const int w1 = (turns && !p.interleaved) ? u + (p.rot >> 4) : 2 * u + 1;
+    // a head's two words, from q, k or v
+    auto fetch = [&](int h, uint4& x0, uint4& x1) {
+        const int which = h < p.q_heads ? 0 : h < p.q_heads + kv ? 1 : 2;
+        const int hh = which == 0 ? h : which == 1 ? h - p.q_heads : h - p.q_heads - kv;
+        const uint16_t* src = which == 0 ? p.q + t * p.q_stride : which == 1 ? p.k + t * p.k_stride : p.v + t * p.v_stride;
+        const uint4* words = reinterpret_cast<const uint4*>(src + (long long)hh * p.dim);
+        x0 = words[which == 2 ? 2 * u : w0];
+        x1 = words[which == 2 ? 2 * u + 1 : w1];
+    };
+    // 4-bit: the first head's words travel while the token's place is looked up, and a head's while the one before is turned
+    uint4 next0 = make_uint4(0, 0, 0, 0), next1 = next0;
+    if (INT4 && !idle && h_begin + slot < h_end) fetch(h_begin + slot, next0, next1);
 
     // the token's sequence: how many sequences end at or before it, counted by a warp at a time
     const int lane = threadIdx.x & 31;
@@ -117,10 +137,6 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
             row = page * p.c.page_stride + (pos & ((1 << p.c.page_shift) - 1)) * p.c.token_stride;
         }
     }
-    const int pairs = p.rot >> 1;                // rotated pairs of a head
-    const bool turns = u < (p.rot >> 4);
-    const int w0 = (turns && !p.interleaved) ? u : 2 * u;
-    const int w1 = (turns && !p.interleaved) ? u + (p.rot >> 4) : 2 * u + 1;
     float co[8], si[8];
     if (turns && there) {
         const float4* c4 = reinterpret_cast<const float4*>(p.cos_sin + (long long)pos * p.rot + 8 * u);
@@ -130,15 +146,21 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
         si[0] = s0.x; si[1] = s0.y; si[2] = s0.z; si[3] = s0.w; si[4] = s1.x; si[5] = s1.y; si[6] = s1.z; si[7] = s1.w;
     }
 
-#pragma unroll 4
+    constexpr int kUnroll = INT4 ? 1 : 4;
+#pragma unroll kUnroll
     for (int h = h_begin + slot; h < h_end; h += p.head_step) {
         const int which = h < p.q_heads ? 0 : h < p.q_heads + kv ? 1 : 2;
         const int hh = which == 0 ? h : which == 1 ? h - p.q_heads : h - p.q_heads - kv;
-        const uint16_t* src = which == 0 ? p.q + t * p.q_stride : which == 1 ? p.k + t * p.k_stride : p.v + t * p.v_stride;
         const bool turn = turns && which != 2;
         const int a0 = which == 2 ? 2 * u : w0, a1 = which == 2 ? 2 * u + 1 : w1;
-        const uint4* words = reinterpret_cast<const uint4*>(src + (long long)hh * p.dim);
-        uint4 x0 = words[a0], x1 = words[a1];
+        uint4 x0, x1;
+        if constexpr (INT4) {
+            x0 = next0;
+            x1 = next1;
+            if (h + p.head_step < h_end) fetch(h + p.head_step, next0, next1);
+        } else {
+            fetch(h, x0, x1);
+        }
         if (which != 0 && !there) continue;
         float f0[8], f1[8];
         if (turn || (KIND != SASQ_KV_16BIT && which != 0)) {
@@ -294,7 +316,11 @@ extern "C" int sasq_rope_kv_append(const sasq_kv_cache_t* cache, const sasq_kv_b
     p.interleaved = interleaved != 0;
     p.cos_sin = cos_sin;
     p.max_positions = max_positions;
-    p.head_step = kAppendThreads / (p.dim >> 4);
+    // Codes of 4 bits cost more instructions than DRAM's time covers, those before a thread's first head among them: with many
+    // tokens a thread takes more heads of one (4815 tokens of 40 + 16 heads of 128, fp16: 34.5 us with 64 threads a block,
+    // 36.5 with 128, 46.6 with 256).  Few tokens leave no choice but more threads.
+    const int threads = cache->kind == SASQ_KV_INT4 && batch->total_q >= 2 * sms ? kAppend4Threads : kAppendThreads;
+    p.head_step = threads / (p.dim >> 4);
     const int heads = p.q_heads + 2 * p.c.kv_heads;
     // few tokens: their heads spread over more blocks, so that a thread has one unit; many: one block per token, whose
     // threads keep their cosines and sines over all heads
@@ -303,7 +329,7 @@ extern "C" int sasq_rope_kv_append(const sasq_kv_cache_t* cache, const sasq_kv_b
     p.heads_per_block = (steps + ways - 1) / ways * p.head_step;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)batch->total_q, (unsigned)((heads + p.heads_per_block - 1) / p.heads_per_block));
-    cfg.blockDim = dim3(kAppendThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute attr = pdl_attribute();
     cfg.attrs = &attr;
