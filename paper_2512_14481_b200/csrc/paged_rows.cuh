@@ -31,20 +31,8 @@ namespace {
 
 // Blocks of 16 keys of a warp's step: with 8 rows as many bytes are under way whatever the cache holds (16 rows' sums leave
 // no registers for that), and keys of a unit: a step of four warps.
-__device__ __forceinline__ uint4 lds_again(const uint4& x) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"((uint32_t)__cvta_generic_to_shared(&x)));
-    return v;
-}
-#ifndef QLOAD
-#define QLOAD lds_again
-#endif
-#ifndef SUB4
-#define SUB4 2
-#define BLK4 3
-#endif
 template <int NB, int KIND>
-constexpr int kRowsSub = NB != 1 || KIND == SASQ_KV_16BIT ? 1 : KIND == SASQ_KV_INT4 ? SUB4 : 2;
+constexpr int kRowsSub = NB != 1 || KIND == SASQ_KV_16BIT ? 1 : 2;
 template <int NB, int KIND>
 constexpr int kRowsUnit = 64 * kRowsSub<NB, KIND>;
 constexpr int kClusterBlocks = 8;
@@ -125,12 +113,18 @@ __device__ __forceinline__ void mma_16832(int (&d)[4], const uint32_t (&a)[4], u
         : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 16 bytes of shared memory, read where it stands: the compiler may not keep them in registers over a loop
+__device__ __forceinline__ uint4 lds_again(const uint4& x) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"((uint32_t)__cvta_generic_to_shared(&x)));
+    return v;
+}
 constexpr uint32_t kMagic = 0x4B400000u;                     // 1.5 * 2^23
 
 // Blocks that an SM holds: as many as the registers of the fragments leave room for.  At this bound the variants for 8 rows
 // over int8 codes spill 4 to 20 bytes a thread, outside the loop over the keys (2072 local loads in a launch of 1776 warps).
 template <int D, int NB, int KIND>
-constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : KIND == SASQ_KV_INT4 ? (D == 128 ? BLK4 : BLK4 + 1) : D == 128 ? 3 : 4;
+constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
 
 // Both products are taken transposed, keys (then dimensions) on the 16-row side of m16n8k16 and query rows on its
 // 8-column side, so that one query row wastes 7/8 of the instruction and not 15/16, and neither K nor V passes through
@@ -467,7 +461,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                                for (int l = 0; l < 3; ++l) qq[nb][l] = QLOAD(sm_q[nb][l][e / 2][lane]);
+                                for (int l = 0; l < 3; ++l) qq[nb][l] = lds_again(sm_q[nb][l][e / 2][lane]);
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
                                 const uint32_t a[4] = {k0[e + i] << 4 & 0xF0F0F0F0u, k1[e + i] << 4 & 0xF0F0F0F0u, k0[e + i] & 0xF0F0F0F0u,
