@@ -347,15 +347,17 @@ SASQ_API int sasq_static_w8a8_linear_tiles(int64_t T, int64_t N, int num_pairs, 
 
 /* Linear layer with 4-bit weights and group factors, for the few tokens of a decode step: bound by the weights, half a byte
  * each.  Groups are `group` consecutive columns; c[n,k] in [-8, 7] are codes of Eq. 1 with b = 4:
- *   y[t,n] = narrow( sum_g s[n,g] * sum_{k in group g} x[t,k] c[n,k] (+ bias[n]) )      products exact, sums in fp32
- *                                                                                     (order unspecified, but fixed)
+ *   y[t,n] = narrow( sum_g s[n,g] * sum_{k in group g} x[t,k] c[n,k] (+ bias[n]) )      sums in fp32 (order
+ *                                                                                     unspecified, but fixed)
+ * The products are exact.  For one or two tokens x is first taken to 2^-22 of the largest of its 256 columns (256 i to
+ * 256 i + 255), half a step off at most, and a group's sum is exact.
  * x: [T, K] of `dt`, as it is.  w: [N, K / 2] bytes, column 2i in the low half of byte i, two's complement.  w_scale:
  * [N, K / group] of `dt`.  bias: [N] of `dt` or NULL, added in fp32.  y: [T, N] of `dt`, must not overlap x.
- * group: 32, 64 or 128, a divisor of K; any N; otherwise SASQ_ERR_UNSUPPORTED (also T > 2^20, N > 2^30, K > 2^24).  Any T
- * is served, 32 tokens at a time: for many tokens the W8A8 linears are the faster ones.  The weights are frozen: w and
+ * group: 32, 64 or 128, a divisor of K; any N; otherwise SASQ_ERR_UNSUPPORTED (also T > 2^19, N > 2^30, K > 2^24).  Any T
+ * is served, 16 tokens at a time: for many tokens the W8A8 linears are the faster ones.  The weights are frozen: w and
  * w_scale are read as soon as the kernel is resident, which can be before an earlier call of this library on the same stream
  * has finished; do not hand over a buffer that such a call is still writing (sasq_quantize_weight_w4 does not let its successor
- * start early).  A non-finite x reaches only its own token's row of y.  No workspace. */
+ * start early).  A non-finite x reaches only its own token's row of y (all of it, for one or two tokens).  No workspace. */
 SASQ_API int sasq_w4_linear(const void* x, const uint8_t* w, const void* w_scale, const void* bias, void* y, int64_t T,
                             int64_t N, int64_t K, int64_t group, int dt, void* stream);
 
@@ -449,7 +451,8 @@ SASQ_API size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, con
  * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 or 4-bit cache to f16.
  * Bit-identical from run to run for equal host bounds.  Infinities or NaN among a sequence's OWN keys and values are
  * outside the contract: they may reach any row of that sequence, rows that do not see them included.  A NaN in q makes
- * its own (token, head) NaN, out and lse, unless that sees no key.
+ * its own (token, head) NaN, out and lse, unless that sees no key.  4-bit cache: q times K's factors is taken, for
+ * few rows, to 2^-22 of the (token, head)'s largest; it and the logits have to be finite.
  * q: as for sasq_rope_kv_append (already rotated); out: [total_q, num_q_heads, head_dim] of `dt`, rows at out_stride;
  * must not alias q.  lse: [total_q, num_q_heads] fp32 (natural logarithm) or NULL.  head_dim: 64 or 128.
  * workspace: >= sasq_paged_attention_workspace() bytes, 16-byte aligned, contents need no initialisation; calls that

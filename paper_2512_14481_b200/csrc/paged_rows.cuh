@@ -635,8 +635,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     float2 v = make_float2(o[k][nb][e], o[k][nb][e + 2]);
                     if constexpr (INT4) {
                         const float2 f = __ldg(reinterpret_cast<const float2*>(p.c.v_scale + it.h * D + at));
-                        v.x = (v.x - lift[nb][e]) * (16777216.0f * factor4(f.x));
-                        v.y = fmaf(v.y, 0.0625f, -lift[nb][e]) * (16777216.0f * factor4(f.y));
+                        v.x = (v.x - lift[nb][e]) * 16777216.0f * factor4(f.x);
+                        v.y = fmaf(v.y, 0.0625f, -lift[nb][e]) * 16777216.0f * factor4(f.y);
                     }
                     *reinterpret_cast<float2*>(&sm_o[warp][r][at]) = v;
                 }

@@ -811,7 +811,7 @@ int sasq_w4_linear(const void* x, const uint8_t* w, const void* w_scale, const v
     if (w == nullptr || w_scale == nullptr || !aligned16(w) || !aligned16(w_scale) || !aligned16(bias)) return SASQ_ERR_INVALID_ARG;
     if (T > 0 && (x == nullptr || y == nullptr || !aligned16(x) || !aligned16(y) || x == y)) return SASQ_ERR_INVALID_ARG;
     if ((group != 32 && group != 64 && group != 128) || K % group != 0) return SASQ_ERR_UNSUPPORTED;
-    if (T > (1 << 20) || N > (1 << 30) || K > (1 << 24)) return SASQ_ERR_UNSUPPORTED;
+    if (T > (1 << 19) || N > (1 << 30) || K > (1 << 24)) return SASQ_ERR_UNSUPPORTED;
     if (T == 0) return SASQ_OK;
     const int sms = device_sm_count_if_sm100();
     if (sms <= 0) return SASQ_ERR_UNSUPPORTED;

@@ -56,3 +56,8 @@ def test_binding_refuses_cpu_tensors():
         P.sasq_w4_linear(x, w, s, torch.zeros((1, 8)).half())
     with pytest.raises(TypeError):
         P.sasq_quantize_weight_w4(torch.zeros((8, 64)), w, s)
+
+
+def test_the_most_tokens_and_columns(addr):
+    assert linear(addr, T=(1 << 19) + 1) == UNSUPPORTED and linear(addr, K=(1 << 24) + 128) == UNSUPPORTED
+    assert linear(addr, N=(1 << 30) + 1) == UNSUPPORTED
