@@ -2,7 +2,7 @@
 cache, attention over the cache, o linear.  Prompts go through in chunks, then every sequence gets one token a step, the
 step being replayed from a CUDA graph.  With --int4 the layer's weights have 4 bits with group factors, and the cache 4 bits
 with a factor for each channel (its linears are made for decode steps: of a prompt's chunk they read the weights once for every
-16 tokens).
+64 tokens).
 
     python examples/serve_attention.py [--batch 8] [--prompt 1000] [--steps 64] [--int8 | --int4]
 """

@@ -354,7 +354,7 @@ SASQ_API int sasq_static_w8a8_linear_tiles(int64_t T, int64_t N, int num_pairs, 
  * x: [T, K] of `dt`, as it is.  w: [N, K / 2] bytes, column 2i in the low half of byte i, two's complement.  w_scale:
  * [N, K / group] of `dt`.  bias: [N] of `dt` or NULL, added in fp32.  y: [T, N] of `dt`, must not overlap x.
  * group: 32, 64 or 128, a divisor of K; any N; otherwise SASQ_ERR_UNSUPPORTED (also T > 2^19, N > 2^30, K > 2^24).  Any T
- * is served, 16 tokens at a time: for many tokens the W8A8 linears are the faster ones.  The weights are frozen: w and
+ * is served, 64 tokens at a time: for many tokens the W8A8 linears are the faster ones.  The weights are frozen: w and
  * w_scale are read as soon as the kernel is resident, which can be before an earlier call of this library on the same stream
  * has finished; do not hand over a buffer that such a call is still writing (sasq_quantize_weight_w4 does not let its successor
  * start early).  A non-finite x reaches only its own token's row of y (all of it, for one or two tokens).  No workspace. */

@@ -147,6 +147,9 @@ constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
 //   O: masked in place, two nibbles are the two halves of an f16 operand (nibbles_low, nibbles_high): six instructions for eight codes
 //      of two keys each.  The nibble stands for code + 8: eight times the sum of the rounded probabilities is taken off again,
 //      which a product with a constant operand adds up.
+// 64 ragged sequences of 30 to 4500 keys, 32/8 heads of 128, bf16, 150 MB: 57 us, 2.6 TB/s, 40 % of a plain copy's rate (78 us with
+// the codes as f16 for both products and every key tested; 61 us with the queries' digits in registers); 8 sequences of 8000 to
+// 32000 keys: 53 us; one of 1000 keys, 32 heads, in clusters: 8.4 us.
 template <int D, int NB, bool BF, int KIND, bool CLUSTER, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, NB, KIND> : 1) paged_rows_kernel(const __grid_constant__ AttendParams p) {
     constexpr int R = 8 * NB, kThreads = 32 * WARPS;

@@ -274,6 +274,8 @@ __device__ __forceinline__ void store_codes4(uint8_t* tile, int r, int chunk, in
 
 // The warps that fill the ring from an int8 or 4-bit cache (`me` of kConvertThreads): K and V of each unit in turn, in the layout
 // that the 16-bit copies leave: keys along the rows, 128-byte swizzle.  Keys behind the sequence's last are zeros.
+// 4-bit, a chunk of 1024 tokens over 15000 keys, 32/8 heads of 128, bf16: 350 us, 744 TFLOP/s.  Neither the conversion nor its loads
+// bound it (without either the time stays), but the softmax chain at 128 registers a thread, as over int8 codes (305 us).
 template <int D, bool BF, int KIND>
 __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uint8_t* ring, TileTail* tail) {
     using Shape = TileShape<D>;

@@ -4,7 +4,11 @@
 //
 // Bound by the weights: half a byte each, read once.  The products run on mma.sync with 16 rows of weights on its wide side and
 // the tokens on the other, so that a weight goes from its byte to the operand in registers, where its group's factor can be
-// applied to the group's sum.
+// applied to the group's sum.  More than 16 tokens go to the tensor cores' fifth generation instead (w4_batch.cuh).
+//
+// Replayed from a graph, weights out of DRAM, bf16, groups of 128: one token of 4096 x 4096 4.5 us (floor 1.3: launch, two round
+// trips to memory, the meeting of the sums), of 22016 x 4096 9.6 us (4.8 TB/s, 75 % of a plain copy's rate); 8 tokens of 11008 x
+// 4096 11.3 us, 16 of 4096 x 4096 10.5 us; 7 of 5120 x 13824, groups of 64, 17.1 us (bound by instructions from 3 tokens on).
 #include <atomic>
 #include <type_traits>
 
@@ -29,6 +33,8 @@ struct W4Params {
     int pass_tiles;             // tiles whose sums a block holds at once
     int parts, part_windows;    // a block's windows are taken in parts whose tokens fit shared memory
     int sc_whole;               // a row's factors are whole windows
+    int* status;                // of waits that ran out, and their limit in clocks
+    long long wait_limit;
 };
 
 // 16 bytes from global to shared memory without a register
@@ -160,7 +166,7 @@ __device__ __forceinline__ void window_words(uint32_t row_base, int turn, int j,
 // digits to the base 256, from -128 to 127, are three columns of the product: digit l of token t is column 2 l + t.  A group's
 // sums are exact integers of at most 2^21; they start at the bits of the float 1.5 * 2^23, so that the float they end as is that
 // plus the sum.
-// FLOATS (up to 16 tokens; more in turns): exact products of 16-bit floats in fp32 sums, 32 rows at a time, so that what is read
+// FLOATS (up to 16 tokens): exact products of 16-bit floats in fp32 sums, 32 rows at a time, so that what is read
 // of x from shared memory serves twice.
 //
 // TOKENS: 2 for digits; 8 or 16.
@@ -314,64 +320,70 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
             next[e] = fetch(ahead);
             hop(ahead);
         }
+        // (a register under way can't be moved without waiting for it: the loads take turns with theirs)
+        bool more = true;
 #pragma unroll 1
-        for (; __any_sync(0xFFFFFFFFu, now.w < windows); hop(now)) {
-            const uint32_t raw[4] = {next[0].x, next[0].y, next[0].z, next[0].w};
-            const int w = now.w, t = now.t;
+        while (more) {
 #pragma unroll
-            for (int e = 0; e + 1 < kAhead; ++e) next[e] = next[e + 1];
-            next[kAhead - 1] = fetch(ahead);
-            hop(ahead);
-            if constexpr (kDigits) {
-                // Words 2q and 2q + 1 of lanes jj = 0 ... 3 lie side by side, and every other column of the product has
-                // neighbouring pairs the other way round, in other banks.
-                float f[8];
-                uint32_t seen = 0;                         // NaN compares as the largest
+            for (int turn_of = 0; turn_of < kAhead; ++turn_of) {
+                more = __any_sync(0xFFFFFFFFu, now.w < windows);
+                if (!more) break;
+                const uint32_t raw[4] = {next[turn_of].x, next[turn_of].y, next[turn_of].z, next[turn_of].w};
+                const int w = now.w, t = now.t;
+                hop(now);
+                next[turn_of] = fetch(ahead);
+                hop(ahead);
+                if constexpr (kDigits) {
+                    // Words 2q and 2q + 1 of lanes jj = 0 ... 3 lie side by side, and every other column of the product has
+                    // neighbouring pairs the other way round, in other banks.
+                    float f[8];
+                    uint32_t seen = 0;                         // NaN compares as the largest
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 a = widen2<BF>(raw[e]);
-                    f[2 * e] = a.x;
-                    f[2 * e + 1] = a.y;
-                    seen = max(seen, max(__float_as_uint(a.x) & 0x7FFFFFFFu, __float_as_uint(a.y) & 0x7FFFFFFFu));
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 a = widen2<BF>(raw[e]);
+                        f[2 * e] = a.x;
+                        f[2 * e + 1] = a.y;
+                        seen = max(seen, max(__float_as_uint(a.x) & 0x7FFFFFFFu, __float_as_uint(a.y) & 0x7FFFFFFFu));
+                    }
+                    seen = __reduce_max_sync(0xFFFFFFFFu, seen);
+                    // the largest becomes 2^21 ... 2^22
+                    const uint32_t top = max(seen & 0x7F800000u, 26u << 23);
+                    const float up = __uint_as_float((275u << 23) - top);
+                    uint32_t d[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        d[e] = __float_as_uint(fmaf(f[e], up, __uint_as_float(kMagic))) - kMagic + 0x00808080u;
+                    auto gather = [](uint32_t a, uint32_t b, uint32_t c4, uint32_t d4, uint32_t (&to)[3]) {
+                        const uint32_t ab = __byte_perm(a, b, 0x5140), cd = __byte_perm(c4, d4, 0x5140);
+                        to[0] = __byte_perm(ab, cd, 0x5410) ^ 0x80808080u;
+                        to[1] = __byte_perm(ab, cd, 0x7632) ^ 0x80808080u;
+                        to[2] = __byte_perm(__byte_perm(a, b, 0x0062), __byte_perm(c4, d4, 0x0062), 0x5410) ^ 0x80808080u;
+                    };
+                    uint32_t even[3], odd[3];                  // digits of columns 0, 2, 4, 6 and of 1, 3, 5, 7
+                    gather(d[0], d[2], d[4], d[6], even);
+                    gather(d[1], d[3], d[5], d[7], odd);
+                    const uint32_t place = (q >> 1) * 64 + jj * 16 + (q & 1) * 8;
+#pragma unroll
+                    for (int l = 0; l < 3; ++l) {
+                        const int row = l * p.x_rows + t;
+                        const uint32_t to = x_base + w * x_window + row * 256 + (place ^ ((row & 1) << 6));
+                        asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(even[l]), "r"(odd[l]) : "memory");
+                    }
+                    // factors: of the digit, less 16 times the code; a window with infinities or NaN: NaN; columns that stand for
+                    // nothing (others' digits): 0
+                    const float unit = seen >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top - (25u << 23));
+                    const int l = lane >> 1, tt = lane & 1;
+                    if (lane < 8 && (tt == t || (tt >= tokens && t == 0)))
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + w * Shape::kTable + lane * 4),
+                                     "f"(l < 3 && tt == t ? unit * __uint_as_float((127u + 8u * l) << 23) : 0.0f) : "memory");
+                } else if (w < windows) {
+                    // the pairs that come out of a word together: (0, 4), (2, 6), (1, 5), (3, 7).  Every other token has
+                    // neighbouring words the other way round, in other banks.
+                    const uint32_t to = x_base + w * x_window + t * 256 + ((q * 64 + jj * 16) ^ ((t & 1) << 6));
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(__byte_perm(raw[0], raw[2], 0x5410)),
+                                 "r"(__byte_perm(raw[1], raw[3], 0x5410)), "r"(__byte_perm(raw[0], raw[2], 0x7632)),
+                                 "r"(__byte_perm(raw[1], raw[3], 0x7632)) : "memory");
                 }
-                seen = __reduce_max_sync(0xFFFFFFFFu, seen);
-                // the largest becomes 2^21 ... 2^22
-                const uint32_t top = max(seen & 0x7F800000u, 26u << 23);
-                const float up = __uint_as_float((275u << 23) - top);
-                uint32_t d[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    d[e] = __float_as_uint(fmaf(f[e], up, __uint_as_float(kMagic))) - kMagic + 0x00808080u;
-                auto gather = [](uint32_t a, uint32_t b, uint32_t c4, uint32_t d4, uint32_t (&to)[3]) {
-                    const uint32_t ab = __byte_perm(a, b, 0x5140), cd = __byte_perm(c4, d4, 0x5140);
-                    to[0] = __byte_perm(ab, cd, 0x5410) ^ 0x80808080u;
-                    to[1] = __byte_perm(ab, cd, 0x7632) ^ 0x80808080u;
-                    to[2] = __byte_perm(__byte_perm(a, b, 0x0062), __byte_perm(c4, d4, 0x0062), 0x5410) ^ 0x80808080u;
-                };
-                uint32_t even[3], odd[3];                  // digits of columns 0, 2, 4, 6 and of 1, 3, 5, 7
-                gather(d[0], d[2], d[4], d[6], even);
-                gather(d[1], d[3], d[5], d[7], odd);
-                const uint32_t place = (q >> 1) * 64 + jj * 16 + (q & 1) * 8;
-#pragma unroll
-                for (int l = 0; l < 3; ++l) {
-                    const int row = l * p.x_rows + t;
-                    const uint32_t to = x_base + w * x_window + row * 256 + (place ^ ((row & 1) << 6));
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(even[l]), "r"(odd[l]) : "memory");
-                }
-                // factors: of the digit, less 16 times the code; a window with infinities or NaN: NaN; columns that stand for
-                // nothing (others' digits): 0
-                const float unit = seen >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top - (25u << 23));
-                const int l = lane >> 1, tt = lane & 1;
-                if (lane < 8 && (tt == t || (tt >= tokens && t == 0)))
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + w * Shape::kTable + lane * 4),
-                                 "f"(l < 3 && tt == t ? unit * __uint_as_float((127u + 8u * l) << 23) : 0.0f) : "memory");
-            } else if (w < windows) {
-                // the pairs that come out of a word together: (0, 4), (2, 6), (1, 5), (3, 7).  Every other token has
-                // neighbouring words the other way round, in other banks.
-                const uint32_t to = x_base + w * x_window + t * 256 + ((q * 64 + jj * 16) ^ ((t & 1) << 6));
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(__byte_perm(raw[0], raw[2], 0x5410)),
-                             "r"(__byte_perm(raw[1], raw[3], 0x5410)), "r"(__byte_perm(raw[0], raw[2], 0x7632)),
-                             "r"(__byte_perm(raw[1], raw[3], 0x7632)) : "memory");
             }
         }
     };
@@ -671,11 +683,10 @@ __global__ void __launch_bounds__(512, 1) cluster_room_kernel() {}
 // blocks alone would allow, for a cluster stays within a part of the chip (B200: 33 clusters of 8 at two an SM, not 37).
 int cluster_slots(int split, int per_sm, int threads, int sms) {
     if (split == 1) return sms * per_sm;
-    static std::atomic<int> known[64][4][4];               // (threads do not matter: shared memory decides)
+    static std::atomic<int> known[64][9][4];               // (threads do not matter: shared memory decides)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 1;
-    const int log = split == 2 ? 1 : split == 4 ? 2 : 3;
-    std::atomic<int>& k = known[dev & 63][log][per_sm & 3];
+    std::atomic<int>& k = known[dev & 63][split][per_sm & 3];
     if (k.load() == 0) {
         int n = 0;
         cudaLaunchConfig_t cfg{};
@@ -785,12 +796,23 @@ cudaError_t launch_w4(W4Params p, int sms, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, w4_linear_kernel<TOKENS, STAGES, BF, G>, p, kBits<BF>);
 }
 
+}  // namespace
+}  // namespace sasq
+
+#include "w4_batch.cuh"
+
+namespace sasq {
+namespace {
+
 template <bool BF, int G>
 cudaError_t launch_tokens(const W4Params& p, int sms, cudaStream_t st) {
     // windows of a ring: as many as leave the tokens their room
     if (p.T <= 2) return launch_w4<2, 4, BF, G>(p, sms, st);
     if (p.T <= 8) return launch_w4<8, 3, BF, G>(p, sms, st);
-    return launch_w4<16, 2, BF, G>(p, sms, st);
+    // (in turns of 16: 17 tokens of 4096 x 4096 14.8 us, here 9.6; 64 of 11008 x 4096 43.8 and 25.8, 32 of them 24.8 and 23.4; 61 of
+    // 6144 x 4096, groups of 32, 29.3 and 23.4; 16 tokens of 4096 x 4096 10.4 and 10.3, 12 of 11008 x 4096 14.3 and above 23)
+    if (p.T <= 16) return launch_w4<16, 2, BF, G>(p, sms, st);
+    return p.T <= 32 ? launch_w4_batch<32, BF, G>(p, sms, st) : launch_w4_batch<64, BF, G>(p, sms, st);
 }
 template <bool BF>
 cudaError_t launch_group(const W4Params& p, int group, int sms, cudaStream_t st) {
@@ -821,6 +843,9 @@ int sasq_w4_linear(const void* x, const uint8_t* w, const void* w_scale, const v
     p.ws = static_cast<const uint16_t*>(w_scale);
     p.bias = static_cast<const uint16_t*>(bias);
     p.y = static_cast<uint16_t*>(y);
+    p.wait_limit = debug_wait_limit();
+    p.status = paged_status_ptr();
+    if (p.status == nullptr) return SASQ_ERR_CUDA;
     p.T = (int)T;
     p.N = (int)N;
     p.K = (int)K;

@@ -134,3 +134,22 @@ def test_two_streams_and_two_graphs_at_once():
     assert P.sasq_device_status() == 0
     for _, _, out, y, want, want_y, _ in sides:
         assert torch.equal(out, want) and torch.equal(y, want_y)
+
+
+def test_a_linears_wait_that_runs_out_is_reported_and_the_next_call_is_clean():
+    """More than 16 tokens go through barriers; with a wait limit of zero cycles the kernel winds down, and the status word says so."""
+    x, codes, scale, _ = problem(40, 6000, 4096, 64, torch.bfloat16)
+    on = [t.cuda() for t in (x, R4.packed(codes), scale)]
+    y = torch.empty((40, 6000), dtype=torch.bfloat16, device="cuda")
+    assert P.sasq_device_status() == 0
+    P.sasq_debug_set_wait_limit(0)
+    try:
+        P.sasq_w4_linear(*on, y)
+        status = P.sasq_device_status()
+    finally:
+        P.sasq_debug_set_wait_limit(-1)
+    assert status == 5
+    P.sasq_w4_linear(*on, y)
+    assert P.sasq_device_status() == 0
+    want, tol = exact(x, codes, scale, None)
+    assert (np.abs(y.cpu().double().numpy() - want) <= tol).all()
