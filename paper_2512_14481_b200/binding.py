@@ -737,13 +737,23 @@ def sasq_w4_linear(x, w, w_scale, y, bias=None, stream=None) -> None:
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise TypeError("x must be a CUDA tensor")
     device, dt = x.get_device(), x.dtype
-    _on(device, (x, "x", None), (w, "w", torch.uint8), (w_scale, "w_scale", dt), (y, "y", dt), (bias, "bias", dt))
-    if x.dim() != 2 or w.dim() != 2 or w_scale.dim() != 2 or y.dim() != 2:
+    if _current_device() != device:
+        _on(device)
+    _flat(x, "x", device)
+    _flat(w, "w", device, torch.uint8)
+    _flat(w_scale, "w_scale", device, dt)
+    _flat(y, "y", device, dt)
+    if bias is not None:
+        _flat(bias, "bias", device, dt)
+    xs, ws, ss, ys = x.shape, w.shape, w_scale.shape, y.shape
+    if len(xs) != 2 or len(ws) != 2 or len(ss) != 2 or len(ys) != 2:
         raise ValueError("x, w, w_scale and y must be matrices")
-    (T, K), (N, half), (rows, groups) = x.shape, w.shape, w_scale.shape
-    if K != 2 * half or rows != N or groups <= 0 or K % groups != 0 or y.shape != (T, N) or (bias is not None and bias.shape != (N,)):
+    T, K = xs
+    N, half = ws
+    rows, groups = ss
+    if K != 2 * half or rows != N or groups <= 0 or K % groups != 0 or ys != (T, N) or (bias is not None and bias.shape != (N,)):
         raise ValueError(f"x [{T}, K], w [N, K / 2], w_scale [N, K / group], y [{T}, N] and bias [N] do not fit together: "
-                         f"{tuple(x.shape)}, {tuple(w.shape)}, {tuple(w_scale.shape)}, {tuple(y.shape)}")
+                         f"{tuple(xs)}, {tuple(ws)}, {tuple(ss)}, {tuple(ys)}")
     status = (_lib or load_library()).sasq_w4_linear(x.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _ptr(bias), y.data_ptr(), T, N, K,
                                                      K // groups, _dt(x), _stream_of(device, stream))
     if status != 0 or _DEBUG_STATUS:

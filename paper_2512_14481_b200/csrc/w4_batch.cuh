@@ -333,6 +333,9 @@ cudaError_t launch_w4_batch(W4Params p, int sms, cudaStream_t st) {
     p.windows_each = windows / p.split;
     p.windows_more = windows % p.split;
     p.sc_whole = p.K % Shape::kWindow == 0;
+    p.wait_limit = debug_wait_limit();
+    p.status = paged_status_ptr();
+    if (p.status == nullptr) return cudaErrorUnknown;
     static std::atomic<unsigned long long> ready{0};       // devices whose shared-memory limit has been raised
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

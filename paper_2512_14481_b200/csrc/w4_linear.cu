@@ -843,9 +843,6 @@ int sasq_w4_linear(const void* x, const uint8_t* w, const void* w_scale, const v
     p.ws = static_cast<const uint16_t*>(w_scale);
     p.bias = static_cast<const uint16_t*>(bias);
     p.y = static_cast<uint16_t*>(y);
-    p.wait_limit = debug_wait_limit();
-    p.status = paged_status_ptr();
-    if (p.status == nullptr) return SASQ_ERR_CUDA;
     p.T = (int)T;
     p.N = (int)N;
     p.K = (int)K;
