@@ -92,22 +92,17 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
     const int h_end = min(h_begin + p.heads_per_block, total_heads);
     const bool idle = slot >= p.head_step;
 
-    const int pairs = p.rot >> 1;                // rotated pairs of a head
-    const bool turns = u < (p.rot >> 4);
-    const int w0 = (turns && !p.interleaved) ? u : 2 * u;
-    const int w1 = (turns && !p.interleaved) ? u + (p.rot >> 4) : 2 * u + 1;
-    // a head's two words, from q, k or v
-    auto fetch = [&](int h, uint4& x0, uint4& x1) {
-        const int which = h < p.q_heads ? 0 : h < p.q_heads + kv ? 1 : 2;
-        const int hh = which == 0 ? h : which == 1 ? h - p.q_heads : h - p.q_heads - kv;
-        const uint16_t* src = which == 0 ? p.q + t * p.q_stride : which == 1 ? p.k + t * p.k_stride : p.v + t * p.v_stride;
-        const uint4* words = reinterpret_cast<const uint4*>(src + (long long)hh * p.dim);
-        x0 = words[which == 2 ? 2 * u : w0];
-        x1 = words[which == 2 ? 2 * u + 1 : w1];
-    };
     // 4-bit: the first head's words travel while the token's place is looked up, and a head's while the one before is turned
-    uint4 next0 = make_uint4(0, 0, 0, 0), next1 = next0;
-    if (INT4 && !idle && h_begin + slot < h_end) fetch(h_begin + slot, next0, next1);
+    [[maybe_unused]] uint4 next0, next1;
+    [[maybe_unused]] auto fetch = [&](int h) {
+        if (idle || h >= h_end) return;
+        const int which = h < p.q_heads ? 0 : h < p.q_heads + kv ? 1 : 2, step = which != 2 && u < (p.rot >> 4) && !p.interleaved ? p.rot >> 4 : 0;
+        const uint16_t* src = which == 0 ? p.q + t * p.q_stride : which == 1 ? p.k + t * p.k_stride : p.v + t * p.v_stride;
+        const uint4* words = reinterpret_cast<const uint4*>(src + (long long)(which == 0 ? h : which == 1 ? h - p.q_heads : h - p.q_heads - kv) * p.dim);
+        next0 = words[step != 0 ? u : 2 * u];
+        next1 = words[step != 0 ? u + step : 2 * u + 1];
+    };
+    if constexpr (INT4) fetch(h_begin + slot);
 
     // the token's sequence: how many sequences end at or before it, counted by a warp at a time
     const int lane = threadIdx.x & 31;
@@ -137,6 +132,10 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
             row = page * p.c.page_stride + (pos & ((1 << p.c.page_shift) - 1)) * p.c.token_stride;
         }
     }
+    const int pairs = p.rot >> 1;                // rotated pairs of a head
+    const bool turns = u < (p.rot >> 4);
+    const int w0 = (turns && !p.interleaved) ? u : 2 * u;
+    const int w1 = (turns && !p.interleaved) ? u + (p.rot >> 4) : 2 * u + 1;
     float co[8], si[8];
     if (turns && there) {
         const float4* c4 = reinterpret_cast<const float4*>(p.cos_sin + (long long)pos * p.rot + 8 * u);
@@ -151,15 +150,18 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
     for (int h = h_begin + slot; h < h_end; h += p.head_step) {
         const int which = h < p.q_heads ? 0 : h < p.q_heads + kv ? 1 : 2;
         const int hh = which == 0 ? h : which == 1 ? h - p.q_heads : h - p.q_heads - kv;
+        const uint16_t* src = which == 0 ? p.q + t * p.q_stride : which == 1 ? p.k + t * p.k_stride : p.v + t * p.v_stride;
         const bool turn = turns && which != 2;
         const int a0 = which == 2 ? 2 * u : w0, a1 = which == 2 ? 2 * u + 1 : w1;
         uint4 x0, x1;
         if constexpr (INT4) {
             x0 = next0;
             x1 = next1;
-            if (h + p.head_step < h_end) fetch(h + p.head_step, next0, next1);
+            fetch(h + p.head_step);
         } else {
-            fetch(h, x0, x1);
+            const uint4* words = reinterpret_cast<const uint4*>(src + (long long)hh * p.dim);
+            x0 = words[a0];
+            x1 = words[a1];
         }
         if (which != 0 && !there) continue;
         float f0[8], f1[8];

@@ -6,7 +6,8 @@ import torch
 
 import kv4_reference as R4
 import paper_2512_14481_b200 as P
-from test_gpu_kv4_attention import attend, check
+from test_gpu_kv4_append import run_case
+from test_gpu_kv4_attention import check
 from test_gpu_w4_linear import exact, problem, run
 
 pytestmark = pytest.mark.gpu
@@ -153,3 +154,10 @@ def test_a_linears_wait_that_runs_out_is_reported_and_the_next_call_is_clean():
     assert P.sasq_device_status() == 0
     want, tol = exact(x, codes, scale, None)
     assert (np.abs(y.cpu().double().numpy() - want) <= tol).all()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dim,rot", [(32, 32), (96, 32), (160, 0), (224, 224), (256, 128)])
+def test_many_tokens_of_other_head_dims(dim, rot, in_place):
+    """Many tokens go to blocks of 64 threads, which every head_dim shares out in its own way."""
+    run_case([300, 0, 7, 350], [250, 0, 7, 340], 7, 3, dim, 32, torch.bfloat16, rot, dim == 96, in_place=in_place)
