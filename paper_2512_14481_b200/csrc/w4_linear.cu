@@ -211,8 +211,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
     const int rank = p.split > 1 ? (int)ptx::cluster_ctarank() : 0;
     const int cluster = blockIdx.x >> p.split_log;
-    const int t0 = kDigits ? 0 : blockIdx.y * TOKENS;      // tokens of this block
-    const int tokens = kDigits ? p.T : min(TOKENS, p.T - t0);
+    const int tokens = p.T;
     const int tile_begin = cluster * p.tiles_each + min(cluster, p.tiles_more), tile_end = tile_begin + p.tiles_each + (cluster < p.tiles_more);
     const int begin = rank * p.windows_each + min(rank, p.windows_more), end = begin + p.windows_each + (rank < p.windows_more);
     const int half_k = p.K >> 1;                           // bytes of a weight row
@@ -307,7 +306,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
         };
         auto fetch = [&](const Pair& a) {
             const int col = (from + a.w) * kWindow + 8 * c;
-            return a.w < windows && col < p.K ? *reinterpret_cast<const uint4*>(p.x + (long long)(t0 + a.t) * p.K + col) : make_uint4(0, 0, 0, 0);
+            return a.w < windows && col < p.K ? *reinterpret_cast<const uint4*>(p.x + (long long)a.t * p.K + col) : make_uint4(0, 0, 0, 0);
         };
         constexpr int kAhead = kDigits ? 2 : 4;            // loads that travel while one is taken apart
         Pair now, ahead;
@@ -400,7 +399,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
         const int n_row = kRows * pass + row;
         if (n_row >= p.N) return;
         if (p.bias != nullptr) v += widen1<BF>(p.bias[n_row]);
-        p.y[(long long)(t0 + t) * p.N + n_row] = narrow1<BF>(v);
+        p.y[(long long)t * p.N + n_row] = narrow1<BF>(v);
     };
     uint32_t at = ring;                                    // the slot that is read next
     for (int pass = tile_begin; pass < tile_end; pass += p.pass_tiles) {
@@ -714,7 +713,7 @@ struct W4Plan {
     size_t smem;
 };
 template <int TOKENS, int STAGES, int G>
-W4Plan plan_w4(int tiles_all, int windows_all, int x_rows, int chunks, int sms) {
+W4Plan plan_w4(int tiles_all, int windows_all, int x_rows, int sms) {
     using Shape = W4Shape<TOKENS, STAGES, G>;
     W4Plan best{};
     long long least = -1;
@@ -722,8 +721,8 @@ W4Plan plan_w4(int tiles_all, int windows_all, int x_rows, int chunks, int sms) 
         const int windows = ceil_div(windows_all, split);
         for (int per_sm = Shape::kPerSm; per_sm >= 1; --per_sm) {
             const long long room = kSmSmem / per_sm - 1024 - Shape::kRing;
-            const int slots = cluster_slots(split, per_sm, Shape::kThreads, sms) / chunks;
-            const int clusters = tiles_all < slots ? tiles_all : slots < 1 ? 1 : slots;
+            const int slots = cluster_slots(split, per_sm, Shape::kThreads, sms);
+            const int clusters = tiles_all < slots ? tiles_all : slots;
             const int tiles = ceil_div(tiles_all, clusters);
             // sums of the block's rows get up to half of the room, tokens the rest
             int passes = 1;
@@ -750,18 +749,18 @@ W4Plan plan_w4(int tiles_all, int windows_all, int x_rows, int chunks, int sms) 
 template <int TOKENS, int STAGES, bool BF, int G>
 cudaError_t launch_w4(W4Params p, int sms, cudaStream_t st) {
     using Shape = W4Shape<TOKENS, STAGES, G>;
-    const int chunks = ceil_div(p.T, TOKENS), tiles = ceil_div(p.N, Shape::kRows), windows = ceil_div(p.K, Shape::kWindow);
-    p.x_rows = p.T < TOKENS ? p.T : TOKENS;
+    const int tiles = ceil_div(p.N, Shape::kRows), windows = ceil_div(p.K, Shape::kWindow);
+    p.x_rows = p.T;
     p.sc_whole = p.K % Shape::kWindow == 0;
     // a decode loop asks for the same few shapes again and again: the last ones' plans are kept, by their sizes
     struct Known {
-        int tiles, windows, x_rows, chunks, sms;
+        int tiles, windows, x_rows, sms;
         W4Plan plan;
     };
     static thread_local Known known[8];
     Known& k = known[(unsigned)(tiles * 31 + windows * 7 + p.x_rows) % 8];
-    if (k.tiles != tiles || k.windows != windows || k.x_rows != p.x_rows || k.chunks != chunks || k.sms != sms)
-        k = Known{tiles, windows, p.x_rows, chunks, sms, plan_w4<TOKENS, STAGES, G>(tiles, windows, p.x_rows, chunks, sms)};
+    if (k.tiles != tiles || k.windows != windows || k.x_rows != p.x_rows || k.sms != sms)
+        k = Known{tiles, windows, p.x_rows, sms, plan_w4<TOKENS, STAGES, G>(tiles, windows, p.x_rows, sms)};
     p.split = k.plan.split;
     for (p.split_log = 0; 1 << p.split_log < p.split; ++p.split_log) {}
     p.tiles_each = tiles / k.plan.clusters;
@@ -782,7 +781,7 @@ cudaError_t launch_w4(W4Params p, int sms, cudaStream_t st) {
         ready.fetch_or(1ull << (dev & 63));
     }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(k.plan.clusters * p.split), (unsigned)chunks);
+    cfg.gridDim = dim3((unsigned)(k.plan.clusters * p.split));
     cfg.blockDim = dim3(Shape::kThreads);
     cfg.dynamicSmemBytes = k.plan.smem;
     cfg.stream = st;
