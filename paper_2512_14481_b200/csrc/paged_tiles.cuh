@@ -408,7 +408,7 @@ __device__ __forceinline__ void convert_queries(const AttendParams& p, int x, ui
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) continue;
         const int token0 = it.first_token + it.first_row / p.group + (it.fold != 0 ? 0 : x * tokens);
-        // the rows behind the sequence's last stay as they are: their products are not stored
+        // the rows behind the sequence's last stay as they are: they move no row's reference, and nothing of them is stored
         const int rows = min(tokens * p.group, it.rows - it.first_row - (it.fold != 0 ? 0 : x * tokens * p.group));
         auto fetch = [&](int r) {
             const int t = r / p.group;
@@ -916,7 +916,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (step == 0) continue;
                     if (step == 1) {
                         most *= scale;
-                        if (__any_sync(0xFFFFFFFFu, most > m + (kRescaleAt + kHeadroom<!PBF>))) {
+                        // rows that no query owns hold what shared memory held, or others' queries: they have no vote
+                        if (__any_sync(0xFFFFFFFFu, valid && most > m + (kRescaleAt + kHeadroom<!PBF>))) {
                             const float m_new = fmaxf(m, most - kHeadroom<!PBF>);
                             const float f = m_new == -INFINITY ? 1.0f : exp2_approx(m - m_new);
                             m = m_new;
