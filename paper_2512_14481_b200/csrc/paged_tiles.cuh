@@ -493,7 +493,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&tail->q_full[x], 1);
             ptx::mbar_init(&tail->q_empty[x], 1);
-            ptx::mbar_init(&tail->unit_empty[x], 4);
+            if constexpr (kConvertsQ) ptx::mbar_init(&tail->unit_empty[x], 4);      // (elsewhere it costs: 16-bit mixed batch 128.5 us against 125.5)
             ptx::mbar_init(&tail->s_full[x], 1);
             ptx::mbar_init(&tail->p_full[x][0], 128);
             ptx::mbar_init(&tail->p_full[x][1], 128);
