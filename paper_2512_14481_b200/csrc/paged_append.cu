@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
     const int h_end = min(h_begin + p.heads_per_block, total_heads);
     const bool idle = slot >= p.head_step;
 
-    // 4-bit: the first head's words travel while the token's place is looked up, and a head's while the one before is turned
+    // 4-bit: the first head's words travel while the token's page is looked up, and a head's while the one before is turned
     [[maybe_unused]] uint4 next0, next1;
     [[maybe_unused]] auto fetch = [&](int h) {
         if (idle || h >= h_end) return;
@@ -102,7 +102,6 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
         next0 = words[step != 0 ? u : 2 * u];
         next1 = words[step != 0 ? u + step : 2 * u + 1];
     };
-    if constexpr (INT4) fetch(h_begin + slot);
 
     // the token's sequence: how many sequences end at or before it, counted by a warp at a time
     const int lane = threadIdx.x & 31;
@@ -114,6 +113,7 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv_append_kernel(const __
     if (b >= p.c.batch || idle) return;          // padding behind the last sequence
     const Sequence s = load_sequence(p.c, b);
     if (t < s.first || t >= s.first + s.new_len) return;
+    if constexpr (INT4) fetch(h_begin + slot);   // rows of padding are not read
     // from the length as given: a token that the table has no room for is skipped, it does not move to another's place
     const long long place = (long long)s.given_len - s.new_len + (t - s.first);
     bool there = place >= 0 && place < (long long)p.c.max_pages << p.c.page_shift;      // (reported by load_sequence)
