@@ -640,9 +640,8 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
                     const int at = INT8 || INT4 ? (D / 8) * g + 2 * k : 8 * (g + 8 * (k >> 2)) + 2 * (k & 3);
                     float2 v = make_float2(o[k][nb][e], o[k][nb][e + 2]);
                     if constexpr (INT4) {
-                        const float2 f = __ldg(reinterpret_cast<const float2*>(p.c.v_scale + it.h * D + at));
-                        v.x = (v.x - lift[nb][e]) * 16777216.0f * factor4(f.x);
-                        v.y = fmaf(v.y, 0.0625f, -lift[nb][e]) * 16777216.0f * factor4(f.y);
+                        v.x = (v.x - lift[nb][e]) * 16777216.0f;
+                        v.y = fmaf(v.y, 0.0625f, -lift[nb][e]) * 16777216.0f;
                     }
                     *reinterpret_cast<float2*>(&sm_o[warp][r][at]) = v;
                 }
@@ -654,11 +653,21 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
         // four elements of the item's result
         auto write = [&](int r, int d, float m, float sum, const float (&acc)[4]) {
             const float inv = sum != 0.0f ? vs / sum : 0.0f;      // 0: a row without keys; NaN is not one
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = acc[i] * inv;
+            if constexpr (INT4) {                            // averages of codes meet V's factors: finite where a factor is
+                const float4 f = __ldg(reinterpret_cast<const float4*>(p.c.v_scale + it.h * D + d));
+                y[0] *= factor4(f.x);
+                y[1] *= factor4(f.y);
+                y[2] *= factor4(f.z);
+                y[3] *= factor4(f.w);
+            }
             const int row = first_row + r, tok = row / p.group;
             const int head = it.h * p.group + row - tok * p.group;
             const long long t = it.s.first + tok;
             *reinterpret_cast<uint2*>(p.out + t * p.out_stride + (long long)head * D + d) =
-                make_uint2(narrow2<BF>(acc[0] * inv, acc[1] * inv), narrow2<BF>(acc[2] * inv, acc[3] * inv));
+                make_uint2(narrow2<BF>(y[0], y[1]), narrow2<BF>(y[2], y[3]));
             if (d == 0 && p.lse != nullptr)
                 p.lse[t * p.heads + head] = sum != 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
         };
@@ -753,7 +762,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
     const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const PartItem pi = p.part_items[c];
     if (pi.last < 0) return;
-    const float vs = p.c.kind == SASQ_KV_INT8 ? __ldg(p.c.v_scale + pi.h) : 1.0f;      // (4-bit: already in the parts)
+    const float vs = p.c.kind == SASQ_KV_INT8 ? __ldg(p.c.v_scale + pi.h) : 1.0f;
     constexpr int kStep = WIDE ? 8 : 1;                        // parts from one of a warp to its next
     for (int r = WIDE ? blockIdx.y : blockIdx.y * 8 + warp; r < R; r += WIDE ? gridDim.y : gridDim.y * 8) {
         const int item_row = r / TILE * pi.tile_rows + r % TILE;
@@ -816,7 +825,14 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
         const long long t = pi.first_token + tok;
         uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + t * p.out_stride + (long long)head * D + lane * N);
 #pragma unroll
-        for (int e = 0; e < N / 2; ++e) dst[e] = narrow2<BF>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+        for (int e = 0; e < N; ++e) acc[e] *= inv;
+        if (p.c.kind == SASQ_KV_INT4) {
+            const float* f = p.c.v_scale + pi.h * D + lane * N;
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] *= factor4(__ldg(f + e));
+        }
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) dst[e] = narrow2<BF>(acc[2 * e], acc[2 * e + 1]);
         if (lane == 0 && p.lse != nullptr)
             p.lse[t * p.heads + head] = sum != 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
     }

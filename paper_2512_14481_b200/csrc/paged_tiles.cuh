@@ -978,6 +978,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             const bool whole = it.whole;
             const float inv = sum != 0.0f ? (INT8 ? __ldg(p.c.v_scale + it.h) : 1.0f) / sum : 0.0f;
+            const float times = INT4 ? 1.0f : inv;                 // (4-bit: already taken)
             const int tok = item_row / p.group;
             const int head = it.h * p.group + item_row - tok * p.group;
             const long long token = it.first_token + tok;
@@ -1003,7 +1004,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0;
                 }
-                if constexpr (INT4) {                              // channels in their order; V's factors, of the parts too
+                if constexpr (INT4) {                              // channels in their order; a whole item's averages meet V's factors
                     const float4* f4 = reinterpret_cast<const float4*>(p.c.v_scale + it.h * D + c);
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
@@ -1011,7 +1012,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
                         uint32_t v[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(__uint_as_float(o[e + (k & 3) * 2 + (k >> 2)]) * factor4(f[k]));
+                        for (int k = 0; k < 8; ++k) {
+                            v[k] = o[e + (k & 3) * 2 + (k >> 2)];
+                            if (whole) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv * factor4(f[k]));
+                        }
 #pragma unroll
                         for (int k = 0; k < 8; ++k) o[e + k] = v[k];
                     }
@@ -1023,7 +1027,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         uint32_t w[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            w[k] = sum != 0.0f ? narrow2<BF>(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv) : 0u;
+                            w[k] = sum != 0.0f ? narrow2<BF>(__uint_as_float(o[8 * e + 2 * k]) * times, __uint_as_float(o[8 * e + 2 * k + 1]) * times) : 0u;
                         dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 } else if (valid) {
