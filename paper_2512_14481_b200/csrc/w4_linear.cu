@@ -119,12 +119,13 @@ __device__ __forceinline__ void mma_float(float (&d)[4], const uint32_t (&a)[4],
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 constexpr uint32_t kMagic = 0x4B400000u;                   // 1.5 * 2^23
+constexpr uint32_t kSumStart = kMagic - (22u << 23);       // 1.5 * 2: sums of digits count in 2^-22
 template <bool FIRST>
 __device__ __forceinline__ void mma_s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (FIRST)
         asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
             : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(kMagic));
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(kSumStart));
     else
         asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
@@ -164,8 +165,8 @@ __device__ __forceinline__ void window_words(uint32_t row_base, int turn, int j,
 // times the code, they are a shift and two masks, and one s8 product of m16n8k32 takes twice as many of them.  So x becomes
 // integers: in a window of 256 columns a token's values are multiples of a power of two, 2^-22 of the window's largest, whose
 // digits to the base 256, from -128 to 127, are three columns of the product: digit l of token t is column 2 l + t.  A group's
-// sums are exact integers of at most 2^21; they start at the bits of the float 1.5 * 2^23, so that the float they end as is that
-// plus the sum.
+// sums are exact integers of at most 2^21; they start at the bits of the float 1.5 * 2, so that the float they end as is that plus
+// the sum times 2^-22.
 // FLOATS (up to 16 tokens): exact products of 16-bit floats in fp32 sums, 32 rows at a time, so that what is read
 // of x from shared memory serves twice.
 //
@@ -184,7 +185,7 @@ struct W4Shape {
     static constexpr int kSlot = kRows * kRowBytes;        // a window of a tile: 2 KB
     static constexpr int kRing = kWarps * STAGES * kSlot;
     static constexpr int kTiles = kDigits ? 1 : TOKENS / 8;        // 8-column blocks of the product
-    static constexpr int kTable = kDigits ? 32 : 0;        // bytes of a window's factors, one for each column
+    static constexpr int kTable = kDigits ? 32 : 0;        // bytes of a window's units, one for each column
     static constexpr int kTokenBytes = kDigits ? 3 * 256 : 256;    // of a token's window
     static constexpr int kPiece = kRows + 4;               // floats of a piece's token: neighbouring ones lie in different banks
     static size_t x_bytes(int tokens, int windows) { return (size_t)windows * (tokens * kTokenBytes + kTable); }
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
     auto piece_of = [&](int w, int last) {
         return last ? reinterpret_cast<float*>(smem + (size_t)w * STAGES * kSlot) : pieces + w * p.x_rows * Shape::kPiece;
     };
-    const uint32_t table = ptx::smem_u32(piece_tile + 2 * WK);                 // digits: a window's factors, [8]
+    const uint32_t table = ptx::smem_u32(piece_tile + 2 * WK);                 // digits: a window's units, [8]
     const uint32_t x_base = table + p.part_windows * Shape::kTable;            // [window][digit][token], or [window][token], of 256 bytes
     const uint32_t x_window = p.x_rows * Shape::kTokenBytes;
     pdl_launch_dependents();
@@ -368,13 +369,12 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
                         const uint32_t to = x_base + w * x_window + row * 256 + (place ^ ((row & 1) << 6));
                         asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(even[l]), "r"(odd[l]) : "memory");
                     }
-                    // factors: of the digit, less 16 times the code; a window with infinities or NaN: NaN; columns that stand for
-                    // nothing (others' digits): 0
-                    const float unit = seen >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top - (25u << 23));
+                    // What the lowest digit stands for, less 16 times the code, times the 2^22 that sums of digits lack; a window with
+                    // infinities or NaN: NaN; columns that stand for nothing (others' digits): 0
+                    const float unit = seen >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top - (3u << 23));
                     const int l = lane >> 1, tt = lane & 1;
                     if (lane < 8 && (tt == t || (tt >= tokens && t == 0)))
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + w * Shape::kTable + lane * 4),
-                                     "f"(l < 3 && tt == t ? unit * __uint_as_float((127u + 8u * l) << 23) : 0.0f) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + w * Shape::kTable + lane * 4), "f"(l < 3 && tt == t ? unit : 0.0f) : "memory");
                 } else if (w < windows) {
                     // the pairs that come out of a word together: (0, 4), (2, 6), (1, 5), (3, 7).  Every other token has
                     // neighbouring words the other way round, in other banks.
@@ -505,6 +505,9 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
                     for (int e = 0; e < 2 * MT; ++e) window_words<G>(at + (8 * e + g) * kRowBytes, turn(8 * e + g), j, wv[e]);
                     at = at + kSlot == ring + STAGES * kSlot ? ring : at + kSlot;
                     if constexpr (kDigits) {
+                        // Nothing on the way passes fp32's end: a window's sums are below 2^22 2^-22 times its largest factor, a unit
+                        // is at most 2^124, and digit j's power of 256 comes behind all windows.  (A sum times a factor below 2^-104
+                        // may be a subnormal number, off by 2^-150.)
                         float win[4];
                         int acc[4];
 #pragma unroll
@@ -520,7 +523,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
                                 if (q % WG == WG - 1) {
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) {
-                                        const float v = __int_as_float(acc[e]) - __uint_as_float(kMagic);
+                                        const float v = __int_as_float(acc[e]) - __uint_as_float(kSumStart);
                                         win[e] = s == 0 ? v * sc[e >> 1][s] : fmaf(v, sc[e >> 1][s], win[e]);
                                     }
                                 }
@@ -565,6 +568,7 @@ __global__ void __launch_bounds__(W4Shape<TOKENS, STAGES, G>::kThreads, W4Shape<
                 if constexpr (kDigits) {                   // the digits' columns meet, among the four lanes of a row
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
+                        tot[0][0][e] *= __uint_as_float((127u + 8u * j) << 23);
                         tot[0][0][e] += __shfl_xor_sync(0xFFFFFFFFu, tot[0][0][e], 1);
                         tot[0][0][e] += __shfl_xor_sync(0xFFFFFFFFu, tot[0][0][e], 2);
                     }
