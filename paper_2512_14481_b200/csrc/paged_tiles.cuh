@@ -858,14 +858,15 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 uint32_t largest = 0;
 #pragma unroll
                 for (int d = lane; d < D; d += 32) largest = max(largest, __float_as_uint(factor4(__ldg(p.c.k_scale + it.h * D + d))) & 0x7FFFFFFFu);
-                signed_scale *= __uint_as_float(head_unit(__reduce_max_sync(0xFFFFFFFFu, largest)));
+                float unit = __uint_as_float(head_unit(__reduce_max_sync(0xFFFFFFFFu, largest)));
                 if (kConvertsQ && any) {
                     if (!wait(&tail->q_full[x], q_fills & 1u)) break;
-                    signed_scale *= __uint_as_float((uint32_t)tail->row_exponent[x][row] << 23);
+                    unit *= __uint_as_float((uint32_t)tail->row_exponent[x][row] << 23);
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(&tail->unit_empty[x]);
                     ++q_fills;
                 }
+                signed_scale *= unit;                              // (one by one a far scale and unit may leave a subnormal number)
             }
             // A scale of zero, or one that vanished in the product with the factor, would turn masked logits, -inf, into NaN; the
             // smallest number there is gives the same equal weights.

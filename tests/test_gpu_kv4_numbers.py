@@ -90,3 +90,17 @@ def test_long_keys_with_faint_logits(new, hi, dim, dtype):
             else:
                 tol = tol + (l + 40) * 2.0 ** -23 * size
             assert (np.abs(got[rows, c] - want) <= tol).all()
+
+
+@pytest.mark.parametrize("new", [1, 4, 50])
+@pytest.mark.parametrize("q_by,f_by,s_by", [(60, -60, 0), (-60, 60, 0), (-90, 60, 30), (-80, 112, -32), (118, -100, -18), (122, -92, -30), (110, -116, 6)])
+def test_powers_of_two_cancel(new, q_by, f_by, s_by):
+    """Queries, key factors and the scale times powers of two whose product is 1: the same logits, bit for bit."""
+    results = []
+    for by in ((0, 0, 0), (q_by, f_by, s_by)):
+        bt = R4.Batch([400, 333], [new, new], 4, 2, 128, 16, torch.bfloat16, seed=4)
+        bt.k_scale = bt.k_scale * 2.0 ** by[1]
+        bt.q_wide = bt.q_wide * 2.0 ** by[0]
+        bt.q = bt.q_wide.cuda()
+        results.append(attend(bt, scale=0.0877 * 2.0 ** by[2]))
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
