@@ -171,7 +171,7 @@ cudaError_t launch_rows(const Plan& pl, const AttendParams& p, cudaStream_t st) 
     if (pl.cluster != 0) return launch(paged_rows_kernel<D, NB, BF, KIND, true, 4>, grid, 128, 0, st, p, kClusterBlocks);
     const cudaError_t e = launch(paged_rows_kernel<D, NB, BF, KIND, false, 4>, grid, 128, 0, st, p);
     if (e != cudaSuccess || !p.split) return e;
-    return launch(paged_join_kernel<8 * NB, 8 * NB, D, BF, true>, dim3(p.max_blocks, 8 * NB), 256, 0, st, p);
+    return launch(paged_join_kernel<8 * NB, 8 * NB, D, BF, true, KIND == SASQ_KV_INT4>, dim3(p.max_blocks, 8 * NB), 256, 0, st, p);
 }
 template <int D, bool BF, int KIND>
 cudaError_t launch_few(const Plan& pl, const AttendParams& p, cudaStream_t st) {
@@ -253,7 +253,7 @@ cudaError_t launch_tiles(const AttendParams& p, const sasq_kv_cache_t* c, int ma
     cfg.numAttrs = 1;
     e = cudaLaunchKernelEx(&cfg, paged_tiles_kernel<D, BF, KIND>, map_q, map_k, map_v, p);
     if (e != cudaSuccess || !p.split) return e;
-    return launch(paged_join_kernel<256, 128, D, BF, false>, dim3(p.max_blocks, join_rows(p, max_rows)), 256, 0, st, p);
+    return launch(paged_join_kernel<256, 128, D, BF, false, KIND == SASQ_KV_INT4>, dim3(p.max_blocks, join_rows(p, max_rows)), 256, 0, st, p);
 }
 
 template <int D, bool BF>

@@ -752,7 +752,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
 // and in the first slots of the blocks after it.  R rows of a slot, in row tiles of TILE of which an item may use fewer.
 // WIDE: a block per row, its eight warps taking the parts in turn (few rows, long keys: up to hundreds of parts); else a
 // warp per row (many rows, two or three parts).  The order of additions is fixed either way.
-template <int R, int TILE, int D, bool BF, bool WIDE>
+template <int R, int TILE, int D, bool BF, bool WIDE, bool INT4>
 __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttendParams p) {
     constexpr int N = D / 32;                                  // elements of a lane
     __shared__ float warp_m[8], warp_sum[8];
@@ -825,14 +825,15 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
         const long long t = pi.first_token + tok;
         uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + t * p.out_stride + (long long)head * D + lane * N);
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] *= inv;
-        if (p.c.kind == SASQ_KV_INT4) {
-            const float* f = p.c.v_scale + pi.h * D + lane * N;
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] *= factor4(__ldg(f + e));
+        for (int e = 0; e < N / 2; ++e) {
+            float2 y = make_float2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+            if constexpr (INT4) {
+                const float2 f = __ldg(reinterpret_cast<const float2*>(p.c.v_scale + pi.h * D + lane * N + 2 * e));
+                y.x *= factor4(f.x);
+                y.y *= factor4(f.y);
+            }
+            dst[e] = narrow2<BF>(y.x, y.y);
         }
-#pragma unroll
-        for (int e = 0; e < N / 2; ++e) dst[e] = narrow2<BF>(acc[2 * e], acc[2 * e + 1]);
         if (lane == 0 && p.lse != nullptr)
             p.lse[t * p.heads + head] = sum != 0.0f ? (m + log2f(sum)) * 0.6931471805599453f : -INFINITY;
     }
