@@ -349,15 +349,16 @@ SASQ_API int sasq_static_w8a8_linear_tiles(int64_t T, int64_t N, int num_pairs, 
  * each.  Groups are `group` consecutive columns; c[n,k] in [-8, 7] are codes of Eq. 1 with b = 4:
  *   y[t,n] = narrow( sum_g s[n,g] * sum_{k in group g} x[t,k] c[n,k] (+ bias[n]) )      sums in fp32 (order
  *                                                                                     unspecified, but fixed)
- * The products are exact.  For one or two tokens x is first taken to 2^-22 of the largest of its 256 columns (256 i to
- * 256 i + 255), half a step off at most, and a group's sum is exact.
+ * The products are exact.  For one or two tokens x is first rounded to multiples of 2^-21 of the power of two at or below the
+ * largest of its 256 columns (256 i to 256 i + 255), so it is off by at most 2^-22 of that largest, and a group's sum is exact.
  * x: [T, K] of `dt`, as it is.  w: [N, K / 2] bytes, column 2i in the low half of byte i, two's complement.  w_scale:
  * [N, K / group] of `dt`.  bias: [N] of `dt` or NULL, added in fp32.  y: [T, N] of `dt`, must not overlap x.
  * group: 32, 64 or 128, a divisor of K; any N; otherwise SASQ_ERR_UNSUPPORTED (also T > 2^19, N > 2^30, K > 2^24).  Any T
  * is served, 64 tokens at a time: for many tokens the W8A8 linears are the faster ones.  The weights are frozen: w and
  * w_scale are read as soon as the kernel is resident, which can be before an earlier call of this library on the same stream
  * has finished; do not hand over a buffer that such a call is still writing (sasq_quantize_weight_w4 does not let its successor
- * start early).  A non-finite x reaches only its own token's row of y (all of it, for one or two tokens).  No workspace. */
+ * start early).  A non-finite x reaches only its own token's row of y (all of it, for one or two tokens); a w_scale that is
+ * infinite or NaN makes its own column n of y non-finite, and nothing reports it.  No workspace. */
 SASQ_API int sasq_w4_linear(const void* x, const uint8_t* w, const void* w_scale, const void* bias, void* y, int64_t T,
                             int64_t N, int64_t K, int64_t group, int dt, void* stream);
 
@@ -400,7 +401,7 @@ typedef struct {
 /* The sequences of a call (host struct; the arrays are int32 in DEVICE memory and are read when the kernels run, so
  * a captured call follows their values).  The new tokens of all sequences lie one after another in q / k / v / out:
  * sequence b owns rows q_starts[b] ... q_starts[b+1] - 1 (q_starts ascends from >= 0; rows from q_starts[batch] on are
- * padding, neither read nor written).  New token i of a sequence with n new tokens has position
+ * padding: not written, and what they hold does not matter).  New token i of a sequence with n new tokens has position
  *   p = seq_lens[b] - n + i
  * and lives in row p % page_size of page page_table[b][p / page_size].  A token with p < 0 has no place: it is not
  * appended and sees no key. */
@@ -451,8 +452,9 @@ SASQ_API size_t sasq_paged_attention_workspace(const sasq_kv_cache_t* cache, con
  * the probabilities are rounded once, as operands of the second product: to `dt`, over an int8 or 4-bit cache to f16.
  * Bit-identical from run to run for equal host bounds.  Infinities or NaN among a sequence's OWN keys and values are
  * outside the contract: they may reach any row of that sequence, rows that do not see them included.  A NaN in q makes
- * its own (token, head) NaN, out and lse, unless that sees no key.  4-bit cache: q times K's factors is taken, for
- * few rows, to 2^-22 of the (token, head)'s largest; it and the logits have to be finite.
+ * its own (token, head) NaN, out and lse, unless that sees no key.  4-bit cache: q times K's factors is off, for few
+ * rows, by at most 2^-22 of the (token, head)'s largest (steps of 2^-21 of the power of two at or below it); it and the
+ * logits have to be finite.
  * q: as for sasq_rope_kv_append (already rotated); out: [total_q, num_q_heads, head_dim] of `dt`, rows at out_stride;
  * must not alias q.  lse: [total_q, num_q_heads] fp32 (natural logarithm) or NULL.  head_dim: 64 or 128.
  * workspace: >= sasq_paged_attention_workspace() bytes, 16-byte aligned, contents need no initialisation; calls that

@@ -5,7 +5,7 @@
 // of a plain copy's rate) and by the launch for single tokens (2.8 us replayed from a graph).  4096 tokens into an int8 cache
 // (32 + 16 heads of 128, interleaved pairs, tokens first): 28.7 us, 94 MB, 3.3 TB/s; single tokens 3.4 us.  4815 tokens into a
 // 4-bit cache (40 + 16 heads of 128, a factor for each channel): 34.5 us, 124 MB, 3.6 TB/s, bound by instructions; single
-// tokens 3.6 us.
+// tokens 3.7 us.
 #include "paged_common.cuh"
 
 namespace sasq {

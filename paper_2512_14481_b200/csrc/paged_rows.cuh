@@ -142,17 +142,17 @@ constexpr int kRowsBlocksPerSm = NB == 2 ? 2 : D == 128 ? 3 : 4;
 // and into the result for V.  The logic pipe, which runs at
 // half the others' rate, is what a conversion to 16-bit floats would fill.
 //   S: as signed bytes, 16 times the code, eight codes are a shift and two masks, and one s8 product of m16n8k32 takes all of them.
-//      Query times factor becomes an integer, a multiple of 2^-22 of the row's largest (a bf16 or f16 query times a bf16 factor has 16
-//      or 19 bits), whose three digits to the base 256, from -128 to 127, each have their product.  The sums are exact integers of at
+//      Query times factor becomes an integer, in steps of 2^-21 of the power of two at or below the row's largest (a bf16 or f16 query
+//      times a bf16 factor has 16 or 19 bits), whose three digits to the base 256, from -128 to 127, each have their product.  The sums are exact integers of at
 //      most 2^21; they start at the bits of the float 1.5 * 2^23, so that the float they end as is that plus the sum.
 //   O: masked in place, two nibbles are the two halves of an f16 operand (nibbles_low, nibbles_high): six instructions for eight codes
 //      of two keys each.  The nibble stands for code + 8: eight times the sum of the rounded probabilities is taken off again,
 //      which a product with a constant operand adds up.
-// 64 ragged sequences of 30 to 4500 keys, 32/8 heads of 128, bf16, 150 MB: 57 us, 2.6 TB/s, 40 % of a plain copy's rate (78 us with
+// 64 ragged sequences of 30 to 4500 keys, 32/8 heads of 128, bf16, 150 MB: 57.7 us, 2.6 TB/s, 40 % of a plain copy's rate (78 us with
 // the codes as f16 for both products and every key tested; 61 us with the queries' digits in registers).  Bound by a step's chain of instructions at
 // the 12 warps that 168 registers leave an SM: 42 % of the issue slots, 37 % of the logic pipe, 33 % of DRAM's peak are in use, and
 // asking for later keys' lines in L2 changes nothing (58.5 us).  8 sequences of 8000 to
-// 32000 keys: 53 us; one of 1000 keys, 32 heads, in clusters: 8.4 us.
+// 32000 keys: 52 us; one of 1000 keys, 32 heads, in clusters: 8.2 us.
 template <int D, int NB, bool BF, int KIND, bool CLUSTER, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, NB, KIND> : 1) paged_rows_kernel(const __grid_constant__ AttendParams p) {
     constexpr int R = 8 * NB, kThreads = 32 * WARPS;

@@ -274,8 +274,10 @@ __device__ __forceinline__ void store_codes4(uint8_t* tile, int r, int chunk, in
 
 // The warps that fill the ring from an int8 or 4-bit cache (`me` of kConvertThreads): K and V of each unit in turn, in the layout
 // that the 16-bit copies leave: keys along the rows, 128-byte swizzle.  Keys behind the sequence's last are zeros.
-// 4-bit, a chunk of 1024 tokens over 15000 keys, 32/8 heads of 128, bf16: 350 us, 744 TFLOP/s.  Neither the conversion nor its loads
-// bound it (without either the time stays), but the softmax chain at 128 registers a thread, as over int8 codes (305 us).
+// 4-bit, a chunk of 1024 tokens over 15000 keys, 32/8 heads of 128: f16 queries 294 us, bf16 ones 350 us, 744 TFLOP/s (int8 codes
+// 304 us, a 16-bit cache 233 us).  Each of a KV head's 16 items converts the same codes again, beside a softmax at 128 registers a
+// thread.  In the bf16 form neither the conversion of the codes nor their loads bound it (without either the time stays); what
+// converted queries cost it has not been taken apart.
 template <int D, bool BF, int KIND>
 __device__ __forceinline__ void convert_tiles(const AttendParams& p, int me, uint8_t* ring, TileTail* tail) {
     using Shape = TileShape<D>;

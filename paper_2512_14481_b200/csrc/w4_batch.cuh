@@ -12,11 +12,14 @@ namespace {
 // are the tokens; a group's sums leave the tensor core for a buffer of their own in TMEM, from where a thread for each row takes
 // them times the row's factor into its fp32 sums.  A cluster's blocks share a tile's columns, and their sums meet in shared memory.
 //
-// Bound by instructions (64 tokens of 11008 x 4096, groups of 128: 25.8 us, 224 TFLOP/s; 61 of 6144 x 4096, groups of 32: 23.4 us):
-// the conversion of the codes, some 220 a thread and window, and for small groups the way of their sums through TMEM.  Without
-// the loads of codes, tokens and factors the first would take 16 us, without the conversion too 14.
+// 64 tokens of 11008 x 4096, groups of 128: 26.0 us, 222 TFLOP/s; 61 of 6144 x 4096, groups of 32: 23.5 us; 4096 of 4096 x 4096: 350
+// us, 393 TFLOP/s.  Bound by waits between the roles more than by instructions, which fill half of the busy SMs' issue slots (8.5
+// million warp instructions in the second case, on 96 SMs): every group is a round trip of products, commit, load and arrival, a
+// tile begins and ends with a block, and equal shares of a tile leave SMs without one.  Without the loads of codes, tokens and
+// factors the first case would take 16 us, without the conversion (some 220 instructions a thread and window) too 14.
 //
-// Warps 0-7 bring codes and tokens to a ring of shared memory (128-byte swizzle, K-major); then four warps for each 32 tokens, which add up; the last one issues the products.
+// Warps 0-7 bring codes and tokens to a ring of shared memory (128-byte swizzle, K-major); then four warps for each 32 tokens, which
+// add up; the last one issues the products.
 template <int TOKENS>
 struct W4Batch {
     static constexpr int kRows = 128, kWindow = 128, kStages = 4;

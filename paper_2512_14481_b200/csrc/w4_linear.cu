@@ -6,9 +6,10 @@
 // the tokens on the other, so that a weight goes from its byte to the operand in registers, where its group's factor can be
 // applied to the group's sum.  More than 16 tokens go to the tensor cores' fifth generation instead (w4_batch.cuh).
 //
-// Replayed from a graph, weights out of DRAM, bf16, groups of 128: one token of 4096 x 4096 4.5 us (floor 1.3: launch, two round
-// trips to memory, the meeting of the sums), of 22016 x 4096 9.6 us (4.8 TB/s, 75 % of a plain copy's rate); 8 tokens of 11008 x
-// 4096 11.3 us, 16 of 4096 x 4096 10.5 us; 7 of 5120 x 13824, groups of 64, 17.1 us (bound by instructions from 3 tokens on).
+// Replayed from a graph, weights out of DRAM, bf16, groups of 128: one token of 4096 x 4096 5.1 us (floor 1.3: launch, two round
+// trips to memory, the meeting of the sums), of 22016 x 4096 10.2 us (4.6 TB/s, 71 % of a plain copy's rate); 7 tokens of 11008 x
+// 4096 12.0 us, 16 of 4096 x 4096 11.0 us; 7 of 5120 x 13824, groups of 64, 18.5 us (from 3 tokens on the codes' conversion and
+// the tokens' way to shared memory count).
 #include <atomic>
 #include <type_traits>
 
@@ -78,7 +79,8 @@ struct Bits {
 template <bool BF>
 constexpr Bits kBits = BF ? Bits{0x43084308u, 0x43084308u} : Bits{0x64086408u, 0x64806480u};
 
-// Eight codes of a word as 16-bit floats: pairs (0, 4), (2, 6) in lo and (1, 5), (3, 7) in hi.  With the sign bit flipped a nibble
+// Eight codes of a word as 16-bit floats, by the exponent that makes a nibble the low bits of a mantissa (a known way of weight-only
+// kernels; the numbers follow from the formats): pairs (0, 4), (2, 6) in lo and (1, 5), (3, 7) in hi.  With the sign bit flipped a nibble
 // is u = code + 8.  bf16: 128 + u, less 136.  f16: 1024 + u, less 1032; one nibble further up 1024 + 16 u, which a fused
 // multiply-add brings to the code.  5 instructions of the logic pipe, which runs at half the others' rate, for f16, 7 for bf16.
 template <bool BF>
@@ -163,8 +165,8 @@ __device__ __forceinline__ void window_words(uint32_t row_base, int turn, int j,
 //
 // DIGITS (one or two tokens): as 16-bit floats 8 codes cost 5 to 7 instructions of the logic pipe and 4 others.  As signed bytes, 16
 // times the code, they are a shift and two masks, and one s8 product of m16n8k32 takes twice as many of them.  So x becomes
-// integers: in a window of 256 columns a token's values are multiples of a power of two, 2^-22 of the window's largest, whose
-// digits to the base 256, from -128 to 127, are three columns of the product: digit l of token t is column 2 l + t.  A group's
+// integers: in a window of 256 columns a token's values are multiples of a power of two, 2^-21 of that at or below the window's
+// largest, whose digits to the base 256, from -128 to 127, are three columns of the product: digit l of token t is column 2 l + t.  A group's
 // sums are exact integers of at most 2^21; they start at the bits of the float 1.5 * 2, so that the float they end as is that plus
 // the sum times 2^-22.
 // FLOATS (up to 16 tokens): exact products of 16-bit floats in fp32 sums, 32 rows at a time, so that what is read
@@ -176,7 +178,7 @@ template <int TOKENS, int STAGES, int G>
 struct W4Shape {
     static constexpr bool kDigits = TOKENS == 2;
     // Floats' sums and operands take 128 registers: 16 warps of one block share the tokens that two blocks of 8 would each bring
-    // (12 tokens of 11008 x 4096: 14.3 us against 16.0; 61 of 6144 x 4096: 29.3 against 33.9).
+    // (12 tokens of 11008 x 4096: 14.3 us against 16.0).
     static constexpr int kWarps = kDigits ? 8 : 16, kThreads = 32 * kWarps;
     static constexpr int kPerSm = kWarps <= 8 ? 2 : 1;     // blocks of an SM by their registers
     static constexpr int kRows = kDigits ? 16 : 32;        // of a tile
@@ -711,7 +713,10 @@ int cluster_slots(int split, int per_sm, int threads, int sms) {
 }
 
 // How a call is cut: blocks of a cluster, what a block holds at once.  Cost in clocks of an SM's sub-partition: a warp's windows, at
-// the pace of an SM's warps together or of one alone; its share of bringing the tokens to shared memory; the ends.
+// the pace of an SM's warps together or of one alone; its share of bringing the tokens to shared memory; the ends.  The clocks are
+// rough and set by hand.  Against every split and number of blocks an SM, forced, for 1, 2, 7 and 16 tokens of seven matrices: within
+// 1.5 % of the best in 15 of 28 cases, within 6 % in 25, at worst 18 % behind (2 tokens of 6144 x 4096, groups of 64: 8.45 us, one
+// block an SM and no cluster 7.14).
 struct W4Plan {
     int split, pass_tiles, parts, part_windows, clusters;
     size_t smem;
