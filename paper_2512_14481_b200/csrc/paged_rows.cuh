@@ -658,10 +658,12 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 4 ? kRowsBlocksPerSm<D, N
             for (int i = 0; i < 4; ++i) y[i] = acc[i] * inv;
             if constexpr (INT4) {                            // averages of codes meet V's factors: finite where a factor is
                 const float4 f = __ldg(reinterpret_cast<const float4*>(p.c.v_scale + it.h * D + d));
-                y[0] *= factor4(f.x);
-                y[1] *= factor4(f.y);
-                y[2] *= factor4(f.z);
-                y[3] *= factor4(f.w);
+                if (sum != 0.0f) {                           // (+0 stays +0 whatever a factor's sign is)
+                    y[0] *= factor4(f.x);
+                    y[1] *= factor4(f.y);
+                    y[2] *= factor4(f.z);
+                    y[3] *= factor4(f.w);
+                }
             }
             const int row = first_row + r, tok = row / p.group;
             const int head = it.h * p.group + row - tok * p.group;
@@ -829,8 +831,10 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
             float2 y = make_float2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
             if constexpr (INT4) {
                 const float2 f = __ldg(reinterpret_cast<const float2*>(p.c.v_scale + pi.h * D + lane * N + 2 * e));
-                y.x *= factor4(f.x);
-                y.y *= factor4(f.y);
+                if (sum != 0.0f) {
+                    y.x *= factor4(f.x);
+                    y.y *= factor4(f.y);
+                }
             }
             dst[e] = narrow2<BF>(y.x, y.y);
         }

@@ -104,3 +104,12 @@ def test_powers_of_two_cancel(new, q_by, f_by, s_by):
         bt.q = bt.q_wide.cuda()
         results.append(attend(bt, scale=0.0877 * 2.0 ** by[2]))
     assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+
+
+@pytest.mark.parametrize("lens,new,dim", [([1, 40], [2, 2], 128), ([2, 9000], [4, 4], 64), ([3, 9000], [40, 60], 128), ([10, 5], [90, 90], 64)])
+def test_rows_without_keys_are_plus_zero_under_negative_factors(lens, new, dim):
+    bt = R4.Batch(lens, new, 4, 2, dim, 16, torch.bfloat16, seed=3)
+    bt.v_scale = -bt.v_scale
+    out, lse = check(bt)
+    empty = torch.isneginf(lse)
+    assert empty.any() and (out[empty].view(torch.int16) == 0).all()
