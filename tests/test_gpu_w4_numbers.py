@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-import paper_2512_14481_b200 as P  # noqa: F401
+import paper_2512_14481_b200 as P
 from test_gpu_w4_linear import exact, problem, run
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +62,19 @@ def test_a_factor_that_is_not_finite_reaches_no_other_column(T, bad):
     y = run(x, codes, scale, None)
     others = [n for n in range(80) if n not in (33, 79)]
     assert torch.equal(y[:, others], want[:, others]) and not torch.isfinite(y[:, [33, 79]]).any()
+
+
+@pytest.mark.parametrize("T", [1, 2, 3, 9, 17, 33, 70])
+@pytest.mark.parametrize("N,K,group", [(200, 1056, 32), (1000, 4160, 64), (130, 13824, 128)])
+def test_what_ran_before_does_not_show(N, K, group, T):
+    """The same call behind linears of every kind that leave loud numbers, or zeros, in shared memory."""
+    x, codes, scale, bias = problem(T, N, K, group, torch.float16, bias=True)
+    w = torch.randint(0, 256, (19000, 1024), dtype=torch.uint8, device="cuda")
+    w_scale = torch.rand((19000, 32), device="cuda").to(torch.float16)
+    results = []
+    for loud in (1000.0, 0.0):
+        for tokens in (2, 8, 16, 32, 64):
+            before = (torch.randn((tokens, 2048), device="cuda") * loud).to(torch.float16)
+            P.sasq_w4_linear(before, w, w_scale, torch.empty((tokens, 19000), dtype=torch.float16, device="cuda"))
+        results.append(run(x, codes, scale, bias))
+    assert torch.equal(results[0], results[1])
